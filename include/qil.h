@@ -402,6 +402,82 @@ qil_status qil_linear_int_batch(const qil_igemm_desc* descs /*host*/, int count,
                                 size_t workspace_bytes, qil_stream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Operators between the linears of a decoder layer (the Llama-2 backbone of
+ * the OpenVLA deployment, App. A.4.2), for a server that runs several requests
+ * at once.  All tensors are bf16 and contiguous unless said otherwise, sums and
+ * softmax statistics are fp32, results are rounded once.
+ * Requests are packed: the rows of request b are cu_q[b] ... cu_q[b + 1] - 1 of
+ * the token tensors (cu_q [num_seqs + 1] int32 on the device, from 0 to
+ * total_q, not decreasing; a request may have no rows).
+ *
+ * qil_rmsnorm: residual addition and root-mean-square norm.
+ *     h = x + residual (h = x if residual is null);  residual_out = bf16(h)
+ *     v = h / sqrt(sum_k h_k^2 / K + eps) * weight
+ *     y = bf16(v);  s = max |v| / 127 (0 -> 1), qy = clamp(rint(v / s), -128, 127)
+ *   The norm is taken of the fp32 sum, not of residual_out.  qy and scales are
+ *   the operands of qil_linear_w8a8; a code may differ by one from the formula's
+ *   where v / s is within fp32 rounding of a half.
+ *   x, residual, residual_out, y [M][K]   weight [K]   qy [M][K] int8   scales [M] fp32
+ *   At least one of y and qy; scales with qy; residual_out needs a residual and
+ *   may be the residual's (or x's) buffer itself.  K % 8 == 0, K <= 32768 (UNSUPPORTED above).
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also a negative or NaN eps), CUDA.
+ * ---------------------------------------------------------------------- */
+qil_status qil_rmsnorm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, int8_t* qy,
+                       float* scales, int M, int K, float eps, qil_stream_t stream);
+
+/* The paged key / value cache.  k_cache, v_cache [num_pages][num_kv_heads][page_size][head_dim] bf16; cached token j of
+ * request b sits in page block_table[b][j / page_size] (block_table [num_seqs][max_pages] int32), slot j % page_size.
+ * kv_len [num_seqs] int32 counts a request's cached tokens, the new ones of this call among them: new token i of q_len
+ * has position kv_len - q_len + i.  head_dim is 64 or 128, page_size 16, 32, 64 or 128, num_heads a multiple of
+ * num_kv_heads.  Pages named by the table are read and written only if they exist: what a page number outside
+ * [0, num_pages) stands for is unspecified, but nothing outside the caches is touched.  Table entries past a request's
+ * last token are not read as pages.
+ *
+ * qil_rope_append: rotary embedding of the new tokens' queries and keys, and the append of their keys and values.
+ *     (a, b) = (x[i], x[i + head_dim / 2])  ->  (a cos - b sin, b cos + a sin),  cos and sin of cos_sin[position]
+ *   qkv [total_q][(num_heads + 2 num_kv_heads) head_dim]: query heads, key heads, value heads of one fused projection
+ *   cos_sin [max_pos][head_dim] fp32: head_dim / 2 cosines, then as many sines     q_out [total_q][num_heads][head_dim]
+ *   A token whose position is outside [0, max_pos) is not appended and its query is set to zero; one beyond the table's
+ *   max_pages pages, or in a page that does not exist, is not appended.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, CUDA. */
+qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, void* k_cache, void* v_cache, const int* cu_q,
+                           const int* kv_len, const int* block_table, int total_q, int num_seqs, int num_heads,
+                           int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages, int max_pos,
+                           qil_stream_t stream);
+
+/* qil_attn_paged: attention of the new tokens over the cache (append them first).  A new token at position p sees the
+ * cached tokens 0 ... p of its request:
+ *     out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,   k_j, v_j of key head h / (num_heads / num_kv_heads)
+ *   A token that sees nothing (kv_len < q_len) gets zeros.  q, out [total_q][num_heads][head_dim].
+ *   What lies in the caches behind a request's last token, be it infinite or NaN, has no influence.
+ *   max_q_len, max_kv_len: bounds on the requests' q_len and kv_len that the host knows.  They choose how the work is
+ *   split; a request that exceeds them gets unspecified results.
+ *   workspace: qil_attn_paged_workspace_size() bytes, zero-filled once; calls that share it must not overlap.  Its first
+ *   int is a status word (QIL_ERR_TIMEOUT if a bounded device-side wait ran out; see qil_device_status).
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also a scale that is not finite), WORKSPACE, CUDA. */
+size_t qil_attn_paged_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
+                                     int max_q_len, int max_kv_len);
+qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const int* cu_q,
+                          const int* kv_len, const int* block_table, int total_q, int num_seqs, int num_heads,
+                          int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages, int max_q_len,
+                          int max_kv_len, float scale, void* workspace, size_t workspace_bytes, qil_stream_t stream);
+
+/* qil_lora_batch_add: the low-rank side path (qil_lora_side_add) for a batch whose requests bring their own adapters:
+ *     out[m][n] = bf16( y[m][n] + scales[a] sum_j (sum_k x[m][k] A[a][j][k]) B[a][n][j] ),  a = adapter[request of row m]
+ *   x [M][K] with row stride ldx   y, out [M][N] with row strides ldy, ldo (out may be y itself, with the same stride)
+ *   a [num_adapters][rank][K]   b [num_adapters][N][rank]   scales [num_adapters] fp32   adapter [num_seqs] int32
+ *   A request whose adapter is not in [0, num_adapters) has none: out = y.
+ *   The inner product is fp32 in the workspace and enters the second product with 16 significant bits.
+ *   K, N, rank and the strides multiples of 8, rank <= 64 (UNSUPPORTED above; pad smaller ranks with zeros).
+ *   workspace: qil_lora_batch_workspace_size() bytes, no initialisation needed.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA. */
+size_t qil_lora_batch_workspace_size(int M, int num_seqs, int rank);
+qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const void* y, void* out, const int* cu_q,
+                              const int* adapter, const float* scales, int M, int N, int K, int rank, int num_seqs,
+                              int num_adapters, long long ldx, long long ldy, long long ldo, void* workspace,
+                              size_t workspace_bytes, qil_stream_t stream);
+
+/* ------------------------------------------------------------------------
  * Helpers
  * ---------------------------------------------------------------------- */
 const char* qil_status_string(qil_status s);

@@ -19,6 +19,13 @@ SIGNATURES = {
     "qil_linear_w4a16": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
     "qil_lora_side_workspace_size": (_sz, [_i]),
     "qil_lora_side_add": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, C.c_float, _vp, _sz, _vp]),
+    "qil_rmsnorm": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, C.c_float, _vp]),
+    "qil_rope_append": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _i, _vp]),
+    "qil_attn_paged_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
+    "qil_attn_paged": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i, C.c_float, _vp, _sz, _vp]),
+    "qil_lora_batch_workspace_size": (_sz, [_i, _i, _i]),
+    "qil_lora_batch_add": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, C.c_longlong, C.c_longlong,
+                                C.c_longlong, _vp, _sz, _vp]),
     "qil_linear_w4a16_swiglu_workspace_size": (_sz, [_i, _i, _i, _i]),
     "qil_linear_w4a16_swiglu": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _sz, _vp]),
     "qil_linear_w4a16_static_ws": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]),

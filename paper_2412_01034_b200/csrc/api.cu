@@ -1,7 +1,9 @@
 // C ABI of the library: argument validation on the host, then one launcher each.
 #include <atomic>
 
-#include "qil_common.cuh"
+#include <cmath>
+
+#include "layer_common.cuh"
 
 namespace qil {
 
@@ -38,6 +40,21 @@ namespace {
 inline cudaStream_t S(qil_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
 inline bool dtype_ok(int d) { return d == QIL_F32 || d == QIL_BF16 || d == QIL_F16; }
 inline bool layout_ok(int l) { return l == QIL_LAYOUT_CANONICAL || l == QIL_LAYOUT_TILE16 || l == QIL_LAYOUT_STREAM128; }
+// sizes of a paged cache and of the packed requests that use it
+qil_status check_paged(const PagedCache& c) {
+    if (c.total_q <= 0 || c.num_seqs <= 0 || c.num_heads <= 0 || c.num_kv_heads <= 0 || c.num_pages <= 0 || c.max_pages <= 0 ||
+        c.num_heads % c.num_kv_heads != 0)
+        return QIL_ERR_SHAPE;
+    if (c.head_dim != 64 && c.head_dim != 128) return QIL_ERR_UNSUPPORTED;
+    if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128) return QIL_ERR_UNSUPPORTED;
+    // positions, rows of the cache and grid sizes are 32-bit numbers
+    constexpr long long kMost = 0x7FFFFFFF;
+    if ((long long)c.max_pages * c.page_size > kMost || (long long)c.num_pages * c.num_kv_heads * c.page_size > kMost ||
+        (long long)c.total_q * c.num_heads > kMost || c.num_heads + 2LL * c.num_kv_heads > 4096)
+        return QIL_ERR_SHAPE;
+    return QIL_OK;
+}
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool pack_layout_ok(int l) { return l == QIL_LAYOUT_CANONICAL || l == QIL_LAYOUT_TILE16; }
 }  // namespace
 
@@ -245,6 +262,79 @@ qil_status qil_lora_side_add(const void* x, const void* a, const void* b, void* 
     if (!workspace || workspace_bytes < lora_side_workspace(M)) return QIL_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) % 4) return QIL_ERR_ALIGN;
     return launch_lora_side_add(x, a, b, y, M, N, K, rank, scale, workspace, S(stream));
+}
+
+qil_status qil_rmsnorm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, int8_t* qy, float* scales,
+                       int M, int K, float eps, qil_stream_t stream) {
+    if (!x || !weight || (!y && !qy) || (qy && !scales) || (residual_out && !residual)) return QIL_ERR_NULL;
+    if (M <= 0 || K <= 0 || K % 8 != 0) return QIL_ERR_SHAPE;
+    if (!rmsnorm_supported(K) || !(eps >= 0.f)) return QIL_ERR_UNSUPPORTED;
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(residual_out) || !aligned16(y) || !aligned16(qy) ||
+        !aligned4(scales))
+        return QIL_ERR_ALIGN;
+    return launch_rmsnorm(x, residual, weight, residual_out, y, qy, scales, M, K, eps, S(stream));
+}
+
+qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, void* k_cache, void* v_cache, const int* cu_q,
+                           const int* kv_len, const int* block_table, int total_q, int num_seqs, int num_heads, int num_kv_heads,
+                           int head_dim, int page_size, int num_pages, int max_pages, int max_pos, qil_stream_t stream) {
+    if (!qkv || !cos_sin || !q_out || !k_cache || !v_cache || !cu_q || !kv_len || !block_table) return QIL_ERR_NULL;
+    const PagedCache c = {cu_q, kv_len, block_table, total_q, num_seqs, num_heads, num_kv_heads, head_dim, page_size, num_pages, max_pages};
+    const qil_status s = check_paged(c);
+    if (s != QIL_OK) return s;
+    if (max_pos <= 0) return QIL_ERR_SHAPE;
+    if (!aligned16(qkv) || !aligned16(cos_sin) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(cu_q) ||
+        !aligned4(kv_len) || !aligned4(block_table))
+        return QIL_ERR_ALIGN;
+    return launch_rope_append(qkv, cos_sin, q_out, k_cache, v_cache, c, max_pos, S(stream));
+}
+
+size_t qil_attn_paged_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int max_q_len,
+                                     int max_kv_len) {
+    if (total_q <= 0 || num_seqs <= 0 || num_heads <= 0 || num_kv_heads <= 0 || num_heads % num_kv_heads != 0 || head_dim <= 0 ||
+        max_q_len <= 0 || max_kv_len <= 0)
+        return 0;
+    return attn_paged_workspace(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len);
+}
+
+qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const int* cu_q, const int* kv_len,
+                          const int* block_table, int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int page_size,
+                          int num_pages, int max_pages, int max_q_len, int max_kv_len, float scale, void* workspace, size_t workspace_bytes,
+                          qil_stream_t stream) {
+    if (!q || !k_cache || !v_cache || !out || !cu_q || !kv_len || !block_table) return QIL_ERR_NULL;
+    const PagedCache c = {cu_q, kv_len, block_table, total_q, num_seqs, num_heads, num_kv_heads, head_dim, page_size, num_pages, max_pages};
+    const qil_status s = check_paged(c);
+    if (s != QIL_OK) return s;
+    if (max_q_len <= 0 || max_kv_len <= 0) return QIL_ERR_SHAPE;
+    if (!std::isfinite(scale)) return QIL_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace) || !aligned4(cu_q) ||
+        !aligned4(kv_len) || !aligned4(block_table))
+        return QIL_ERR_ALIGN;
+    if (!workspace || workspace_bytes < attn_paged_workspace(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len))
+        return QIL_ERR_WORKSPACE;
+    return launch_attn_paged(q, k_cache, v_cache, out, c, max_q_len, max_kv_len, scale, workspace, S(stream));
+}
+
+size_t qil_lora_batch_workspace_size(int M, int num_seqs, int rank) {
+    if (M <= 0 || num_seqs <= 0 || rank <= 0) return 0;
+    return lora_batch_workspace(M, num_seqs, rank);
+}
+
+qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const void* y, void* out, const int* cu_q, const int* adapter,
+                              const float* scales, int M, int N, int K, int rank, int num_seqs, int num_adapters, long long ldx,
+                              long long ldy, long long ldo, void* workspace, size_t workspace_bytes, qil_stream_t stream) {
+    if (!x || !a || !b || !y || !out || !cu_q || !adapter || !scales) return QIL_ERR_NULL;
+    if (M <= 0 || N <= 0 || K <= 0 || rank <= 0 || num_seqs <= 0 || num_adapters <= 0 || K % 8 != 0 || N % 8 != 0 || rank % 8 != 0)
+        return QIL_ERR_SHAPE;
+    if (ldx < K || ldy < N || ldo < N || ldx % 8 != 0 || ldy % 8 != 0 || ldo % 8 != 0 || (out == y && ldo != ldy)) return QIL_ERR_SHAPE;
+    if (rank > 64) return QIL_ERR_UNSUPPORTED;
+    if ((N + 255) / 256 > 65535) return QIL_ERR_SHAPE;   // (grid size)
+    if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) || !aligned4(cu_q) ||
+        !aligned4(adapter) || !aligned4(scales))
+        return QIL_ERR_ALIGN;
+    if (!workspace || workspace_bytes < lora_batch_workspace(M, num_seqs, rank)) return QIL_ERR_WORKSPACE;
+    return launch_lora_batch_add(x, a, b, y, out, cu_q, adapter, scales, M, N, K, rank, num_seqs, num_adapters, ldx, ldy, ldo, workspace,
+                                 S(stream));
 }
 
 qil_status qil_linear_w4a16_batch(const qil_linear_desc* descs, int count, void* workspace, size_t workspace_bytes,

@@ -1,0 +1,259 @@
+// Low-rank adapters of many requests beside one shared projection (the side path of lora_side.cu for a batch in which every
+// request brings its own adapter, or none):
+//   out[m] = bf16( y[m] + scales[a] * (x[m] A_a^T) B_a^T ),  a = adapter of the request that row m belongs to
+//   A [n][r][K] bf16    B [n][N][r] bf16    rows of request b: cu_q[b] ... cu_q[b+1]
+// Memory bound in both regimes: at decode length the adapters' matrices are what is read, in prompts x and y.  Two kernels:
+//   1. t[slice][m][j] = x . A^T over a slice of K, fp32 in the workspace,
+//   2. out = y + scale t B^T, one pass over y.
+// Rows are cut into tiles per request, so that a tile has one adapter.  The products run on mma.sync (16 x 8 x 16): with a
+// rank of 8 to 64 against two streams of K or N elements per row, a multiply costs nothing next to its operands' bytes.
+// Both kernels take their operands straight from global memory in 16-byte loads and never stage them: the order of a
+// contraction's terms is free, so lane c of four takes 8 neighbouring elements and both operands use the same order; and
+// the columns of a group of four 16 x 8 results are dealt out so that a lane ends up with 8 neighbouring outputs.
+// t is split into two bf16 terms (hi + lo) before it is multiplied: it keeps 16 significant bits.
+#include "layer_common.cuh"
+
+namespace qil {
+
+namespace {
+
+constexpr int kDownWarps = 4, kUpWarps = 8, kMaxSlices = 32;
+
+struct LoraParams {
+    const __nv_bfloat16 *x, *a, *b, *y;
+    __nv_bfloat16* out;
+    float* t;   // [slices][M][rank]
+    const int *cu, *adapter;
+    const float* scales;
+    int M, N, K, rank, num_seqs, num_adapters, slices, slice_blocks;   // a slice is slice_blocks blocks of 32 columns of K
+    long long ldx, ldy, ldo;
+};
+
+// kMT: row tiles of 16 per block; kNR: column tiles of 8 of the rank (the rank padded up to 8, 16, 32 or 64)
+template <int kMT, int kNR>
+__global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const LoraParams p) {
+    __shared__ float part[kDownWarps - 1][kMT * kNR * 4 * 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    int seq, row0, row1;
+    if (!find_tile(p.cu, p.num_seqs, p.M, 16 * kMT, blockIdx.x, seq, row0, row1)) return;
+    const int ad = __ldg(p.adapter + seq);
+    if (ad < 0 || ad >= p.num_adapters) return;
+    const __nv_bfloat16* a = p.a + (size_t)ad * p.rank * p.K;
+    float acc[kMT][kNR][4];
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+        for (int n = 0; n < kNR; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][n][e] = 0.f;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    const int first = blockIdx.y * p.slice_blocks, last = min(first + p.slice_blocks, (p.K + 31) / 32);
+#pragma unroll 2
+    for (int kb = first + warp; kb < last; kb += kDownWarps) {
+        const int k = kb * 32 + c * 8;      // this lane's 8 columns (K is a multiple of 8: all or none of them exist)
+        const bool in = k < p.K;
+        uint4 xv[kMT][2], av[kNR];
+#pragma unroll
+        for (int m = 0; m < kMT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = row0 + 16 * m + 8 * h + g;
+                xv[m][h] = in && row < row1 ? *reinterpret_cast<const uint4*>(p.x + row * p.ldx + k) : zero;
+            }
+#pragma unroll
+        for (int n = 0; n < kNR; ++n) {
+            const int j = 8 * n + g;
+            av[n] = in && j < p.rank ? *reinterpret_cast<const uint4*>(a + (size_t)j * p.K + k) : zero;
+        }
+#pragma unroll
+        for (int m = 0; m < kMT; ++m) {
+            const uint32_t a0[4] = {xv[m][0].x, xv[m][1].x, xv[m][0].y, xv[m][1].y};
+            const uint32_t a1[4] = {xv[m][0].z, xv[m][1].z, xv[m][0].w, xv[m][1].w};
+#pragma unroll
+            for (int n = 0; n < kNR; ++n) {
+                mma16816(acc[m][n], a0, av[n].x, av[n].y);
+                mma16816(acc[m][n], a1, av[n].z, av[n].w);
+            }
+        }
+    }
+    // the warps' parts, added in warp order
+    if (warp > 0) {
+#pragma unroll
+        for (int m = 0; m < kMT; ++m)
+#pragma unroll
+            for (int n = 0; n < kNR; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[warp - 1][((m * kNR + n) * 4 + e) * 32 + lane] = acc[m][n][e];
+    }
+    __syncthreads();
+    if (warp > 0) return;
+    float* t = p.t + (size_t)blockIdx.y * p.M * p.rank;
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+        for (int n = 0; n < kNR; ++n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int w = 0; w < kDownWarps - 1; ++w) acc[m][n][e] += part[w][((m * kNR + n) * 4 + e) * 32 + lane];
+            const int j = 8 * n + 2 * c;
+            if (j < p.rank) {
+                const int row = row0 + 16 * m + g;
+                if (row < row1) *reinterpret_cast<float2*>(t + (size_t)row * p.rank + j) = make_float2(acc[m][n][0], acc[m][n][1]);
+                if (row + 8 < row1) *reinterpret_cast<float2*>(t + (size_t)(row + 8) * p.rank + j) = make_float2(acc[m][n][2], acc[m][n][3]);
+            }
+        }
+}
+
+template <int kMT, int kNR>
+__global__ void __launch_bounds__(32 * kUpWarps) lora_batch_up_kernel(const LoraParams p) {
+    constexpr int kRank = 8 * kNR, kW = kRank / 4, kSteps = kRank <= 16 ? 1 : kRank / 16;   // kW: rank elements of a lane
+    // t as the A operand of the products, in the order of the lanes' registers: [row tile][step][hi, lo][lane][4 words]
+    __shared__ __align__(16) uint32_t frag[kMT * kSteps * 2 * 32 * 4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    int seq, row0, row1;
+    if (!find_tile(p.cu, p.num_seqs, p.M, 16 * kMT, blockIdx.x, seq, row0, row1)) return;
+    const int ad = __ldg(p.adapter + seq);
+    const bool none = ad < 0 || ad >= p.num_adapters;
+    if (none && p.out == p.y) return;
+    const int n0 = (blockIdx.y * kUpWarps + warp) * 32;
+    uint4 bq[4][kW == 16 ? 2 : 1];
+    if (!none) {
+        // B rows of this warp's 32 columns: column (2c, 2c + 1) of result tile i is output n0 + 8 c + 2 i, + 1
+        const __nv_bfloat16* b = p.b + (size_t)ad * p.N * p.rank;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = n0 + 8 * (g >> 1) + 2 * i + (g & 1);
+            const __nv_bfloat16* row = b + (size_t)n * p.rank + kW * c;
+#pragma unroll
+            for (int h = 0; h < (kW == 16 ? 2 : 1); ++h) {
+                bq[i][h] = make_uint4(0u, 0u, 0u, 0u);
+                if (n < p.N && kW * c + 8 * h < p.rank) {
+                    if (kW == 2) bq[i][h].x = *reinterpret_cast<const uint32_t*>(row);
+                    else if (kW == 4) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(row);
+                        bq[i][h].x = v.x;
+                        bq[i][h].y = v.y;
+                    } else bq[i][h] = *reinterpret_cast<const uint4*>(row + 8 * h);
+                }
+            }
+        }
+        const float scale = __ldg(p.scales + ad);
+        for (int i = threadIdx.x; i < kMT * 16 * (kRank / 2); i += blockDim.x) {
+            const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
+            float2 v = make_float2(0.f, 0.f);
+            if (row0 + m < row1 && j < p.rank) {
+                const float* t = p.t + (size_t)(row0 + m) * p.rank + j;
+                for (int s = 0; s < p.slices; ++s) {
+                    const float2 u = *reinterpret_cast<const float2*>(t + (size_t)s * p.M * p.rank);
+                    v.x += u.x;
+                    v.y += u.y;
+                }
+                v.x *= scale;
+                v.y *= scale;
+            }
+            const uint32_t hi = pack2(v.x, v.y);
+            const uint32_t lo = pack2(v.x - __uint_as_float(hi << 16), v.y - __uint_as_float(hi & 0xFFFF0000u));
+            const int at = j % kW, step = at >> 2, reg = ((m & 15) >> 3) + 2 * ((at & 3) >> 1);
+            uint32_t* f = frag + ((((m >> 4) * kSteps + step) * 2) * 32 + (m & 7) * 4 + j / kW) * 4 + reg;
+            f[0] = hi;
+            f[32 * 4] = lo;
+        }
+    }
+    __syncthreads();
+    const int n = n0 + 8 * c;      // this lane's 8 outputs (N is a multiple of 8: all or none of them exist)
+    if (n0 >= p.N) return;
+#pragma unroll
+    for (int m = 0; m < kMT; ++m) {
+        float acc[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
+        if (!none) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(frag + ((((m * kSteps + s) * 2) + part) * 32 + lane) * 4);
+                    const uint32_t a[4] = {v.x, v.y, kW == 2 ? 0u : v.z, kW == 2 ? 0u : v.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 q = bq[i][kW == 16 ? s >> 1 : 0];
+                        if (s & 1) mma16816(acc[i], a, q.z, q.w);
+                        else mma16816(acc[i], a, q.x, kW == 2 ? 0u : q.y);
+                    }
+                }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = row0 + 16 * m + 8 * h + g;
+            if (row < row1 && n < p.N) {
+                float o[8];
+                unpack8(*reinterpret_cast<const uint4*>(p.y + row * p.ldy + n), o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    o[2 * i] += acc[i][2 * h];
+                    o[2 * i + 1] += acc[i][2 * h + 1];
+                }
+                *reinterpret_cast<uint4*>(p.out + row * p.ldo + n) = pack8(o);
+            }
+        }
+    }
+}
+
+// Row tiles of 16 per block.  A tile wastes what its request does not fill, so a batch of single tokens takes tiles of 16;
+// prompts take 64 (32 at rank 64, for the accumulators' registers): the adapter is read once per tile.
+int lora_row_tiles(int M, int num_seqs, int rank) {
+    if (M <= 16 * num_seqs) return 1;
+    return rank > 32 ? 2 : 4;
+}
+int lora_max_tiles(int M, int num_seqs, int rank) { return M / (16 * lora_row_tiles(M, num_seqs, rank)) + num_seqs; }
+
+// Slices of K for the first kernel: two blocks per SM where the row tiles alone are fewer, at least 256 columns each.
+int lora_batch_slices(int M, int num_seqs, int rank, int K) {
+    const int tiles = lora_max_tiles(M, num_seqs, rank);
+    int s = (2 * num_sms() + tiles - 1) / tiles;
+    s = s < K / 256 ? s : K / 256;
+    s = s < kMaxSlices ? s : kMaxSlices;
+    return s < 1 ? 1 : s;
+}
+
+}  // namespace
+
+size_t lora_batch_workspace(int M, int num_seqs, int rank) {
+    return (size_t)lora_batch_slices(M, num_seqs, rank, 1 << 30) * M * rank * sizeof(float);
+}
+
+qil_status launch_lora_batch_add(const void* x, const void* a, const void* b, const void* y, void* out, const int* cu_q, const int* adapter,
+                                 const float* scales, int M, int N, int K, int rank, int num_seqs, int num_adapters, long long ldx,
+                                 long long ldy, long long ldo, void* ws, cudaStream_t st) {
+    LoraParams p;
+    p.x = reinterpret_cast<const __nv_bfloat16*>(x);
+    p.a = reinterpret_cast<const __nv_bfloat16*>(a);
+    p.b = reinterpret_cast<const __nv_bfloat16*>(b);
+    p.y = reinterpret_cast<const __nv_bfloat16*>(y);
+    p.out = reinterpret_cast<__nv_bfloat16*>(out);
+    p.t = reinterpret_cast<float*>(ws);
+    p.cu = cu_q; p.adapter = adapter; p.scales = scales;
+    p.M = M; p.N = N; p.K = K; p.rank = rank; p.num_seqs = num_seqs; p.num_adapters = num_adapters;
+    p.ldx = ldx; p.ldy = ldy; p.ldo = ldo;
+    const int blocks = (K + 31) / 32;
+    p.slices = lora_batch_slices(M, num_seqs, rank, K);
+    p.slice_blocks = (blocks + p.slices - 1) / p.slices;
+    p.slices = (blocks + p.slice_blocks - 1) / p.slice_blocks;
+    const unsigned tiles = (unsigned)lora_max_tiles(M, num_seqs, rank);
+    const dim3 down(tiles, (unsigned)p.slices), up(tiles, (unsigned)((N + 32 * kUpWarps - 1) / (32 * kUpWarps)));
+    auto go = [&](auto kd, auto ku) {
+        kd<<<down, 32 * kDownWarps, 0, st>>>(p);
+        ku<<<up, 32 * kUpWarps, 0, st>>>(p);
+    };
+    const int mt = lora_row_tiles(M, num_seqs, rank);
+    if (rank <= 8) mt == 1 ? go(lora_batch_down_kernel<1, 1>, lora_batch_up_kernel<1, 1>) : go(lora_batch_down_kernel<4, 1>, lora_batch_up_kernel<4, 1>);
+    else if (rank <= 16) mt == 1 ? go(lora_batch_down_kernel<1, 2>, lora_batch_up_kernel<1, 2>) : go(lora_batch_down_kernel<4, 2>, lora_batch_up_kernel<4, 2>);
+    else if (rank <= 32) mt == 1 ? go(lora_batch_down_kernel<1, 4>, lora_batch_up_kernel<1, 4>) : go(lora_batch_down_kernel<4, 4>, lora_batch_up_kernel<4, 4>);
+    else mt == 1 ? go(lora_batch_down_kernel<1, 8>, lora_batch_up_kernel<1, 8>) : go(lora_batch_down_kernel<2, 8>, lora_batch_up_kernel<2, 8>);
+    return launch_status();
+}
+
+}  // namespace qil
