@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libqil.so")
 SOURCES = ["api.cu", "quantize.cu", "w4a16_general.cu", "w4a16_skinny.cu", "w4a4.cu", "ref_gemv.cu",
            "w4a16_static_ws.cu", "w4a16_tc.cu", "w4a16_prefill.cu", "w8a16.cu", "probe_mma.cu", "igemm_list.cu", "lora_side.cu",
-           "rmsnorm.cu", "rope_cache.cu", "attn_paged.cu", "lora_batch.cu"]
+           "rmsnorm.cu", "rope_cache.cu", "attn_paged.cu", "attn_few.cu", "attn_many.cu", "lora_batch.cu"]
 
 
 def _nvcc() -> str:

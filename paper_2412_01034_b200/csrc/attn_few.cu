@@ -1,0 +1,306 @@
+// Attention over the paged cache for requests with few query rows (new tokens x heads of a group <= 16): single tokens and
+// short drafts.  Memory bound: every cached key and value of a request is read once per key head, 4 D bytes a token, and
+// the query rows are one 16-row operand.
+//
+// A block takes `chunk` cached tokens of one request and key head; its four warps take tiles of 16 tokens in turn and are
+// independent of one another: each has its own ring of tiles in shared memory (cp.async, 16-byte pieces, the pieces of a
+// row permuted by row % 8 so that ldmatrix reads every bank once), its own running maximum and sum, and its own
+// accumulators, so that the loop has no block-wide barrier.  S = Q K^T and O += P V run on mma.sync 16 x 8 x 16: the
+// tensor pipe is idle most of the time here and the multiply-adds of up to 16 rows cost the same as those of one.
+// A page holds a multiple of 16 tokens, so a tile lies in one page.  Tokens behind the last one arrive as zeros (cp.async
+// with a source size of zero), so that whatever the page holds there never meets a weight of zero.
+// The warps' results are joined in shared memory.  Where a request has several blocks, each writes its part (fp32, with
+// maximum and sum) to the workspace, and the block that counts itself in last adds the parts in the order of the blocks.
+#include "attn_paged.cuh"
+
+namespace qil {
+
+namespace {
+
+constexpr int kWarps = 4, kTile = 16;
+
+template <int kDim>
+struct FewShape {
+    static constexpr int kTileBytes = kTile * kDim * 2;
+    static constexpr int kStages = kDim == 128 ? 3 : 6;
+    static constexpr int kWarpBytes = kStages * 2 * kTileBytes;
+    static constexpr int kSmem = kWarps * kWarpBytes;
+    static_assert(kWarps * kTile * kDim * 4 <= kSmem, "the warps' results fit where the rings were");
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+
+template <int kDim>
+__global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams p) {
+    using Shape = FewShape<kDim>;
+    constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kPieces = kDim / 8;   // 16-byte pieces of a row
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float s_m[kWarps][16], s_l[kWarps][16];
+    __shared__ float s_scale[2][16];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
+    int row0, row1;
+    request_rows(p.c.cu_q, seq, p.c.total_q, row0, row1);
+    const int q_len = row1 - row0;
+    if (q_len <= 0 || q_len * (long long)G > kFewRows) return;
+    const int rows = q_len * G, end = cache_end(p.c, seq), first_pos = __ldg(p.c.kv_len + seq) - q_len;
+    const int parts = max(1, min((end + p.chunk - 1) / p.chunk, p.slots));
+    if (split >= parts) return;
+    const int begin = split * p.chunk, stop = split + 1 == parts ? end : min(begin + p.chunk, end);
+    const int tiles = (stop - begin + kTile - 1) / kTile;
+    const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
+
+    // the query rows as the A operand: lane (g, c) holds rows g, g + 8, columns 16 k + 2 c ..., 16 k + 8 + 2 c ...
+    uint32_t qa[kDim / 16][4];
+#pragma unroll
+    for (int k = 0; k < kDim / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = g + 8 * (e & 1), d = 16 * k + 2 * c + 8 * (e >> 1);
+            qa[k][e] = r < rows ? *reinterpret_cast<const uint32_t*>(p.q + ((size_t)(row0 + r / G) * H + kvh * G + r % G) * kDim + d) : 0u;
+        }
+    // visible tokens of this lane's two rows
+    int see[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) see[h] = g + 8 * h < rows ? min(first_pos + (g + 8 * h) / G + 1, end) : 0;
+    const int all_see = min(first_pos + 1, end);   // every row sees what the first new token sees
+
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * Shape::kWarpBytes;
+    auto page_of = [&](int i) -> int {   // page of tile i (-1: none)
+        const int tok = begin + i * kTile;
+        return tok < stop ? __ldg(table + tok / p.c.page_size) : -1;
+    };
+    auto fetch = [&](int i, int stage, int page) {
+        const int tok = begin + i * kTile;
+        const bool there = page >= 0 && page < p.c.num_pages;
+        const size_t at = there ? (((size_t)page * p.c.num_kv_heads + kvh) * p.c.page_size + tok % p.c.page_size) * kDim : 0;
+        const uint32_t dst = ring + stage * 2 * kTileBytes;
+#pragma unroll
+        for (int j = 0; j < kTile * kPieces / 32; ++j) {
+            const int piece = j * 32 + lane, r = piece / kPieces, o = piece % kPieces;
+            const uint32_t to = dst + r * (kDim * 2) + ((o & ~7) | ((o ^ r) & 7)) * 16;
+            const uint32_t bytes = there && tok + r < stop ? 16u : 0u;
+            cp_async16(to, p.k + at + piece * 8, bytes);
+            cp_async16(to + kTileBytes, p.v + at + piece * 8, bytes);
+        }
+    };
+
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float o[kDim / 8][4];
+#pragma unroll
+    for (int n = 0; n < kDim / 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+
+    int ahead = warp;               // the next tile to fetch
+    int page = page_of(ahead);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+        if (ahead < tiles) {
+            const int next = page_of(ahead + kWarps);
+            fetch(ahead, s, page);
+            page = next;
+        }
+        ahead += kWarps;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    int stage = 0, into = kStages - 1;
+    // ldmatrix addresses: lane i supplies row i % 16 (keys: tokens; values: tokens), column half i / 16
+    const int lrow = lane & 15, lhalf = lane >> 4;
+    for (int i = warp; i < tiles; i += kWarps) {
+        __syncwarp();               // every lane has read the tile that the next fetch overwrites
+        if (ahead < tiles) {
+            const int next = page_of(ahead + kWarps);   // (asked for one tile ahead of its use)
+            fetch(ahead, into, page);
+            page = next;
+        }
+        ahead += kWarps;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+        const uint32_t kt = ring + stage * 2 * kTileBytes, vt = kt + kTileBytes;
+        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int k = 0; k < kDim / 16; ++k) {
+            // matrices: tokens 0-7 / 8-15 at columns 16 k, then the same at 16 k + 8
+            const int piece = 2 * k + lhalf;
+            uint32_t b[4];
+            ldsm4(b, kt + lrow * (kDim * 2) + ((piece & ~7) | ((piece ^ lrow) & 7)) * 16);
+            mma16816(s[0], qa[k], b[0], b[2]);
+            mma16816(s[1], qa[k], b[1], b[3]);
+        }
+        const int tok = begin + i * kTile;
+        float top[2] = {-INFINITY, -INFINITY};
+        const bool masked = tok + kTile > all_see;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] *= p.scale_log2;
+                if (masked && tok + 8 * n + 2 * c + (e & 1) >= see[e >> 1]) s[n][e] = -INFINITY;
+                top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
+            }
+        uint32_t pa[4];
+        float keep[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float now = fmaxf(m[h], quad_max(top[h]));
+            const float ref = now == -INFINITY ? 0.f : now;
+            keep[h] = fast_exp2(m[h] - ref);
+            m[h] = now;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) s[n][2 * h + e] = fast_exp2(s[n][2 * h + e] - ref);
+            l[h] = l[h] * keep[h] + ((s[0][2 * h] + s[0][2 * h + 1]) + (s[1][2 * h] + s[1][2 * h + 1]));
+        }
+        // the weights are rounded to bf16 for the product with V (the sum keeps them in fp32)
+        pa[0] = pack2(s[0][0], s[0][1]);
+        pa[1] = pack2(s[0][2], s[0][3]);
+        pa[2] = pack2(s[1][0], s[1][1]);
+        pa[3] = pack2(s[1][2], s[1][3]);
+        if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
+#pragma unroll
+            for (int n = 0; n < kDim / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] *= keep[e >> 1];
+        }
+#pragma unroll
+        for (int n = 0; n < kDim / 16; ++n) {
+            // matrices: tokens 0-7 / 8-15 at columns 16 n, then the same at 16 n + 8, transposed
+            const int piece = 2 * n + lhalf;
+            uint32_t b[4];
+            ldsm4t(b, vt + lrow * (kDim * 2) + ((piece & ~7) | ((piece ^ lrow) & 7)) * 16);
+            mma16816(o[2 * n], pa, b[0], b[1]);
+            mma16816(o[2 * n + 1], pa, b[2], b[3]);
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        into = into + 1 == kStages ? 0 : into + 1;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+
+    // join the warps: maxima and sums first, then the accumulators where the rings were
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        l[h] = quad_sum(l[h]);
+        if (c == 0) {
+            s_m[warp][g + 8 * h] = m[h];
+            s_l[warp][g + 8 * h] = l[h];
+        }
+    }
+    __syncthreads();
+    float* so = reinterpret_cast<float*>(smem) + (size_t)warp * kTile * kDim;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = g + 8 * h;
+        float most = s_m[0][r];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) most = fmaxf(most, s_m[w][r]);
+        const float f = m[h] == -INFINITY ? 0.f : fast_exp2(m[h] - most);
+        if (r < rows) {
+#pragma unroll
+            for (int n = 0; n < kDim / 8; ++n)
+                *reinterpret_cast<float2*>(so + r * kDim + 8 * n + 2 * c) = make_float2(o[n][2 * h] * f, o[n][2 * h + 1] * f);
+        }
+    }
+    if (tid < 16) {
+        float most = s_m[0][tid], sum = 0.f;
+        for (int w = 1; w < kWarps; ++w) most = fmaxf(most, s_m[w][tid]);
+        for (int w = 0; w < kWarps; ++w)
+            if (s_m[w][tid] != -INFINITY) sum += s_l[w][tid] * fast_exp2(s_m[w][tid] - most);
+        s_scale[0][tid] = most;
+        s_scale[1][tid] = sum;
+    }
+    __syncthreads();
+    const float* all = reinterpret_cast<const float*>(smem);
+    auto joined = [&](int at) -> float2 {
+        float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float2 u = *reinterpret_cast<const float2*>(all + (size_t)w * kTile * kDim + at);
+            v.x += u.x;
+            v.y += u.y;
+        }
+        return v;
+    };
+    auto write = [&](int at, float2 v, float sum) {
+        const int r = at / kDim, d = at % kDim;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<uint32_t*>(p.out + ((size_t)(row0 + r / G) * H + kvh * G + r % G) * kDim + d) = pack2(v.x * inv, v.y * inv);
+    };
+    if (parts == 1) {
+        for (int at = 2 * tid; at < rows * kDim; at += 2 * blockDim.x) write(at, joined(at), s_scale[1][at / kDim]);
+        return;
+    }
+    // a part: few_rows x kDim accumulators, then few_rows maxima and few_rows sums
+    const size_t part_floats = (size_t)p.few_rows * (kDim + 2);
+    float* mine = p.parts + (((size_t)seq * p.c.num_kv_heads + kvh) * p.slots + split) * part_floats;
+    for (int at = 2 * tid; at < rows * kDim; at += 2 * blockDim.x) *reinterpret_cast<float2*>(mine + at) = joined(at);
+    if (tid < rows) {
+        mine[p.few_rows * kDim + tid] = s_scale[0][tid];
+        mine[p.few_rows * (kDim + 1) + tid] = s_scale[1][tid];
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) s_last = atomicAdd(p.counters + seq * p.c.num_kv_heads + kvh, 1) == parts - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    if (tid == 0) p.counters[seq * p.c.num_kv_heads + kvh] = 0;
+    const float* first = mine - (size_t)split * part_floats;
+    for (int at = 2 * tid; at < rows * kDim; at += 2 * blockDim.x) {
+        const int r = at / kDim;
+        float most = -INFINITY, sum = 0.f;
+        for (int s = 0; s < parts; ++s) most = fmaxf(most, __ldcg(first + s * part_floats + p.few_rows * kDim + r));
+        float2 v = make_float2(0.f, 0.f);
+        for (int s = 0; s < parts; ++s) {
+            const float* q = first + s * part_floats;
+            const float ms = __ldcg(q + p.few_rows * kDim + r);
+            if (ms == -INFINITY) continue;
+            const float f = fast_exp2(ms - most);
+            const float2 u = __ldcg(reinterpret_cast<const float2*>(q + at));
+            sum = fmaf(__ldcg(q + p.few_rows * (kDim + 1) + r), f, sum);
+            v.x = fmaf(u.x, f, v.x);
+            v.y = fmaf(u.y, f, v.y);
+        }
+        write(at, v, sum);
+    }
+}
+
+}  // namespace
+
+qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) {
+    const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)p.c.num_seqs);
+    cudaError_t e;
+    if (p.c.head_dim == 128) {
+        e = cudaFuncSetAttribute(attn_few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<128>::kSmem);
+        if (e == cudaSuccess) attn_few_kernel<128><<<grid, 32 * kWarps, FewShape<128>::kSmem, st>>>(p);
+    } else {
+        e = cudaFuncSetAttribute(attn_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<64>::kSmem);
+        if (e == cudaSuccess) attn_few_kernel<64><<<grid, 32 * kWarps, FewShape<64>::kSmem, st>>>(p);
+    }
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return QIL_ERR_CUDA;
+    }
+    return launch_status();
+}
+
+}  // namespace qil

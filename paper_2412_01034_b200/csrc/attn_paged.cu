@@ -1,70 +1,92 @@
-// Attention of the new tokens of many requests over a paged cache, causal, grouped heads.
+// Attention of the new tokens of many requests over a paged cache, causal, grouped heads: which kernel takes which
+// requests, and how the work is split.
 //   request b: q_len new tokens (rows cu_q[b] ... cu_q[b+1] of q), kv_len cached tokens with the new ones among them
 //   new token i of a request has position p = kv_len - q_len + i and sees the cached tokens j <= p
 //   o = sum_j softmax_j(scale q . k_j) v_j;  a token that sees nothing (p < 0) gets zeros
-#include "layer_common.cuh"
+// The lengths are on the device; the host knows their bounds.  Requests of at most 16 query rows per key head go to
+// attn_few.cu, the others to attn_many.cu; a launch is left out where the bounds show that it would find nothing.
+#include "attn_paged.cuh"
 
 namespace qil {
 
 namespace {
 
-// One warp per (token, head): the cached tokens one after another, lanes over the head's dimension.
-template <int kDim>
-__global__ void __launch_bounds__(128) attn_rows_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ k_cache,
-                                                        const __nv_bfloat16* __restrict__ v_cache, __nv_bfloat16* __restrict__ out,
-                                                        PagedCache c, float scale_log2) {
-    constexpr int kPer = kDim / 32;
-    const int lane = threadIdx.x & 31;
-    const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (item >= (long long)c.total_q * c.num_heads) return;
-    const int t = (int)(item / c.num_heads), head = (int)(item % c.num_heads), kvh = head / (c.num_heads / c.num_kv_heads);
-    const int seq = request_of_row(c.cu_q, c.num_seqs, t);
-    int pos = -1;
-    if (seq < c.num_seqs) {
-        int lo, hi;
-        request_rows(c.cu_q, seq, c.total_q, lo, hi);
-        const int kv = min(max(__ldg(c.kv_len + seq), 0), c.max_pages * c.page_size);
-        pos = kv - (hi - lo) + (t - lo);
+struct AttnPlan {
+    bool few, many;
+    int chunk, slots, few_rows, splits;
+    size_t counter_bytes, part_floats;
+};
+
+AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, int max_kv) {
+    AttnPlan pl = {};
+    const int G = H / Hk;
+    const long long sms = num_sms();
+    if (max_q > total_q) max_q = total_q;
+    pl.many = (long long)max_q * G > kFewRows;
+    // every request has more than kFewRows rows if the others at their longest leave more for it
+    pl.few = !(((long long)total_q - (long long)(num_seqs - 1) * max_q) * G > kFewRows);
+    if (pl.few) {
+        // Two blocks fit an SM.  Up to one round of blocks where the requests are few; about eight rounds, of at most 1024
+        // tokens each, where they are many (their lengths differ, and the rounds even that out).
+        const long long items = (long long)num_seqs * Hk, room = 2 * sms;
+        const long long blocks = items * 2 <= room ? room : 8 * room;
+        long long chunk = (max_kv * items + blocks - 1) / blocks;
+        chunk = (chunk + 63) / 64 * 64;
+        if (items * 2 > room && chunk > 1024) chunk = 1024;
+        pl.chunk = (int)chunk;
+        pl.slots = (int)((max_kv + chunk - 1) / chunk);
+        const long long rows = (long long)max_q * G;
+        pl.few_rows = (int)(rows < kFewRows ? rows : kFewRows);
+        pl.counter_bytes = ((size_t)items * sizeof(int) + 255) & ~(size_t)255;
+        if (pl.slots > 1) pl.part_floats = (size_t)items * pl.slots * pl.few_rows * (D + 2);
     }
-    float qv[kPer], o[kPer], m = -INFINITY, l = 0.f;
-    for (int i = 0; i < kPer; ++i) {
-        qv[i] = __bfloat162float(q[item * kDim + lane * kPer + i]) * scale_log2;
-        o[i] = 0.f;
+    if (pl.many) {
+        // The cache is split where the row tiles alone leave SMs idle, into parts of at least four tiles of 128 tokens.
+        const long long tiles = ((long long)total_q * G + 255) / 256 * Hk;
+        long long s = sms / tiles;
+        if (s > (max_kv + 511) / 512) s = (max_kv + 511) / 512;
+        pl.splits = s < 1 ? 1 : (int)s;
+        if (pl.splits > 1) {
+            const size_t need = (size_t)pl.splits * total_q * H * (D + 2);
+            if (need > pl.part_floats) pl.part_floats = need;
+        }
     }
-    for (int j = 0; j <= pos; ++j) {
-        const int page = __ldg(c.block_table + (size_t)seq * c.max_pages + j / c.page_size);
-        if (page < 0 || page >= c.num_pages) continue;
-        const size_t at = (((size_t)page * c.num_kv_heads + kvh) * c.page_size + j % c.page_size) * kDim + lane * kPer;
-        float s = 0.f;
-        for (int i = 0; i < kPer; ++i) s = fmaf(qv[i], __bfloat162float(k_cache[at + i]), s);
-        s = warp_sum(s);
-        const float top = fmaxf(m, s), keep = exp2f(m - top), p = exp2f(s - top);
-        m = top;
-        l = l * keep + p;
-        for (int i = 0; i < kPer; ++i) o[i] = fmaf(p, __bfloat162float(v_cache[at + i]), o[i] * keep);
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    for (int i = 0; i < kPer; ++i) out[item * kDim + lane * kPer + i] = __float2bfloat16_rn(o[i] * inv);
+    return pl;
 }
+
+constexpr size_t kHeader = 256;   // status word
 
 }  // namespace
 
 size_t attn_paged_workspace(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int max_q_len, int max_kv_len) {
-    return 16;
+    const AttnPlan pl = plan_attn(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len);
+    return kHeader + pl.counter_bytes + pl.part_floats * sizeof(float);
 }
 
 qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const PagedCache& c, int max_q_len,
                              int max_kv_len, float scale, void* ws, cudaStream_t st) {
-    const long long items = (long long)c.total_q * c.num_heads;
-    const float s2 = scale * 1.4426950408889634f;
-    auto go = [&](auto kernel) {
-        kernel<<<(unsigned)((items + 3) / 4), 128, 0, st>>>(
-            reinterpret_cast<const __nv_bfloat16*>(q), reinterpret_cast<const __nv_bfloat16*>(k_cache),
-            reinterpret_cast<const __nv_bfloat16*>(v_cache), reinterpret_cast<__nv_bfloat16*>(out), c, s2);
-    };
-    if (c.head_dim == 128) go(attn_rows_kernel<128>);
-    else go(attn_rows_kernel<64>);
-    return launch_status();
+    const AttnPlan pl = plan_attn(c.total_q, c.num_seqs, c.num_heads, c.num_kv_heads, c.head_dim, max_q_len, max_kv_len);
+    AttnParams p;
+    p.q = reinterpret_cast<const __nv_bfloat16*>(q);
+    p.k = reinterpret_cast<const __nv_bfloat16*>(k_cache);
+    p.v = reinterpret_cast<const __nv_bfloat16*>(v_cache);
+    p.out = reinterpret_cast<__nv_bfloat16*>(out);
+    p.c = c;
+    p.G = c.num_heads / c.num_kv_heads;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.chunk = pl.chunk;
+    p.slots = pl.slots;
+    p.few_rows = pl.few_rows;
+    p.splits = pl.splits;
+    char* base = static_cast<char*>(ws);
+    p.status = reinterpret_cast<int*>(base);
+    p.counters = reinterpret_cast<int*>(base + kHeader);
+    p.parts = reinterpret_cast<float*>(base + kHeader + pl.counter_bytes);
+    if (pl.few) {
+        const qil_status s = launch_attn_few(p, st);
+        if (s != QIL_OK) return s;
+    }
+    return pl.many ? launch_attn_many(p, st) : QIL_OK;
 }
 
 }  // namespace qil
