@@ -7,7 +7,6 @@ turned into an exception.  All arithmetic runs in the CUDA kernels.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 
 import torch
 
@@ -358,30 +357,33 @@ def probe_mma(kind: str, iters: int, commit_every: int = 8, status=None, stream=
 
 # ------------------------------------------------------------------------------------------------------------------
 # operators between the linears of a decoder layer, for packed requests (rows of request b: cu_q[b] ... cu_q[b + 1] - 1)
-# (each also takes stream=s: the call and the tensors it makes belong to stream s)
+# (stream=s: the whole call, with the tensors that it makes and fills, happens on s)
 # ------------------------------------------------------------------------------------------------------------------
 _BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
+# The handle of the current stream without the Stream object that torch.cuda.current_stream() makes around it (3 us of a
+# 10 us call); the raw getter takes the device's index.
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _arg(name, t, dtype, *shape):
-    """The device address of a contiguous CUDA tensor of the given type and shape (None: any size)."""
+def _refuse(name, t, dtype, shape):
     if t.dtype is not dtype:
-        raise ValueError(f"qil: {name} is {t.dtype}, expected {dtype}")
-    got = t.shape
-    if len(got) != len(shape):
-        raise ValueError(f"qil: {name} has shape {tuple(got)}, expected {len(shape)} dimensions")
-    for n, want in zip(got, shape):
-        if n != want and want is not None:
-            raise ValueError(f"qil: {name} has shape {tuple(got)}, expected {shape}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"qil: {name} has to be a contiguous CUDA tensor")
-    return t.data_ptr()
+        raise ValueError(f"qil: {name} is {t.dtype}, expected {str(dtype).removeprefix('torch.')}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"qil: {name} has shape {tuple(t.shape)}, expected {shape}")
+    raise ValueError(f"qil: {name} has to be a contiguous CUDA tensor")
+
+
+def _arg(name, t, dtype, shape):
+    """The device address of a contiguous CUDA tensor of the given type and shape."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _refuse(name, t, dtype, shape)
 
 
 def _arg_rows(name, t, rows, cols):
     """As _arg for a bf16 matrix whose rows may be part of longer ones: (address, row stride)."""
-    if t.dtype is not _BF16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"qil: {name} is {t.dtype} {tuple(t.shape)}, expected bfloat16 {(rows, cols)}")
+    if t.dtype is not _BF16 or t.shape != (rows, cols):
+        _refuse(name, t, _BF16, (rows, cols))
     if not t.is_cuda or (cols > 1 and t.stride(1) != 1):
         raise ValueError(f"qil: the rows of {name} have to be contiguous, on a CUDA device")
     return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), cols)
@@ -396,57 +398,54 @@ def _workspace(ws):
 
 def _current(t):
     """Handle of the current stream, for a call on tensor t's device."""
-    if t.get_device() != torch.cuda.current_device():
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
         raise ValueError("qil: the tensors are not on the current device")
-    return torch.cuda.current_stream().cuda_stream
-
-
-def _on_stream(f):
-    """stream=s: the whole call, with the tensors it makes and fills, happens on s."""
-    @functools.wraps(f)
-    def call(*args, stream=None, **kw):
-        if stream is None:
-            return f(*args, **kw)
-        with torch.cuda.stream(stream):
-            return f(*args, **kw)
-    return call
+    return _raw_stream(dev)
 
 
 def _norm_args(x, weight, residual, residual_out):
-    M, K = x.shape
-    px = _arg("x", x, _BF16, M, K)
-    pw = _arg("weight", weight, _BF16, K)
+    M, K = shape = x.shape
+    px = _arg("x", x, _BF16, shape)
+    pw = _arg("weight", weight, _BF16, (K,))
     if residual is None:
         if residual_out is not None:
             raise ValueError("qil: residual_out without a residual")
         return M, K, px, pw, None, None, None
     if residual_out is None:
         residual_out = torch.empty_like(x)
-    return M, K, px, pw, _arg("residual", residual, _BF16, M, K), residual_out, _arg("residual_out", residual_out, _BF16, M, K)
+    return M, K, px, pw, _arg("residual", residual, _BF16, shape), residual_out, _arg("residual_out", residual_out, _BF16, shape)
 
 
-@_on_stream
-def rmsnorm(x, weight, eps: float = 1e-5, residual=None, out=None, residual_out=None):
+def rmsnorm(x, weight, eps: float = 1e-5, residual=None, out=None, residual_out=None, stream=None):
     """bf16 root-mean-square norm of x [M][K], or of x + residual.  Returns y, or (y, h) with h = bf16(x + residual) where a
     residual is given; residual_out=residual updates the residual stream in place."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rmsnorm(x, weight, eps, residual, out, residual_out)
     M, K, px, pw, pr, h, ph = _norm_args(x, weight, residual, residual_out)
     if out is None:
         out = torch.empty_like(x)
-    _check(_lib.load().qil_rmsnorm(px, pr, pw, ph, _arg("out", out, _BF16, M, K), None, None, M, K, eps,
-                                   _current(x)))
+    code = _lib.load().qil_rmsnorm(px, pr, pw, ph, _arg("out", out, _BF16, (M, K)), None, None, M, K, eps, _current(x))
+    if code:
+        _check(code)
     return out if h is None else (out, h)
 
 
-@_on_stream
-def rmsnorm_a8(x, weight, eps: float = 1e-5, residual=None, out=None, residual_out=None):
+def rmsnorm_a8(x, weight, eps: float = 1e-5, residual=None, out=None, residual_out=None, stream=None):
     """The norm with int8 codes and a scale per row, the operands of linear_w8a8: (codes [M][K], scales [M]), followed by
     h = bf16(x + residual) where a residual is given.  out: a bf16 tensor that receives the unquantised norm as well (an
     adapter beside the W8A8 linear reads it)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rmsnorm_a8(x, weight, eps, residual, out, residual_out)
     M, K, px, pw, pr, h, ph = _norm_args(x, weight, residual, residual_out)
-    codes = torch.empty((M, K), dtype=_I8, device=x.device)
-    scales = torch.empty((M,), dtype=_F32, device=x.device)
-    _check(_lib.load().qil_rmsnorm(px, pr, pw, ph, None if out is None else _arg("out", out, _BF16, M, K), codes.data_ptr(),
-                                   scales.data_ptr(), M, K, eps, _current(x)))
+    codes = torch.empty_like(x, dtype=_I8)
+    scales = x.new_empty(M, dtype=_F32)
+    code = _lib.load().qil_rmsnorm(px, pr, pw, ph, None if out is None else _arg("out", out, _BF16, (M, K)), codes.data_ptr(),
+                                   scales.data_ptr(), M, K, eps, _current(x))
+    if code:
+        _check(code)
     return (codes, scales) if h is None else (codes, scales, h)
 
 
@@ -465,26 +464,34 @@ def new_kv_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: in
 
 
 def _paged_args(k_cache, v_cache, cu_q, kv_len, block_table):
-    pages, kv_heads, page, dim = k_cache.shape
-    seqs = kv_len.shape[0]
-    return (pages, kv_heads, page, dim, seqs, _arg("k_cache", k_cache, _BF16, pages, kv_heads, page, dim),
-            _arg("v_cache", v_cache, _BF16, pages, kv_heads, page, dim), _arg("cu_q", cu_q, _I32, seqs + 1),
-            _arg("kv_len", kv_len, _I32, seqs), _arg("block_table", block_table, _I32, seqs, None))
+    """(pages, kv heads, page size, head dim, requests, table width) and the five addresses."""
+    shape = k_cache.shape
+    pages, kv_heads, page, dim = shape
+    seqs, width = block_table.shape
+    return (pages, kv_heads, page, dim, seqs, width, _arg("k_cache", k_cache, _BF16, shape), _arg("v_cache", v_cache, _BF16, shape),
+            _arg("cu_q", cu_q, _I32, (seqs + 1,)), _arg("kv_len", kv_len, _I32, (seqs,)),
+            _arg("block_table", block_table, _I32, (seqs, width)))
 
 
-@_on_stream
-def rope_append(qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads: int, out=None):
+def rope_append(qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads: int, out=None, stream=None):
     """Rotary embedding of a fused projection's queries and keys, append of keys and values to the paged cache.
     qkv [T][(H + 2 Hk) D]; kv_len counts the new tokens.  Returns the rotated queries [T][H][D]; the caches are updated."""
-    pages, kv_heads, page, dim, seqs, pk, pv, pc, pl, pt = _paged_args(k_cache, v_cache, cu_q, kv_len, block_table)
-    T = qkv.shape[0]
-    pq = _arg("qkv", qkv, _BF16, T, (num_heads + 2 * kv_heads) * dim)
-    pcs = _arg("cos_sin", cos_sin, _F32, None, dim)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rope_append(qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads, out)
+    pages, kv_heads, page, dim, seqs, width, pk, pv, pc, pl, pt = _paged_args(k_cache, v_cache, cu_q, kv_len, block_table)
+    T, max_pos = qkv.shape[0], cos_sin.shape[0]
+    pq = _arg("qkv", qkv, _BF16, (T, (num_heads + 2 * kv_heads) * dim))
+    pcs = _arg("cos_sin", cos_sin, _F32, (max_pos, dim))
     if out is None:
-        out = torch.empty((T, num_heads, dim), dtype=_BF16, device=qkv.device)
-    _check(_lib.load().qil_rope_append(pq, pcs, _arg("out", out, _BF16, T, num_heads, dim), pk, pv, pc, pl, pt, T, seqs,
-                                       num_heads, kv_heads, dim, page, pages, block_table.shape[1], cos_sin.shape[0],
-                                       _current(qkv)))
+        out = qkv.new_empty((T, num_heads, dim))
+        po = out.data_ptr()
+    else:
+        po = _arg("out", out, _BF16, (T, num_heads, dim))
+    code = _lib.load().qil_rope_append(pq, pcs, po, pk, pv, pc, pl, pt, T, seqs, num_heads, kv_heads, dim, page, pages, width, max_pos,
+                                       _current(qkv))
+    if code:
+        _check(code)
     return out
 
 
@@ -493,23 +500,28 @@ def attn_paged_workspace_size(total_q: int, num_seqs: int, num_heads: int, num_k
     return int(_lib.load().qil_attn_paged_workspace_size(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len))
 
 
-@_on_stream
 def attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len: int, max_kv_len: int, scale: float | None = None,
-               out=None, workspace=None):
+               out=None, workspace=None, stream=None):
     """Causal attention of the new tokens q [T][H][D] of all requests over the paged cache (which holds them already).
     max_q_len, max_kv_len bound the requests' lengths; scale defaults to D ** -0.5."""
-    pages, kv_heads, page, dim, seqs, pk, pv, pc, pl, pt = _paged_args(k_cache, v_cache, cu_q, kv_len, block_table)
-    T, heads = q.shape[0], q.shape[1]
-    pq = _arg("q", q, _BF16, T, heads, dim)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
+    pages, kv_heads, page, dim, seqs, width, pk, pv, pc, pl, pt = _paged_args(k_cache, v_cache, cu_q, kv_len, block_table)
+    T, heads, _ = shape = q.shape
+    pq = _arg("q", q, _BF16, (T, heads, dim))
     if out is None:
         out = torch.empty_like(q)
-    po = _arg("out", out, _BF16, T, heads, dim)
+        po = out.data_ptr()
+    else:
+        po = _arg("out", out, _BF16, shape)
     if workspace is None:
         workspace = new_workspace(attn_paged_workspace_size(T, seqs, heads, kv_heads, dim, max_q_len, max_kv_len), q.device)
-    ws = _workspace(workspace)
-    _check(_lib.load().qil_attn_paged(pq, pk, pv, po, pc, pl, pt, T, seqs, heads, kv_heads, dim, page, pages, block_table.shape[1],
-                                      max_q_len, max_kv_len, dim ** -0.5 if scale is None else scale, *ws,
-                                      _current(q)))
+    pw, nbytes = _workspace(workspace)
+    code = _lib.load().qil_attn_paged(pq, pk, pv, po, pc, pl, pt, T, seqs, heads, kv_heads, dim, page, pages, width, max_q_len,
+                                      max_kv_len, dim ** -0.5 if scale is None else scale, pw, nbytes, _current(q))
+    if code:
+        _check(code)
     return out
 
 
@@ -517,24 +529,28 @@ def lora_batch_workspace_size(M: int, num_seqs: int, rank: int) -> int:
     return int(_lib.load().qil_lora_batch_workspace_size(M, num_seqs, rank))
 
 
-@_on_stream
-def lora_batch_add(x, a, b, y, cu_q, adapter, scales, out=None, workspace=None):
+def lora_batch_add(x, a, b, y, cu_q, adapter, scales, out=None, workspace=None, stream=None):
     """out = y + scales[i] * (x . a[i]^T) . b[i]^T with i = adapter[request of the row]; requests whose adapter is negative
     have none.  a [n][r][K], b [n][N][r], r <= 64.  x, y and out may be column slices of wider tensors; without out, y is
     updated in place.  Returns out (or y)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return lora_batch_add(x, a, b, y, cu_q, adapter, scales, out, workspace)
     M, K = x.shape
-    n, r, N = a.shape[0], a.shape[1], b.shape[1]
-    if out is None:
-        out = y
+    n, N, r = shape = b.shape
     px, ldx = _arg_rows("x", x, M, K)
     py, ldy = _arg_rows("y", y, M, N)
-    po, ldo = _arg_rows("out", out, M, N)
+    if out is None:
+        out, po, ldo = y, py, ldy
+    else:
+        po, ldo = _arg_rows("out", out, M, N)
     seqs = adapter.shape[0]
-    pa, pb = _arg("a", a, _BF16, n, r, K), _arg("b", b, _BF16, n, N, r)
     if workspace is None:
         workspace = torch.empty(max(lora_batch_workspace_size(M, seqs, r), 16), dtype=torch.uint8, device=x.device)
-    ws = _workspace(workspace)
-    _check(_lib.load().qil_lora_batch_add(px, pa, pb, py, po, _arg("cu_q", cu_q, _I32, seqs + 1), _arg("adapter", adapter, _I32, seqs),
-                                          _arg("scales", scales, _F32, n), M, N, K, r, seqs, n, ldx, ldy, ldo, *ws,
-                                          _current(x)))
+    pw, nbytes = _workspace(workspace)
+    code = _lib.load().qil_lora_batch_add(px, _arg("a", a, _BF16, (n, r, K)), _arg("b", b, _BF16, shape), py, po,
+                                          _arg("cu_q", cu_q, _I32, (seqs + 1,)), _arg("adapter", adapter, _I32, (seqs,)),
+                                          _arg("scales", scales, _F32, (n,)), M, N, K, r, seqs, n, ldx, ldy, ldo, pw, nbytes, _current(x))
+    if code:
+        _check(code)
     return out

@@ -284,23 +284,17 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     }
 }
 
-}  // namespace
-
-qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) {
+template <int kDim>
+qil_status go(const AttnParams& p, cudaStream_t st) {
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(attn_few_kernel<kDim>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
     const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)p.c.num_seqs);
-    cudaError_t e;
-    if (p.c.head_dim == 128) {
-        e = cudaFuncSetAttribute(attn_few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<128>::kSmem);
-        if (e == cudaSuccess) attn_few_kernel<128><<<grid, 32 * kWarps, FewShape<128>::kSmem, st>>>(p);
-    } else {
-        e = cudaFuncSetAttribute(attn_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<64>::kSmem);
-        if (e == cudaSuccess) attn_few_kernel<64><<<grid, 32 * kWarps, FewShape<64>::kSmem, st>>>(p);
-    }
-    if (e != cudaSuccess) {
-        (void)cudaGetLastError();
-        return QIL_ERR_CUDA;
-    }
+    attn_few_kernel<kDim><<<grid, 32 * kWarps, FewShape<kDim>::kSmem, st>>>(p);
     return launch_status();
 }
+
+}  // namespace
+
+qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) { return p.c.head_dim == 128 ? go<128>(p, st) : go<64>(p, st); }
 
 }  // namespace qil

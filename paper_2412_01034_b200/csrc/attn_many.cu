@@ -533,10 +533,8 @@ qil_status go(const AttnParams& p, cudaStream_t st) {
     if (!encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)) return QIL_ERR_CUDA;
     constexpr int kSmem = ManyShape<kDim>::kSmem;
     static_assert(kSmem <= 232448, "shared memory per block");
-    if (cudaFuncSetAttribute(attn_many_kernel<kDim>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return QIL_ERR_CUDA;
-    }
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
     const long long rows = (long long)p.c.total_q * p.G;
     const dim3 grid((unsigned)(rows / (2 * kRows) + p.c.num_seqs), (unsigned)p.c.num_kv_heads, (unsigned)p.splits);
     attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mk, mv, p);
