@@ -27,6 +27,10 @@ namespace {
 
 constexpr int kRows = 128, kTok = 128, kThreads = 384;
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+#ifndef QIL_POLY_EVERY
+#define QIL_POLY_EVERY 4
+#endif
+constexpr int kPolyEvery = QIL_POLY_EVERY;   // every so many pairs of weights come from the polynomial
 constexpr float kRaise = 8.f;   // log2 by which a score may exceed the reference maximum
 
 template <int kDim>
@@ -111,12 +115,63 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
         "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
         ::"r"(taddr), QIL_I8(v, 0), QIL_I8(v, 8), QIL_I8(v, 16), QIL_I8(v, 24) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : QIL_R8(v, 0), QIL_R8(v, 8) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), QIL_I8(v, 0), QIL_I8(v, 8) : "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int n>
 __device__ __forceinline__ void pin(uint32_t (&v)[n]) {   // the values exist only after the wait before this
 #pragma unroll
     for (int j = 0; j < n; ++j) asm volatile("" : "+r"(v[j]));
+}
+
+// Two fp32 values in a register pair: the packed forms of add and multiply-add issue once for both.
+__device__ __forceinline__ unsigned long long f2(float a, float b) {
+    unsigned long long v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void f2_split(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ unsigned long long f2_fma(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long f2_add(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x of two values on the multiply-add pipe: x = n + f with n the nearest integer (adding 1.5 * 2^23 leaves it in the
+// low bits), a polynomial of degree 4 in f, the minimax one for the relative error on [-1/2, 1/2] (3e-6, found by
+// exchange), and n added to its exponent.  Arguments below -126 give 2^-126.
+__device__ __forceinline__ void poly_exp2(unsigned long long x, float& a, float& b) {
+    constexpr float kMagic = 12582912.f;
+    float xa, xb;
+    f2_split(x, xa, xb);
+    x = f2(fmaxf(xa, -126.f), fmaxf(xb, -126.f));
+    const unsigned long long t = f2_add(x, f2(kMagic, kMagic));
+    const unsigned long long f = f2_fma(f2_add(t, f2(-kMagic, -kMagic)), f2(-1.f, -1.f), x);
+    unsigned long long v = f2_fma(f, f2(0.009570102207f, 0.009570102207f), f2(0.05591785908f, 0.05591785908f));
+    v = f2_fma(v, f, f2(0.2402474433f, 0.2402474433f));
+    v = f2_fma(v, f, f2(0.6931217909f, 0.6931217909f));
+    v = f2_fma(v, f, f2(0.9999992847f, 0.9999992847f));
+    float ta, tb, va, vb;
+    f2_split(t, ta, tb);
+    f2_split(v, va, vb);
+    a = __int_as_float(__float_as_int(va) + (__float_as_int(ta) << 23));
+    b = __int_as_float(__float_as_int(vb) + (__float_as_int(tb) << 23));
 }
 
 // Tiles of 256 rows over the requests with more than kFewRows rows; the later (longer) tiles of a request come first.
@@ -155,9 +210,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int G = p.G, H = p.c.num_heads, kvh = blockIdx.y;
+    const int G = p.G, H = p.c.num_heads, kvh = blockIdx.x % p.c.num_kv_heads;
     int seq, q_lo, q_hi, pair;
-    if (!find_pair(p.c, G, blockIdx.x, seq, q_lo, q_hi, pair)) return;
+    if (!find_pair(p.c, G, blockIdx.x / p.c.num_kv_heads, seq, q_lo, q_hi, pair)) return;
     const int rows = (q_hi - q_lo) * G, row0 = pair * 2 * kRows;
     const int end = cache_end(p.c, seq), first_pos = __ldg(p.c.kv_len + seq) - (q_hi - q_lo);
     // visible tokens of row r; tiles of tokens that row tile i needs, cut to this block's part of the cache
@@ -177,14 +232,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sq = smem_u32(smem), sk = sq + 2 * kTileBytes, sv = sk + kStages * kTileBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kTileBytes + 2 * kStages * kTileBytes);
-    const uint32_t q_full = smem_u32(bars), s_full = q_full + 16, p_full = q_full + 32, o_done = q_full + 48, v_raw = q_full + 64,
-                   drain = q_full + 72, k_full = q_full + 80, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10 + 3 * kStages);
+    const uint32_t q_full = smem_u32(bars), s_full = q_full + 16, p_full = q_full + 32, o_done = q_full + 64, v_raw = q_full + 80,
+                   drain = q_full + 88, k_full = q_full + 96, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 3 * kStages);
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(q_full + 8 * i, 4);   // the group's warps
             mbar_init(s_full + 8 * i, 1);   // commit after S_i
-            mbar_init(p_full + 8 * i, 4);   // the group's warps
+            mbar_init(p_full + 16 * i, 4);      // the group's warps: weights of the first 64 tokens
+            mbar_init(p_full + 16 * i + 8, 4);  // and of the others
             mbar_init(o_done + 8 * i, 1);   // commit after the last product of tile i
         }
         mbar_init(v_raw, 1);                // the copy of a V tile whose last tokens are still to be cleared
@@ -287,13 +343,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                             ok = mbar_wait(v_full + 8 * s, (j / kStages) & 1);
                             v_there = true;
                         }
-                        ok = ok && mbar_wait(p_full + 8 * i, j & 1);
-                        if (!ok) break;
-                        tc_fence_after();
                         const uint32_t b = v_d + (uint32_t)s * (kTileBytes >> 4), o = tmem + Shape::kO + (uint32_t)(i * kDim);
 #pragma unroll
-                        for (int k = 0; k < kTok / 16; ++k)   // 16 tokens: 8 columns of P, 2048 bytes of V
-                            mma_ts(o, tmem + 128 * i + 8 * k, b + 128 * k, kHi, kDescO, j > 0 || k > 0);
+                        for (int h = 0; h < 2; ++h) {
+                            ok = ok && mbar_wait(p_full + 16 * i + 8 * h, j & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 4 * h; k < 4 * h + 4; ++k)   // 16 tokens: 8 columns of P, 2048 bytes of V
+                                mma_ts(o, tmem + 128 * i + 8 * k, b + 128 * k, kHi, kDescO, j > 0 || k > 0);
+                        }
+                        if (!ok) break;
                         if (j + 1 == mine) {
                             tc_commit(o_done + 8 * i);
                             continue;
@@ -330,20 +390,30 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
         // ---------------- softmax of row tile i: one row per thread ----------------
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int i = (warp - 4) >> 2, t = tid - 128 - 128 * i;
-        const int mine = i ? n1 : n0, r = row0 + i * kRows + t, see = visible(r) - j0 * kTok;
+        const int mine = i ? n1 : n0, r = row0 + i * kRows + t, see = r < rows ? visible(r) - j0 * kTok : 0x40000000;   // (rows past the last one never mask)
         // the queries as the MMA's K-major operand with 128-byte swizzle; a negative scale goes into their sign, and for a
         // scale of zero they are zero (zero times a masked score of -inf would be NaN)
         const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
         const float scale = p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2);
         if (mine > 0) {
-            for (int at = t; at < kRows * (kDim / 8); at += 128) {
-                const int rr = at / (kDim / 8), piece = at % (kDim / 8), R = row0 + i * kRows + rr;
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (R < rows && p.scale_log2 != 0.f) {
-                    v = *reinterpret_cast<const uint4*>(p.q + ((size_t)(q_lo + R / G) * H + kvh * G + R % G) * kDim + 8 * piece);
-                    v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
+            constexpr int kPieces = kDim / 8, kPass = 128 / kPieces;   // 16-byte pieces of a row, rows per pass of the group
+            const int piece = t % kPieces;
+#pragma unroll
+            for (int half = 0; half < kRows; half += 8 * kPass) {
+                uint4 v[8];   // (eight loads in flight: one at a time, each pass took a trip to memory)
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int R = row0 + i * kRows + half + x * kPass + t / kPieces;
+                    v[x] = make_uint4(0u, 0u, 0u, 0u);
+                    if (R < rows && p.scale_log2 != 0.f)
+                        v[x] = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)(q_lo + R / G) * H + kvh * G + R % G) * kDim + 8 * piece));
                 }
-                *reinterpret_cast<uint4*>(smem + i * kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + ((piece ^ rr) & 7) * 16) = v;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int rr = half + x * kPass + t / kPieces;
+                    v[x].x ^= sign; v[x].y ^= sign; v[x].z ^= sign; v[x].w ^= sign;
+                    *reinterpret_cast<uint4*>(smem + i * kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + ((piece ^ rr) & 7) * 16) = v[x];
+                }
             }
             fence_async_smem();
             __syncwarp();
@@ -351,6 +421,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
         }
         const uint32_t lane_base = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const uint32_t s_at = lane_base + 128 * i, o_at = lane_base + Shape::kO + (uint32_t)(i * kDim);
+        auto publish = [&](int half) {   // this warp's rows of half of P are in tensor memory
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 16 * i + 8 * half);
+        };
         float ref = -INFINITY, sum = 0.f;
         for (int j = 0; j < mine && ok; ++j) {
             ok = mbar_wait(s_full + 8 * i, j & 1);
@@ -362,56 +438,96 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
             tmem_ld_wait();
             pin(s);
             const int left = see - j * kTok;   // visible tokens from the tile's first
-            if (__any_sync(0xffffffffu, left < kTok)) {
+            const bool edge = __any_sync(0xffffffffu, left < kTok);
+            bool done = false;
+            if (j > 0 && !edge) {
+                // Weights against the present reference while the tile's maximum is still being found: it hardly ever
+                // exceeds the reference by more than the limit, and the exponentials need not wait for it.  The first 64
+                // tokens' product starts while the other weights are computed.
+                const unsigned long long scale2 = f2(scale, scale), base2 = f2(-ref, -ref);
+                unsigned long long acc[2] = {0ull, 0ull};
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto weights = [&](int c, bool find) {
+                    uint32_t w[32];
 #pragma unroll
-                for (int c = 0; c < kTok; ++c)
-                    if (c >= left) s[c] = 0xFF800000u;   // -inf
+                    for (int e = 0; e < 32; ++e) {
+                        const unsigned long long x = f2_fma(f2(__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])), scale2, base2);
+                        float a, b;
+                        if (e % kPolyEvery == kPolyEvery - 1) {
+                            poly_exp2(x, a, b);
+                        } else {
+                            f2_split(x, a, b);
+                            a = fast_exp2(a);
+                            b = fast_exp2(b);
+                        }
+                        if (find) {
+                            top[e & 1] = max3(top[e & 1], __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+                            top[2 + (e & 1)] = max3(top[2 + (e & 1)], __uint_as_float(s[64 + 2 * e]), __uint_as_float(s[64 + 2 * e + 1]));
+                        }
+                        acc[e & 1] = f2_add(acc[e & 1], f2(a, b));
+                        w[e] = pack2(a, b);
+                    }
+                    tmem_st32(s_at + c / 2, w);
+                };
+                weights(0, true);
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+                done = !__any_sync(0xffffffffu, !(most <= ref + kRaise));
+                if (done) {
+                    publish(0);
+                    weights(64, false);
+                    publish(1);
+                    float a, b;
+                    f2_split(f2_add(acc[0], acc[1]), a, b);
+                    sum += a + b;
+                }
             }
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (!done) {
+                if (edge) {
 #pragma unroll
-            for (int c = 0; c < kTok; c += 4)
+                    for (int c = 0; c < kTok; ++c)
+                        if (c >= left) s[c] = 0xFF800000u;   // -inf
+                }
+                float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], __uint_as_float(s[c + e]));
-            const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
-            const bool raise = most > ref + kRaise;   // (also the first visible score: ref is -inf before it)
-            if (__any_sync(0xffffffffu, raise)) {
-                const float to = raise ? most : ref;
-                const float keep = raise ? fast_exp2(ref - to) : 1.f;
-                ref = to;
-                sum *= keep;
-                if (j > 0) {   // (S_i(j) is there, so the product before it is complete)
+                for (int c = 0; c < kTok; c += 2) top[(c >> 1) & 1] = max3(top[(c >> 1) & 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                const float most = fmaxf(top[0], top[1]) * scale;
+                const bool raise = most > ref + kRaise;   // (also the first visible score: ref is -inf before it)
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float to = raise ? most : ref;
+                    const float keep = raise ? fast_exp2(ref - to) : 1.f;
+                    ref = to;
+                    sum *= keep;
+                    if (j > 0) {   // (S_i(j) is there, so the product before it is complete)
 #pragma unroll 1
-                    for (int c = 0; c < kDim; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(o_at + c, o);
-                        tmem_ld_wait();
-                        pin(o);
+                        for (int c = 0; c < kDim; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_at + c, o);
+                            tmem_ld_wait();
+                            pin(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                        tmem_st32(o_at + c, o);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                            tmem_st16(o_at + c, o);
+                        }
                     }
                 }
-            }
-            const float base = ref == -INFINITY ? 0.f : -ref;
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
+                const float base = ref == -INFINITY ? 0.f : -ref;
+                float part[2] = {0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < kTok; c += 64) {
-                uint32_t w[32];
+                for (int c = 0; c < kTok; c += 64) {
+                    uint32_t w[32];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float a = fast_exp2(fmaf(__uint_as_float(s[c + 2 * e]), scale, base));
-                    const float b = fast_exp2(fmaf(__uint_as_float(s[c + 2 * e + 1]), scale, base));
-                    part[e & 1] += a;
-                    part[2 + (e & 1)] += b;
-                    w[e] = pack2(a, b);
+                    for (int e = 0; e < 32; ++e) {
+                        const float a = fast_exp2(fmaf(__uint_as_float(s[c + 2 * e]), scale, base));
+                        const float b = fast_exp2(fmaf(__uint_as_float(s[c + 2 * e + 1]), scale, base));
+                        part[0] += a;
+                        part[1] += b;
+                        w[e] = pack2(a, b);
+                    }
+                    tmem_st32(s_at + c / 2, w);
+                    publish(c / 64);
                 }
-                tmem_st32(s_at + c / 2, w);
+                sum += part[0] + part[1];
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 8 * i);
         }
         // the rows' results
         if (mine > 0 && ok) ok = mbar_wait(o_done + 8 * i, 0);
@@ -536,7 +652,8 @@ qil_status go(const AttnParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
     const long long rows = (long long)p.c.total_q * p.G;
-    const dim3 grid((unsigned)(rows / (2 * kRows) + p.c.num_seqs), (unsigned)p.c.num_kv_heads, (unsigned)p.splits);
+    // (heads first, so that the long tiles of all heads start before the short ones of any)
+    const dim3 grid((unsigned)(p.c.num_kv_heads * (rows / (2 * kRows) + p.c.num_seqs)), 1u, (unsigned)p.splits);
     attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mk, mv, p);
     if (p.splits > 1) {
         const long long items = (long long)p.c.total_q * p.c.num_heads;
