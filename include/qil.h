@@ -454,7 +454,8 @@ qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, v
  *   split; a request that exceeds them gets unspecified results.
  *   workspace: qil_attn_paged_workspace_size() bytes, zero-filled once; calls that share it must not overlap.  Its first
  *   int is a status word (QIL_ERR_TIMEOUT if a bounded device-side wait ran out; see qil_device_status).
- * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also a scale that is not finite), WORKSPACE, CUDA. */
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also a scale that is not finite, and more than 128 heads to a key head),
+ *   WORKSPACE, CUDA. */
 size_t qil_attn_paged_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
                                      int max_q_len, int max_kv_len);
 qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const int* cu_q,

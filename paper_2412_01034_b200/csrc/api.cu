@@ -306,7 +306,7 @@ qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cach
     const qil_status s = check_paged(c);
     if (s != QIL_OK) return s;
     if (max_q_len <= 0 || max_kv_len <= 0) return QIL_ERR_SHAPE;
-    if (!std::isfinite(scale)) return QIL_ERR_UNSUPPORTED;
+    if (!std::isfinite(scale) || num_heads / num_kv_heads > 128) return QIL_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace) || !aligned4(cu_q) ||
         !aligned4(kv_len) || !aligned4(block_table))
         return QIL_ERR_ALIGN;

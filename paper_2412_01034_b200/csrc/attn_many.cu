@@ -1,7 +1,8 @@
 // Attention over the paged cache for requests with many query rows (prompts, chunks of a prompt): tcgen05.mma with the
 // scores, the weights and the output accumulators in tensor memory.
 //
-// A block takes up to 256 query rows of one request and key head as two tiles of 128 rows, and walks the cache in tiles of
+// A block takes up to 256 query rows of one request and key head as two tiles of 128 rows (whole tokens: 128 / G of them,
+// so that one bulk tensor copy fetches a tile's queries for any group size), and walks the cache in tiles of
 // 128 tokens.  Per tile of tokens and tile i of rows:
 //   S_i = Q_i K^T      128 x 128 x D, both operands in shared memory, fp32 in tensor memory
 //   P_i = exp2(S_i c - m)   by the 128 threads of group i, one row each: tcgen05.ld, running maximum and sum in registers,
@@ -25,12 +26,8 @@ namespace qil {
 
 namespace {
 
-constexpr int kRows = 128, kTok = 128, kThreads = 384;
+constexpr int kRows = kTileRows, kTok = 128, kThreads = 384;
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
-#ifndef QIL_POLY_EVERY
-#define QIL_POLY_EVERY 4
-#endif
-constexpr int kPolyEvery = QIL_POLY_EVERY;   // every so many pairs of weights come from the polynomial
 constexpr float kRaise = 8.f;   // log2 by which a score may exceed the reference maximum
 
 template <int kDim>
@@ -54,21 +51,22 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+// The thread may be suspended while it waits, up to a limit of the hardware's.
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 // Bounded wait: false when the limit ran out.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-    if (mbar_test(bar, parity)) return true;
+    if (mbar_try(bar, parity)) return true;
     unsigned long long t0 = 0, t;
 #pragma unroll 1
     for (uint32_t i = 0;; ++i) {
-        if (mbar_test(bar, parity)) return true;
-        if ((i & 255u) == 0u) {
+        if (mbar_try(bar, parity)) return true;
+        if ((i & 15u) == 0u) {
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
             if (i == 0u) t0 = t;
             else if (t - t0 > kWaitLimitNs) return false;
@@ -78,6 +76,10 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -153,35 +155,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 2^x of two values on the multiply-add pipe: x = n + f with n the nearest integer (adding 1.5 * 2^23 leaves it in the
-// low bits), a polynomial of degree 4 in f, the minimax one for the relative error on [-1/2, 1/2] (3e-6, found by
-// exchange), and n added to its exponent.  Arguments below -126 give 2^-126.
-__device__ __forceinline__ void poly_exp2(unsigned long long x, float& a, float& b) {
-    constexpr float kMagic = 12582912.f;
-    float xa, xb;
-    f2_split(x, xa, xb);
-    x = f2(fmaxf(xa, -126.f), fmaxf(xb, -126.f));
-    const unsigned long long t = f2_add(x, f2(kMagic, kMagic));
-    const unsigned long long f = f2_fma(f2_add(t, f2(-kMagic, -kMagic)), f2(-1.f, -1.f), x);
-    unsigned long long v = f2_fma(f, f2(0.009570102207f, 0.009570102207f), f2(0.05591785908f, 0.05591785908f));
-    v = f2_fma(v, f, f2(0.2402474433f, 0.2402474433f));
-    v = f2_fma(v, f, f2(0.6931217909f, 0.6931217909f));
-    v = f2_fma(v, f, f2(0.9999992847f, 0.9999992847f));
-    float ta, tb, va, vb;
-    f2_split(t, ta, tb);
-    f2_split(v, va, vb);
-    a = __int_as_float(__float_as_int(va) + (__float_as_int(ta) << 23));
-    b = __int_as_float(__float_as_int(vb) + (__float_as_int(tb) << 23));
-}
-
-// Tiles of 256 rows over the requests with more than kFewRows rows; the later (longer) tiles of a request come first.
-__device__ __forceinline__ bool find_pair(const PagedCache& c, int G, int t, int& seq, int& lo, int& hi, int& pair) {
+// Pairs of row tiles (of `tokens` new tokens each) over the requests with more than kFewRows rows; the later (longer) tiles
+// of a request come first.
+__device__ __forceinline__ bool find_pair(const PagedCache& c, int G, int tokens, int t, int& seq, int& lo, int& hi, int& pair) {
     const int lane = threadIdx.x & 31;
     int before = 0;
     for (int base = 0; base < c.num_seqs; base += 32) {
         int a = 0, b = 0;
         if (base + lane < c.num_seqs) request_rows(c.cu_q, base + lane, c.total_q, a, b);
-        const int rows = (b - a) * G, n = rows > kFewRows ? (rows + 2 * kRows - 1) / (2 * kRows) : 0;
+        const int n = (b - a) * G > kFewRows ? (b - a + 2 * tokens - 1) / (2 * tokens) : 0;
         int incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -204,31 +186,13 @@ __device__ __forceinline__ bool find_pair(const PagedCache& c, int G, int t, int
 }
 
 template <int kDim>
-__global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                               const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                               const __grid_constant__ CUtensorMap map_v, const AttnParams p) {
     using Shape = ManyShape<kDim>;
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.G, H = p.c.num_heads, kvh = blockIdx.x % p.c.num_kv_heads;
-    int seq, q_lo, q_hi, pair;
-    if (!find_pair(p.c, G, blockIdx.x / p.c.num_kv_heads, seq, q_lo, q_hi, pair)) return;
-    const int rows = (q_hi - q_lo) * G, row0 = pair * 2 * kRows;
-    const int end = cache_end(p.c, seq), first_pos = __ldg(p.c.kv_len + seq) - (q_hi - q_lo);
-    // visible tokens of row r; tiles of tokens that row tile i needs, cut to this block's part of the cache
-    auto visible = [&](int r) { return r < rows ? max(0, min(first_pos + r / G + 1, end)) : 0; };
-    int need[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int last = min(row0 + (i + 1) * kRows, rows) - 1;
-        need[i] = last >= row0 + i * kRows ? (visible(last) + kTok - 1) / kTok : 0;
-    }
-    const int all = max(need[0], need[1]);
-    const int j0 = (int)((long long)all * blockIdx.z / p.splits), j1 = (int)((long long)all * (blockIdx.z + 1) / p.splits);
-    const int n0 = max(0, min(need[0], j1) - j0), n1 = max(0, min(need[1], j1) - j0), n = max(n0, n1);   // (n0 <= n1, or n1 = 0)
-    const int lead = n1 > 0 ? 1 : 0;              // the row tile that uses every K and V tile, and last
-    const int tail = end % kTok != 0 ? end / kTok - j0 : -1;   // the tile of V whose last tokens do not exist
-
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sq = smem_u32(smem), sk = sq + 2 * kTileBytes, sv = sk + kStages * kTileBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kTileBytes + 2 * kStages * kTileBytes);
@@ -237,18 +201,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 3 * kStages);
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(q_full + 8 * i, 4);   // the group's warps
-            mbar_init(s_full + 8 * i, 1);   // commit after S_i
+            mbar_init(q_full + 8 * i, 1);       // the copy of Q_i
+            mbar_init(s_full + 8 * i, 1);       // commit after S_i
             mbar_init(p_full + 16 * i, 4);      // the group's warps: weights of the first 64 tokens
             mbar_init(p_full + 16 * i + 8, 4);  // and of the others
-            mbar_init(o_done + 8 * i, 1);   // commit after the last product of tile i
+            mbar_init(o_done + 8 * i, 1);       // commit after the last product of tile i
         }
-        mbar_init(v_raw, 1);                // the copy of a V tile whose last tokens are still to be cleared
+        mbar_init(v_raw, 1);                    // the copy of a V tile whose last tokens are still to be cleared
         mbar_init(drain, 1);
         for (int s = 0; s < kStages; ++s) {
             mbar_init(k_full + 8 * s, 1);
             mbar_init(v_full + 8 * s, 1);
-            mbar_init(k_free + 8 * s, 1);   // commit after the last S of a K tile
+            mbar_init(k_free + 8 * s, 1);       // commit after the last S of a K tile
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -256,11 +220,33 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
     }
+    int seq = 0, q_lo = 0, q_hi = 0, pair = 0;
+    const bool found = find_pair(p.c, G, p.tile_tokens, blockIdx.x / p.c.num_kv_heads, seq, q_lo, q_hi, pair);
+    // row r of tile i is new token (2 pair + i) tile_tokens + r / G, query head kvh G + r % G; `tokens` of them are the request's
+    const int token0 = pair * 2 * p.tile_tokens;
+    const int tokens[2] = {min(p.tile_tokens, q_hi - q_lo - token0), min(p.tile_tokens, q_hi - q_lo - token0 - p.tile_tokens)};
+    const int end = cache_end(p.c, seq), first_pos = __ldg(p.c.kv_len + seq) - (q_hi - q_lo);
+    // cached tokens that a new token sees; tiles of them that row tile i needs, cut to this block's part of the cache
+    auto visible = [&](int token) { return max(0, min(first_pos + token + 1, end)); };
+    int need[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) need[i] = tokens[i] > 0 ? (visible(token0 + i * p.tile_tokens + tokens[i] - 1) + kTok - 1) / kTok : 0;
+    const int all = max(need[0], need[1]);
+    const int j0 = (int)((long long)all * blockIdx.z / p.splits), j1 = (int)((long long)all * (blockIdx.z + 1) / p.splits);
+    const int n0 = max(0, min(need[0], j1) - j0), n1 = max(0, min(need[1], j1) - j0), n = max(n0, n1);   // (n0 <= n1, or n1 = 0)
+    const int lead = n1 > 0 ? 1 : 0;              // the row tile that uses every K and V tile, and last
+    const int tail = end % kTok != 0 ? end / kTok - j0 : -1;   // the tile of V whose last tokens do not exist
+
+
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    if (!found) {   // (the grid is sized for the most tiles that the requests could have)
+        if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+        return;
+    }
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
@@ -282,6 +268,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                 return page < 0 || page >= p.c.num_pages ? -page_rows : (page * p.c.num_kv_heads + kvh) * page_rows;
             };
             int row = n > 0 ? first_row(j0 * kTok) : 0;
+            if (lane < 2 && (lane ? n1 : n0) > 0) {   // Q_lane: the heads of the group by tile_tokens tokens, rows in that order
+                mbar_expect_tx(q_full + 8 * lane, (uint32_t)(p.tile_tokens * G * kDim * 2));
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+                    tma_load_3d(sq + lane * kTileBytes + h * kHalfBytes, &map_q, h * 64, kvh * G, q_lo + token0 + lane * p.tile_tokens,
+                                q_full + 8 * lane);
+            }
             int k_sent = 0, v_sent = 0;
             for (int j = 0; j < n; ++j) {
                 const int s = j % kStages, tok0 = (j0 + j) * kTok;
@@ -302,6 +295,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                 row = next;
             }
             // no copy may still be in flight when the block retires (after a time-out elsewhere either)
+            for (int i = 0; i < 2; ++i)
+                if ((i ? n1 : n0) > 0) (void)mbar_wait(q_full + 8 * i, 0);
             for (int j = max(0, k_sent - kStages); j < k_sent; ++j) (void)mbar_wait(k_full + 8 * (j % kStages), (j / kStages) & 1);
             for (int j = max(0, v_sent - kStages); j < v_sent; ++j)
                 (void)(j == tail ? mbar_wait(v_raw, 0) : mbar_wait(v_full + 8 * (j % kStages), (j / kStages) & 1));
@@ -389,36 +384,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     } else {
         // ---------------- softmax of row tile i: one row per thread ----------------
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        const int i = (warp - 4) >> 2, t = tid - 128 - 128 * i;
-        const int mine = i ? n1 : n0, r = row0 + i * kRows + t, see = r < rows ? visible(r) - j0 * kTok : 0x40000000;   // (rows past the last one never mask)
-        // the queries as the MMA's K-major operand with 128-byte swizzle; a negative scale goes into their sign, and for a
-        // scale of zero they are zero (zero times a masked score of -inf would be NaN)
-        const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+        const int i = (warp - 4) >> 2, r = tid & 127, token = r / G;
+        const int my_tokens = i ? tokens[1] : tokens[0];
+        const bool live = token < my_tokens;   // (the other rows hold anything; they take no part in the votes below)
+        const int mine = i ? n1 : n0;
+        const int see = live ? visible(token0 + i * p.tile_tokens + token) - j0 * kTok : 0x40000000;   // (rows that are no token's never mask)
         const float scale = p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2);
-        if (mine > 0) {
-            constexpr int kPieces = kDim / 8, kPass = 128 / kPieces;   // 16-byte pieces of a row, rows per pass of the group
-            const int piece = t % kPieces;
-#pragma unroll
-            for (int half = 0; half < kRows; half += 8 * kPass) {
-                uint4 v[8];   // (eight loads in flight: one at a time, each pass took a trip to memory)
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int R = row0 + i * kRows + half + x * kPass + t / kPieces;
-                    v[x] = make_uint4(0u, 0u, 0u, 0u);
-                    if (R < rows && p.scale_log2 != 0.f)
-                        v[x] = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)(q_lo + R / G) * H + kvh * G + R % G) * kDim + 8 * piece));
-                }
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int rr = half + x * kPass + t / kPieces;
-                    v[x].x ^= sign; v[x].y ^= sign; v[x].z ^= sign; v[x].w ^= sign;
-                    *reinterpret_cast<uint4*>(smem + i * kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + ((piece ^ rr) & 7) * 16) = v[x];
-                }
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_full + 8 * i);
-        }
         const uint32_t lane_base = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const uint32_t s_at = lane_base + 128 * i, o_at = lane_base + Shape::kO + (uint32_t)(i * kDim);
         auto publish = [&](int half) {   // this warp's rows of half of P are in tensor memory
@@ -437,6 +408,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
             for (int c = 0; c < kTok; c += 32) tmem_ld32(s_at + c, s + c);
             tmem_ld_wait();
             pin(s);
+            if (p.scale_log2 <= 0.f) {   // the sign of a negative scale; scores of a scale of zero
+                const uint32_t keep = p.scale_log2 < 0.f ? 0xFFFFFFFFu : 0u, flip = keep & 0x80000000u;
+#pragma unroll
+                for (int c = 0; c < kTok; ++c) s[c] = (s[c] & keep) ^ flip;
+            }
             const int left = see - j * kTok;   // visible tokens from the tile's first
             const bool edge = __any_sync(0xffffffffu, left < kTok);
             bool done = false;
@@ -453,13 +429,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                     for (int e = 0; e < 32; ++e) {
                         const unsigned long long x = f2_fma(f2(__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])), scale2, base2);
                         float a, b;
-                        if (e % kPolyEvery == kPolyEvery - 1) {
-                            poly_exp2(x, a, b);
-                        } else {
-                            f2_split(x, a, b);
-                            a = fast_exp2(a);
-                            b = fast_exp2(b);
-                        }
+                        f2_split(x, a, b);
+                        a = fast_exp2(a);
+                        b = fast_exp2(b);
                         if (find) {
                             top[e & 1] = max3(top[e & 1], __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
                             top[2 + (e & 1)] = max3(top[2 + (e & 1)], __uint_as_float(s[64 + 2 * e]), __uint_as_float(s[64 + 2 * e + 1]));
@@ -471,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                 };
                 weights(0, true);
                 const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
-                done = !__any_sync(0xffffffffu, !(most <= ref + kRaise));
+                done = !__any_sync(0xffffffffu, live && !(most <= ref + kRaise));
                 if (done) {
                     publish(0);
                     weights(64, false);
@@ -491,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < kTok; c += 2) top[(c >> 1) & 1] = max3(top[(c >> 1) & 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
                 const float most = fmaxf(top[0], top[1]) * scale;
-                const bool raise = most > ref + kRaise;   // (also the first visible score: ref is -inf before it)
+                const bool raise = live && most > ref + kRaise;   // (also the first visible score: ref is -inf before it)
                 if (__any_sync(0xffffffffu, raise)) {
                     const float to = raise ? most : ref;
                     const float keep = raise ? fast_exp2(ref - to) : 1.f;
@@ -534,38 +506,62 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         if (ok) {
-            const bool live = r < rows;
-            const size_t at = live ? (size_t)(q_lo + r / G) * H + kvh * G + r % G : 0;
+            // A thread holds a row, a row's results belong side by side: each warp turns its 32 rows around in its part of the
+            // group's query tile (8 KB a time, pieces permuted by the row; the tile has been read, the last S is long there)
+            // and writes 16 bytes a lane, whole rows at once.
             const bool whole = p.splits == 1;
             const float inv = 1.f / sum;
             const size_t items = (size_t)p.c.total_q * H;
-            float* part = p.parts + ((size_t)blockIdx.z * items + at) * kDim;
+            const int item = live ? (q_lo + token0 + i * p.tile_tokens + token) * H + kvh * G + (r - token * G) : 0;   // this thread's (token, head)
+            unsigned char* turn = smem + i * kTileBytes + (warp & 3) * (32 * kDim * 2);
+            const int w_rows = my_tokens * G - 32 * (warp & 3);   // rows from the warp's first
             if (!whole && live)
-                *reinterpret_cast<float2*>(p.parts + (size_t)p.splits * items * kDim + 2 * ((size_t)blockIdx.z * items + at)) = make_float2(ref, sum);
+                *reinterpret_cast<float2*>(p.parts + (size_t)p.splits * items * kDim + 2 * ((size_t)blockIdx.z * items + item)) =
+                    make_float2(ref, sum);
+            constexpr int kUnit = kDim * 2 / 16;   // 16-byte pieces of a row and turn: kDim bf16 or kDim / 2 fp32
+            const int turns = whole ? 1 : 2, cols = kDim / turns;
+            // (rows that saw nothing in this part of the cache have a sum of zero, by which the join leaves them out)
+            for (int h = 0; h < turns && w_rows > 0; ++h) {
 #pragma unroll 1
-            for (int c = 0; c < kDim; c += 32) {
-                uint32_t o[32];
-                if (mine > 0) {
-                    tmem_ld32(o_at + c, o);
-                    tmem_ld_wait();
-                    pin(o);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0u;
-                }
-                if (!live) continue;
-                if (whole) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        float f[8];
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) f[x] = sum == 0.f ? 0.f : __uint_as_float(o[e + x]) * inv;
-                        *reinterpret_cast<uint4*>(p.out + at * kDim + c + e) = pack8(f);
+                for (int c = 0; c < cols; c += 16) {
+                    uint32_t o[16];
+                    if (mine > 0) {
+                        tmem_ld16(o_at + h * cols + c, o);
+                        tmem_ld_wait();
+                        pin(o);
                     }
-                } else if (sum != 0.f) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    for (int e = 0; e < 16; ++e)
+                        if (mine == 0 || sum == 0.f) o[e] = 0u;
+                    if (whole) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8) {
+                            float f[8];
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) f[x] = sum == 0.f ? 0.f : __uint_as_float(o[e + x]) * inv;
+                            const int at = (c + e) / 8;
+                            *reinterpret_cast<uint4*>(turn + lane * (kUnit * 16) + ((at & ~7) | ((at ^ lane) & 7)) * 16) = pack8(f);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) {
+                            const int at = (c + e) / 4;
+                            *reinterpret_cast<uint4*>(turn + lane * (kUnit * 16) + ((at & ~7) | ((at ^ lane) & 7)) * 16) =
+                                make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        }
+                    }
                 }
+                __syncwarp();
+#pragma unroll 4
+                for (int x = 0; x < kUnit; ++x) {
+                    const int rr = (x * 32 + lane) / kUnit, at = lane % kUnit;
+                    const uint4 v = *reinterpret_cast<const uint4*>(turn + rr * (kUnit * 16) + ((at & ~7) | ((at ^ rr) & 7)) * 16);
+                    const size_t to = (size_t)__shfl_sync(0xffffffffu, item, rr);
+                    if (rr >= w_rows) continue;
+                    if (whole) *reinterpret_cast<uint4*>(p.out + to * kDim + 8 * at) = v;
+                    else *reinterpret_cast<uint4*>(p.parts + ((size_t)blockIdx.z * items + to) * kDim + h * cols + 4 * at) = v;
+                }
+                __syncwarp();
             }
         }
     }
@@ -643,18 +639,29 @@ bool encode_cache(CUtensorMap* map, const void* cache, const PagedCache& c) {
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The queries as [total_q][H][D]; a copy takes 64 columns of the G heads of a group for tile_tokens tokens.
+bool encode_queries(CUtensorMap* map, const AttnParams& p) {
+    const EncodeFn enc = encode_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)p.c.head_dim, (cuuint64_t)p.c.num_heads, (cuuint64_t)p.c.total_q};
+    const cuuint64_t strides[2] = {(cuuint64_t)p.c.head_dim * 2, (cuuint64_t)p.c.num_heads * p.c.head_dim * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tile_tokens}, estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int kDim>
 qil_status go(const AttnParams& p, cudaStream_t st) {
-    CUtensorMap mk, mv;
-    if (!encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)) return QIL_ERR_CUDA;
+    CUtensorMap mq, mk, mv;
+    if (!encode_queries(&mq, p) || !encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)) return QIL_ERR_CUDA;
     constexpr int kSmem = ManyShape<kDim>::kSmem;
     static_assert(kSmem <= 232448, "shared memory per block");
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
-    const long long rows = (long long)p.c.total_q * p.G;
     // (heads first, so that the long tiles of all heads start before the short ones of any)
-    const dim3 grid((unsigned)(p.c.num_kv_heads * (rows / (2 * kRows) + p.c.num_seqs)), 1u, (unsigned)p.splits);
-    attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mk, mv, p);
+    const dim3 grid((unsigned)((long long)p.c.num_kv_heads * (p.c.total_q / (2 * p.tile_tokens) + p.c.num_seqs)), 1u, (unsigned)p.splits);
+    attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mq, mk, mv, p);
     if (p.splits > 1) {
         const long long items = (long long)p.c.total_q * p.c.num_heads;
         attn_many_join_kernel<kDim><<<(unsigned)((items + 3) / 4), 128, 0, st>>>(p);

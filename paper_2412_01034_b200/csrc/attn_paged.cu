@@ -78,6 +78,7 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     p.slots = pl.slots;
     p.few_rows = pl.few_rows;
     p.splits = pl.splits;
+    p.tile_tokens = kTileRows / p.G;
     char* base = static_cast<char*>(ws);
     p.status = reinterpret_cast<int*>(base);
     p.counters = reinterpret_cast<int*>(base + kHeader);
