@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -86,3 +87,20 @@ def load() -> C.CDLL:
             fn.argtypes = args
         _lib = lib
     return _lib
+
+
+_binding = None
+
+
+def binding():
+    """The compiled marshalling of the layer operators (``_qil_torch.so``, which needs ``libqil.so``)."""
+    global _binding
+    if _binding is None:
+        load()
+        path = os.path.join(_HERE, "_qil_torch.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_2412_01034_b200.build`")
+        spec = importlib.util.spec_from_file_location("_qil_torch", path)
+        _binding = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_binding)
+    return _binding

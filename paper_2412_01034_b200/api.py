@@ -359,94 +359,30 @@ def probe_mma(kind: str, iters: int, commit_every: int = 8, status=None, stream=
 # operators between the linears of a decoder layer, for packed requests (rows of request b: cu_q[b] ... cu_q[b + 1] - 1)
 # (stream=s: the whole call, with the tensors that it makes and fills, happens on s)
 # ------------------------------------------------------------------------------------------------------------------
-_BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
-# The handle of the current stream without the Stream object that torch.cuda.current_stream() makes around it (3 us of a
-# 10 us call); the raw getter takes the device's index.
-_raw_stream = torch._C._cuda_getCurrentRawStream
-
-
-def _refuse(name, t, dtype, shape):
-    if t.dtype is not dtype:
-        raise ValueError(f"qil: {name} is {t.dtype}, expected {str(dtype).removeprefix('torch.')}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"qil: {name} has shape {tuple(t.shape)}, expected {shape}")
-    raise ValueError(f"qil: {name} has to be a contiguous CUDA tensor")
-
-
-def _arg(name, t, dtype, shape):
-    """The device address of a contiguous CUDA tensor of the given type and shape."""
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    return _refuse(name, t, dtype, shape)
-
-
-def _arg_rows(name, t, rows, cols):
-    """As _arg for a bf16 matrix whose rows may be part of longer ones: (address, row stride)."""
-    if t.dtype is not _BF16 or t.shape != (rows, cols):
-        _refuse(name, t, _BF16, (rows, cols))
-    if not t.is_cuda or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"qil: the rows of {name} have to be contiguous, on a CUDA device")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), cols)
-
-
-def _workspace(ws):
-    """Address and size of a workspace."""
-    if not ws.is_cuda or not ws.is_contiguous():
-        raise ValueError("qil: the workspace has to be a contiguous CUDA tensor")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
-
-
-def _current(t):
-    """Handle of the current stream, for a call on tensor t's device."""
-    dev = t.get_device()
-    if dev != torch.cuda.current_device():
-        raise ValueError("qil: the tensors are not on the current device")
-    return _raw_stream(dev)
-
-
-def _norm_args(x, weight, residual, residual_out):
-    M, K = shape = x.shape
-    px = _arg("x", x, _BF16, shape)
-    pw = _arg("weight", weight, _BF16, (K,))
-    if residual is None:
-        if residual_out is not None:
-            raise ValueError("qil: residual_out without a residual")
-        return M, K, px, pw, None, None, None
-    if residual_out is None:
-        residual_out = torch.empty_like(x)
-    return M, K, px, pw, _arg("residual", residual, _BF16, shape), residual_out, _arg("residual_out", residual_out, _BF16, shape)
+def _call(name, stream, *args):
+    """An operator of the compiled binding, which tests the tensors, makes the outputs and launches on the current stream."""
+    f = getattr(_lib._binding or _lib.binding(), name)
+    if stream is None:
+        r = f(*args)
+    else:
+        with torch.cuda.stream(stream):
+            r = f(*args)
+    if r.__class__ is int:
+        _check(r)
+    return r
 
 
 def rmsnorm(x, weight, eps: float = 1e-5, residual=None, out=None, residual_out=None, stream=None):
     """bf16 root-mean-square norm of x [M][K], or of x + residual.  Returns y, or (y, h) with h = bf16(x + residual) where a
     residual is given; residual_out=residual updates the residual stream in place."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return rmsnorm(x, weight, eps, residual, out, residual_out)
-    M, K, px, pw, pr, h, ph = _norm_args(x, weight, residual, residual_out)
-    if out is None:
-        out = torch.empty_like(x)
-    code = _lib.load().qil_rmsnorm(px, pr, pw, ph, _arg("out", out, _BF16, (M, K)), None, None, M, K, eps, _current(x))
-    if code:
-        _check(code)
-    return out if h is None else (out, h)
+    return _call("rmsnorm", stream, x, weight, eps, residual, out, residual_out, False)
 
 
 def rmsnorm_a8(x, weight, eps: float = 1e-5, residual=None, out=None, residual_out=None, stream=None):
     """The norm with int8 codes and a scale per row, the operands of linear_w8a8: (codes [M][K], scales [M]), followed by
     h = bf16(x + residual) where a residual is given.  out: a bf16 tensor that receives the unquantised norm as well (an
     adapter beside the W8A8 linear reads it)."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return rmsnorm_a8(x, weight, eps, residual, out, residual_out)
-    M, K, px, pw, pr, h, ph = _norm_args(x, weight, residual, residual_out)
-    codes = torch.empty_like(x, dtype=_I8)
-    scales = x.new_empty(M, dtype=_F32)
-    code = _lib.load().qil_rmsnorm(px, pr, pw, ph, None if out is None else _arg("out", out, _BF16, (M, K)), codes.data_ptr(),
-                                   scales.data_ptr(), M, K, eps, _current(x))
-    if code:
-        _check(code)
-    return (codes, scales) if h is None else (codes, scales, h)
+    return _call("rmsnorm", stream, x, weight, eps, residual, out, residual_out, True)
 
 
 def rope_table(max_pos: int, head_dim: int, theta: float = 10000.0, device="cuda"):
@@ -454,45 +390,19 @@ def rope_table(max_pos: int, head_dim: int, theta: float = 10000.0, device="cuda
     half = head_dim // 2
     freq = theta ** (-torch.arange(half, dtype=torch.float64) / half)
     angle = torch.arange(max_pos, dtype=torch.float64)[:, None] * freq
-    return torch.cat([angle.cos(), angle.sin()], dim=1).to(_F32).to(device)
+    return torch.cat([angle.cos(), angle.sin()], dim=1).to(torch.float32).to(device)
 
 
 def new_kv_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, device="cuda"):
     """(k_cache, v_cache), each [num_pages][num_kv_heads][page_size][head_dim] bf16."""
     shape = (num_pages, num_kv_heads, page_size, head_dim)
-    return tuple(torch.zeros(shape, dtype=_BF16, device=device) for _ in range(2))
-
-
-def _paged_args(k_cache, v_cache, cu_q, kv_len, block_table):
-    """(pages, kv heads, page size, head dim, requests, table width) and the five addresses."""
-    shape = k_cache.shape
-    pages, kv_heads, page, dim = shape
-    seqs, width = block_table.shape
-    return (pages, kv_heads, page, dim, seqs, width, _arg("k_cache", k_cache, _BF16, shape), _arg("v_cache", v_cache, _BF16, shape),
-            _arg("cu_q", cu_q, _I32, (seqs + 1,)), _arg("kv_len", kv_len, _I32, (seqs,)),
-            _arg("block_table", block_table, _I32, (seqs, width)))
+    return tuple(torch.zeros(shape, dtype=torch.bfloat16, device=device) for _ in range(2))
 
 
 def rope_append(qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads: int, out=None, stream=None):
     """Rotary embedding of a fused projection's queries and keys, append of keys and values to the paged cache.
     qkv [T][(H + 2 Hk) D]; kv_len counts the new tokens.  Returns the rotated queries [T][H][D]; the caches are updated."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return rope_append(qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads, out)
-    pages, kv_heads, page, dim, seqs, width, pk, pv, pc, pl, pt = _paged_args(k_cache, v_cache, cu_q, kv_len, block_table)
-    T, max_pos = qkv.shape[0], cos_sin.shape[0]
-    pq = _arg("qkv", qkv, _BF16, (T, (num_heads + 2 * kv_heads) * dim))
-    pcs = _arg("cos_sin", cos_sin, _F32, (max_pos, dim))
-    if out is None:
-        out = qkv.new_empty((T, num_heads, dim))
-        po = out.data_ptr()
-    else:
-        po = _arg("out", out, _BF16, (T, num_heads, dim))
-    code = _lib.load().qil_rope_append(pq, pcs, po, pk, pv, pc, pl, pt, T, seqs, num_heads, kv_heads, dim, page, pages, width, max_pos,
-                                       _current(qkv))
-    if code:
-        _check(code)
-    return out
+    return _call("rope_append", stream, qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads, out)
 
 
 def attn_paged_workspace_size(total_q: int, num_seqs: int, num_heads: int, num_kv_heads: int, head_dim: int, max_q_len: int,
@@ -504,25 +414,7 @@ def attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len: int, m
                out=None, workspace=None, stream=None):
     """Causal attention of the new tokens q [T][H][D] of all requests over the paged cache (which holds them already).
     max_q_len, max_kv_len bound the requests' lengths; scale defaults to D ** -0.5."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
-    pages, kv_heads, page, dim, seqs, width, pk, pv, pc, pl, pt = _paged_args(k_cache, v_cache, cu_q, kv_len, block_table)
-    T, heads, _ = shape = q.shape
-    pq = _arg("q", q, _BF16, (T, heads, dim))
-    if out is None:
-        out = torch.empty_like(q)
-        po = out.data_ptr()
-    else:
-        po = _arg("out", out, _BF16, shape)
-    if workspace is None:
-        workspace = new_workspace(attn_paged_workspace_size(T, seqs, heads, kv_heads, dim, max_q_len, max_kv_len), q.device)
-    pw, nbytes = _workspace(workspace)
-    code = _lib.load().qil_attn_paged(pq, pk, pv, po, pc, pl, pt, T, seqs, heads, kv_heads, dim, page, pages, width, max_q_len,
-                                      max_kv_len, dim ** -0.5 if scale is None else scale, pw, nbytes, _current(q))
-    if code:
-        _check(code)
-    return out
+    return _call("attn_paged", stream, q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
 
 
 def lora_batch_workspace_size(M: int, num_seqs: int, rank: int) -> int:
@@ -533,24 +425,4 @@ def lora_batch_add(x, a, b, y, cu_q, adapter, scales, out=None, workspace=None, 
     """out = y + scales[i] * (x . a[i]^T) . b[i]^T with i = adapter[request of the row]; requests whose adapter is negative
     have none.  a [n][r][K], b [n][N][r], r <= 64.  x, y and out may be column slices of wider tensors; without out, y is
     updated in place.  Returns out (or y)."""
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return lora_batch_add(x, a, b, y, cu_q, adapter, scales, out, workspace)
-    M, K = x.shape
-    n, N, r = shape = b.shape
-    px, ldx = _arg_rows("x", x, M, K)
-    py, ldy = _arg_rows("y", y, M, N)
-    if out is None:
-        out, po, ldo = y, py, ldy
-    else:
-        po, ldo = _arg_rows("out", out, M, N)
-    seqs = adapter.shape[0]
-    if workspace is None:
-        workspace = torch.empty(max(lora_batch_workspace_size(M, seqs, r), 16), dtype=torch.uint8, device=x.device)
-    pw, nbytes = _workspace(workspace)
-    code = _lib.load().qil_lora_batch_add(px, _arg("a", a, _BF16, (n, r, K)), _arg("b", b, _BF16, shape), py, po,
-                                          _arg("cu_q", cu_q, _I32, (seqs + 1,)), _arg("adapter", adapter, _I32, (seqs,)),
-                                          _arg("scales", scales, _F32, (n,)), M, N, K, r, seqs, n, ldx, ldy, ldo, pw, nbytes, _current(x))
-    if code:
-        _check(code)
-    return out
+    return _call("lora_batch_add", stream, x, a, b, y, cu_q, adapter, scales, out, workspace)
