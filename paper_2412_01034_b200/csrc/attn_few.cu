@@ -19,10 +19,10 @@ namespace {
 
 constexpr int kWarps = 4, kTile = 16;
 
-template <int kDim>
+template <int kDim, bool kDeep>
 struct FewShape {
     static constexpr int kTileBytes = kTile * kDim * 2;
-    static constexpr int kStages = kDim == 128 ? 3 : 6;
+    static constexpr int kStages = (kDeep ? 6 : 3) * (128 / kDim);   // 96 KB a block, two blocks an SM; deep: 192 KB
     static constexpr int kWarpBytes = kStages * 2 * kTileBytes;
     static constexpr int kSmem = kWarps * kWarpBytes;
     static_assert(kWarps * kTile * kDim * 4 <= kSmem, "the warps' results fit where the rings were");
@@ -46,9 +46,9 @@ __device__ __forceinline__ float quad_sum(float v) {
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-template <int kDim>
+template <int kDim, bool kDeep>
 __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams p) {
-    using Shape = FewShape<kDim>;
+    using Shape = FewShape<kDim, kDeep>;
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kPieces = kDim / 8;   // 16-byte pieces of a row
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float s_m[kWarps][16], s_l[kWarps][16];
@@ -67,15 +67,6 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     const int tiles = (stop - begin + kTile - 1) / kTile;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
 
-    // the query rows as the A operand: lane (g, c) holds rows g, g + 8, columns 16 k + 2 c ..., 16 k + 8 + 2 c ...
-    uint32_t qa[kDim / 16][4];
-#pragma unroll
-    for (int k = 0; k < kDim / 16; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int r = g + 8 * (e & 1), d = 16 * k + 2 * c + 8 * (e >> 1);
-            qa[k][e] = r < rows ? *reinterpret_cast<const uint32_t*>(p.q + ((size_t)(row0 + r / G) * H + kvh * G + r % G) * kDim + d) : 0u;
-        }
     // visible tokens of this lane's two rows
     int see[2];
 #pragma unroll
@@ -83,14 +74,13 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     const int all_see = min(first_pos + 1, end);   // every row sees what the first new token sees
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * Shape::kWarpBytes;
-    auto page_of = [&](int i) -> int {   // page of tile i (-1: none)
-        const int tok = begin + i * kTile;
-        return tok < stop ? __ldg(table + tok / p.c.page_size) : -1;
+    auto page_of = [&](int i) -> int {   // page of tile i (of the last tile where there is none)
+        return __ldg(table + (min(begin + i * kTile, stop - 1) >> p.page_shift));
     };
     auto fetch = [&](int i, int stage, int page) {
         const int tok = begin + i * kTile;
         const bool there = page >= 0 && page < p.c.num_pages;
-        const size_t at = there ? (((size_t)page * p.c.num_kv_heads + kvh) * p.c.page_size + tok % p.c.page_size) * kDim : 0;
+        const size_t at = there ? (((size_t)page * p.c.num_kv_heads + kvh) * p.c.page_size + (tok & (p.c.page_size - 1))) * kDim : 0;
         const uint32_t dst = ring + stage * 2 * kTileBytes;
 #pragma unroll
         for (int j = 0; j < kTile * kPieces / 32; ++j) {
@@ -110,7 +100,7 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
         for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
 
     int ahead = warp;               // the next tile to fetch
-    int page = page_of(ahead);
+    int page = tiles > 0 ? page_of(ahead) : 0;
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
         if (ahead < tiles) {
@@ -120,6 +110,20 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
         }
         ahead += kWarps;
         asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // The query rows as the A operand: lane (g, c) holds rows g, g + 8, columns 16 k + 2 c ..., 16 k + 8 + 2 c ...  (Rows past
+    // the last one repeat it: nothing reads their results, and a condition around each load would make the loads wait for
+    // one another.)
+    uint32_t qa[kDim / 16][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = min(g + 8 * h, rows - 1), tok = r / G;
+        const __nv_bfloat16* row = p.q + ((size_t)(row0 + tok) * H + kvh * G + (r - tok * G)) * kDim + 2 * c;
+#pragma unroll
+        for (int k = 0; k < kDim / 16; ++k) {
+            qa[k][h] = __ldg(reinterpret_cast<const uint32_t*>(row + 16 * k));
+            qa[k][2 + h] = __ldg(reinterpret_cast<const uint32_t*>(row + 16 * k + 8));
+        }
     }
     int stage = 0, into = kStages - 1;
     // ldmatrix addresses: lane i supplies row i % 16 (keys: tokens; values: tokens), column half i / 16
@@ -284,17 +288,23 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     }
 }
 
-template <int kDim>
+template <int kDim, bool kDeep>
 qil_status go(const AttnParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(attn_few_kernel<kDim>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
+    constexpr int kSmem = FewShape<kDim, kDeep>::kSmem;
+    if (!allow_smem(attn_few_kernel<kDim, kDeep>, kSmem, allowed)) return QIL_ERR_CUDA;
     const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)p.c.num_seqs);
-    attn_few_kernel<kDim><<<grid, 32 * kWarps, FewShape<kDim>::kSmem, st>>>(p);
+    attn_few_kernel<kDim, kDeep><<<grid, 32 * kWarps, kSmem, st>>>(p);
     return launch_status();
 }
 
 }  // namespace
 
-qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) { return p.c.head_dim == 128 ? go<128>(p, st) : go<64>(p, st); }
+// Where every block can have an SM of its own, its rings take twice the tiles ahead.
+qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) {
+    const bool deep = (long long)p.slots * p.c.num_kv_heads * p.c.num_seqs <= num_sms();
+    if (p.c.head_dim == 128) return deep ? go<128, true>(p, st) : go<128, false>(p, st);
+    return deep ? go<64, true>(p, st) : go<64, false>(p, st);
+}
 
 }  // namespace qil

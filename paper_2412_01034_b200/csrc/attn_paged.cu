@@ -26,13 +26,11 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
     // every request has more than kFewRows rows if the others at their longest leave more for it
     pl.few = !(((long long)total_q - (long long)(num_seqs - 1) * max_q) * G > kFewRows);
     if (pl.few) {
-        // Two blocks fit an SM.  Up to one round of blocks where the requests are few; about eight rounds, of at most 1024
-        // tokens each, where they are many (their lengths differ, and the rounds even that out).
+        // Two blocks fit an SM: one round of blocks, each of 384 tokens at least (a block's start and its part's way through
+        // the workspace cost as much as 300 tokens) and 2048 at most (the requests' lengths differ).
         const long long items = (long long)num_seqs * Hk, room = 2 * sms;
-        const long long blocks = items * 2 <= room ? room : 8 * room;
-        long long chunk = (max_kv * items + blocks - 1) / blocks;
-        chunk = (chunk + 63) / 64 * 64;
-        if (items * 2 > room && chunk > 1024) chunk = 1024;
+        long long chunk = (max_kv * items + room - 1) / room;
+        chunk = chunk < 384 ? 384 : chunk > 2048 ? 2048 : (chunk + 63) / 64 * 64;
         pl.chunk = (int)chunk;
         pl.slots = (int)((max_kv + chunk - 1) / chunk);
         const long long rows = (long long)max_q * G;
@@ -74,6 +72,7 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     p.c = c;
     p.G = c.num_heads / c.num_kv_heads;
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.page_shift = c.page_size == 16 ? 4 : c.page_size == 32 ? 5 : c.page_size == 64 ? 6 : 7;
     p.chunk = pl.chunk;
     p.slots = pl.slots;
     p.few_rows = pl.few_rows;

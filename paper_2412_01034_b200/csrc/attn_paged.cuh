@@ -19,6 +19,7 @@ struct AttnParams {
     PagedCache c;
     int G;               // query heads of a key head
     float scale_log2;    // scale * log2(e)
+    int page_shift;      // log2 of the page size
     int chunk;           // few rows: cached tokens of one block
     int slots;           // few rows: blocks per request and key head at most
     int few_rows;        // few rows: rows of a part in the workspace

@@ -46,33 +46,49 @@ __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const 
         for (int n = 0; n < kNR; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[m][n][e] = 0.f;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    // Rows past the tile's last and rank rows past the last repeat the last one (nobody reads their results) and the block
+    // of K that reaches beyond K is cleared: with a condition around each load the loads would wait for one another.
+    const __nv_bfloat16 *xr[kMT][2], *ar[kNR];
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) xr[m][h] = p.x + min(row0 + 16 * m + 8 * h + g, row1 - 1) * p.ldx;
+#pragma unroll
+    for (int n = 0; n < kNR; ++n) ar[n] = a + (size_t)min(8 * n + g, p.rank - 1) * p.K;
     const int first = blockIdx.y * p.slice_blocks, last = min(first + p.slice_blocks, (p.K + 31) / 32);
-#pragma unroll 2
-    for (int kb = first + warp; kb < last; kb += kDownWarps) {
-        const int k = kb * 32 + c * 8;      // this lane's 8 columns (K is a multiple of 8: all or none of them exist)
-        const bool in = k < p.K;
-        uint4 xv[kMT][2], av[kNR];
+    uint4 xv[kMT][2], av[kNR];
+    auto load = [&](int kb) {
+        const int at = min(kb * 32 + c * 8, p.K - 8);   // this lane's 8 columns (K is a multiple of 8: all or none of them exist)
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = row0 + 16 * m + 8 * h + g;
-                xv[m][h] = in && row < row1 ? *reinterpret_cast<const uint4*>(p.x + row * p.ldx + k) : zero;
-            }
+            for (int h = 0; h < 2; ++h) xv[m][h] = __ldg(reinterpret_cast<const uint4*>(xr[m][h] + at));
 #pragma unroll
-        for (int n = 0; n < kNR; ++n) {
-            const int j = 8 * n + g;
-            av[n] = in && j < p.rank ? *reinterpret_cast<const uint4*>(a + (size_t)j * p.K + k) : zero;
+        for (int n = 0; n < kNR; ++n) av[n] = __ldg(reinterpret_cast<const uint4*>(ar[n] + at));
+    };
+    if (first + warp < last) load(first + warp);
+#pragma unroll 1
+    for (int kb = first + warp; kb < last; kb += kDownWarps) {
+        uint4 xn[kMT][2], an[kNR];
+#pragma unroll
+        for (int m = 0; m < kMT; ++m) xn[m][0] = xv[m][0], xn[m][1] = xv[m][1];
+#pragma unroll
+        for (int n = 0; n < kNR; ++n) an[n] = av[n];
+        load(min(kb + kDownWarps, last - 1));           // (the next block's operands are on the way during the products)
+        if (kb * 32 + 32 > p.K && kb * 32 + c * 8 >= p.K) {
+#pragma unroll
+            for (int m = 0; m < kMT; ++m) xn[m][0] = xn[m][1] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int n = 0; n < kNR; ++n) an[n] = make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll
         for (int m = 0; m < kMT; ++m) {
-            const uint32_t a0[4] = {xv[m][0].x, xv[m][1].x, xv[m][0].y, xv[m][1].y};
-            const uint32_t a1[4] = {xv[m][0].z, xv[m][1].z, xv[m][0].w, xv[m][1].w};
+            const uint32_t a0[4] = {xn[m][0].x, xn[m][1].x, xn[m][0].y, xn[m][1].y};
+            const uint32_t a1[4] = {xn[m][0].z, xn[m][1].z, xn[m][0].w, xn[m][1].w};
 #pragma unroll
             for (int n = 0; n < kNR; ++n) {
-                mma16816(acc[m][n], a0, av[n].x, av[n].y);
-                mma16816(acc[m][n], a1, av[n].z, av[n].w);
+                mma16816(acc[m][n], a0, an[n].x, an[n].y);
+                mma16816(acc[m][n], a1, an[n].z, an[n].w);
             }
         }
     }
@@ -106,7 +122,7 @@ __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const 
 }
 
 template <int kMT, int kNR>
-__global__ void __launch_bounds__(32 * kUpWarps) lora_batch_up_kernel(const LoraParams p) {
+__global__ void __launch_bounds__(32 * kUpWarps, 2) lora_batch_up_kernel(const LoraParams p) {
     constexpr int kRank = 8 * kNR, kW = kRank / 4, kSteps = kRank <= 16 ? 1 : kRank / 16;   // kW: rank elements of a lane
     // t as the A operand of the products, in the order of the lanes' registers: [row tile][step][hi, lo][lane][4 words]
     __shared__ __align__(16) uint32_t frag[kMT * kSteps * 2 * 32 * 4];
@@ -117,41 +133,44 @@ __global__ void __launch_bounds__(32 * kUpWarps) lora_batch_up_kernel(const Lora
     const bool none = ad < 0 || ad >= p.num_adapters;
     if (none && p.out == p.y) return;
     const int n0 = (blockIdx.y * kUpWarps + warp) * 32;
+    const int n = n0 + 8 * c;      // this lane's 8 outputs (N is a multiple of 8: all or none of them exist)
+    // y first: the longest way.  (Rows past the tile's last and columns past N repeat others and are not written.)
+    uint4 yv[kMT][2];
+#pragma unroll
+    for (int m = 0; m < kMT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            yv[m][h] = *reinterpret_cast<const uint4*>(p.y + min(row0 + 16 * m + 8 * h + g, row1 - 1) * p.ldy + min(n, p.N - 8));
     uint4 bq[4][kW == 16 ? 2 : 1];
     if (!none) {
-        // B rows of this warp's 32 columns: column (2c, 2c + 1) of result tile i is output n0 + 8 c + 2 i, + 1
+        // B rows of this warp's 32 columns: column (2c, 2c + 1) of result tile i is output n0 + 8 c + 2 i, + 1.  (Columns and
+        // rank elements that do not exist repeat others; the latter meet zeros of t, the former are not written.)
         const __nv_bfloat16* b = p.b + (size_t)ad * p.N * p.rank;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int n = n0 + 8 * (g >> 1) + 2 * i + (g & 1);
-            const __nv_bfloat16* row = b + (size_t)n * p.rank + kW * c;
+            const __nv_bfloat16* row = b + (size_t)min(n0 + 8 * (g >> 1) + 2 * i + (g & 1), p.N - 1) * p.rank;
 #pragma unroll
             for (int h = 0; h < (kW == 16 ? 2 : 1); ++h) {
-                bq[i][h] = make_uint4(0u, 0u, 0u, 0u);
-                if (n < p.N && kW * c + 8 * h < p.rank) {
-                    if (kW == 2) bq[i][h].x = *reinterpret_cast<const uint32_t*>(row);
-                    else if (kW == 4) {
-                        const uint2 v = *reinterpret_cast<const uint2*>(row);
-                        bq[i][h].x = v.x;
-                        bq[i][h].y = v.y;
-                    } else bq[i][h] = *reinterpret_cast<const uint4*>(row + 8 * h);
-                }
+                const __nv_bfloat16* from = row + min(kW * c + 8 * h, p.rank - (kW < 8 ? kW : 8));
+                if (kW == 2) bq[i][h] = make_uint4(__ldg(reinterpret_cast<const uint32_t*>(from)), 0u, 0u, 0u);
+                else if (kW == 4) {
+                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(from));
+                    bq[i][h] = make_uint4(v.x, v.y, 0u, 0u);
+                } else bq[i][h] = __ldg(reinterpret_cast<const uint4*>(from));
             }
         }
         const float scale = __ldg(p.scales + ad);
         for (int i = threadIdx.x; i < kMT * 16 * (kRank / 2); i += blockDim.x) {
             const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
+            const float* t = p.t + (size_t)min(row0 + m, row1 - 1) * p.rank + min(j, p.rank - 2);
             float2 v = make_float2(0.f, 0.f);
-            if (row0 + m < row1 && j < p.rank) {
-                const float* t = p.t + (size_t)(row0 + m) * p.rank + j;
-                for (int s = 0; s < p.slices; ++s) {
-                    const float2 u = *reinterpret_cast<const float2*>(t + (size_t)s * p.M * p.rank);
-                    v.x += u.x;
-                    v.y += u.y;
-                }
-                v.x *= scale;
-                v.y *= scale;
+            for (int s = 0; s < p.slices; ++s) {
+                const float2 u = *reinterpret_cast<const float2*>(t + (size_t)s * p.M * p.rank);
+                v.x += u.x;
+                v.y += u.y;
             }
+            v.x = j < p.rank ? v.x * scale : 0.f;
+            v.y = j < p.rank ? v.y * scale : 0.f;
             const uint32_t hi = pack2(v.x, v.y);
             const uint32_t lo = pack2(v.x - __uint_as_float(hi << 16), v.y - __uint_as_float(hi & 0xFFFF0000u));
             const int at = j % kW, step = at >> 2, reg = ((m & 15) >> 3) + 2 * ((at & 3) >> 1);
@@ -161,7 +180,6 @@ __global__ void __launch_bounds__(32 * kUpWarps) lora_batch_up_kernel(const Lora
         }
     }
     __syncthreads();
-    const int n = n0 + 8 * c;      // this lane's 8 outputs (N is a multiple of 8: all or none of them exist)
     if (n0 >= p.N) return;
 #pragma unroll
     for (int m = 0; m < kMT; ++m) {
@@ -190,7 +208,7 @@ __global__ void __launch_bounds__(32 * kUpWarps) lora_batch_up_kernel(const Lora
             const int row = row0 + 16 * m + 8 * h + g;
             if (row < row1 && n < p.N) {
                 float o[8];
-                unpack8(*reinterpret_cast<const uint4*>(p.y + row * p.ldy + n), o);
+                unpack8(yv[m][h], o);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     o[2 * i] += acc[i][2 * h];
