@@ -328,7 +328,7 @@ qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const
         return QIL_ERR_SHAPE;
     if (ldx < K || ldy < N || ldo < N || ldx % 8 != 0 || ldy % 8 != 0 || ldo % 8 != 0 || (out == y && ldo != ldy)) return QIL_ERR_SHAPE;
     if (rank > 64) return QIL_ERR_UNSUPPORTED;
-    if ((N + 255) / 256 > 65535) return QIL_ERR_SHAPE;   // (grid size)
+    if ((N + 127) / 128 > 65535) return QIL_ERR_SHAPE;   // (grid size)
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) || !aligned4(cu_q) ||
         !aligned4(adapter) || !aligned4(scales))
         return QIL_ERR_ALIGN;

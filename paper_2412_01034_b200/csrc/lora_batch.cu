@@ -17,7 +17,7 @@ namespace qil {
 
 namespace {
 
-constexpr int kDownWarps = 4, kUpWarps = 8, kMaxSlices = 32;
+constexpr int kDownWarps = 4, kUpWarps = 4, kUpBlocks = 3, kMaxSlices = 32;   // kUpBlocks: blocks of the second kernel per SM
 
 struct LoraParams {
     const __nv_bfloat16 *x, *a, *b, *y;
@@ -34,6 +34,7 @@ template <int kMT, int kNR>
 __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const LoraParams p) {
     __shared__ float part[kDownWarps - 1][kMT * kNR * 4 * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the second kernel's blocks may come up as these leave
     int seq, row0, row1;
     if (!find_tile(p.cu, p.num_seqs, p.M, 16 * kMT, blockIdx.x, seq, row0, row1)) return;
     const int ad = __ldg(p.adapter + seq);
@@ -121,9 +122,12 @@ __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const 
         }
 }
 
+// A warp takes groups of 32 outputs in turn, with the next group's y and B on the way while it works: a block's way to its
+// first product (the request, its adapter, t) is several trips to memory long and is paid once.
 template <int kMT, int kNR>
-__global__ void __launch_bounds__(32 * kUpWarps, 2) lora_batch_up_kernel(const LoraParams p) {
+__global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel(const LoraParams p) {
     constexpr int kRank = 8 * kNR, kW = kRank / 4, kSteps = kRank <= 16 ? 1 : kRank / 16;   // kW: rank elements of a lane
+    constexpr int kBQ = kW == 16 ? 2 : 1;
     // t as the A operand of the products, in the order of the lanes' registers: [row tile][step][hi, lo][lane][4 words]
     __shared__ __align__(16) uint32_t frag[kMT * kSteps * 2 * 32 * 4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -132,25 +136,22 @@ __global__ void __launch_bounds__(32 * kUpWarps, 2) lora_batch_up_kernel(const L
     const int ad = __ldg(p.adapter + seq);
     const bool none = ad < 0 || ad >= p.num_adapters;
     if (none && p.out == p.y) return;
-    const int n0 = (blockIdx.y * kUpWarps + warp) * 32;
-    const int n = n0 + 8 * c;      // this lane's 8 outputs (N is a multiple of 8: all or none of them exist)
-    // y first: the longest way.  (Rows past the tile's last and columns past N repeat others and are not written.)
-    uint4 yv[kMT][2];
+    const __nv_bfloat16* b = p.b + (size_t)(none ? 0 : ad) * p.N * p.rank;
+    // Rows past the tile's last, columns past N and rank elements past the rank repeat others: the first two are not
+    // written, the last meet zeros of t.  (Conditions around the loads would make them wait for one another.)
+    uint4 yv[kMT][2], bq[4][kBQ];
+    auto load = [&](int n0) {
 #pragma unroll
-    for (int m = 0; m < kMT; ++m)
+        for (int m = 0; m < kMT; ++m)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            yv[m][h] = *reinterpret_cast<const uint4*>(p.y + min(row0 + 16 * m + 8 * h + g, row1 - 1) * p.ldy + min(n, p.N - 8));
-    uint4 bq[4][kW == 16 ? 2 : 1];
-    if (!none) {
-        // B rows of this warp's 32 columns: column (2c, 2c + 1) of result tile i is output n0 + 8 c + 2 i, + 1.  (Columns and
-        // rank elements that do not exist repeat others; the latter meet zeros of t, the former are not written.)
-        const __nv_bfloat16* b = p.b + (size_t)ad * p.N * p.rank;
+            for (int h = 0; h < 2; ++h)
+                yv[m][h] = *reinterpret_cast<const uint4*>(p.y + min(row0 + 16 * m + 8 * h + g, row1 - 1) * p.ldy + min(n0 + 8 * c, p.N - 8));
+        // B rows of the 32 columns: column (2c, 2c + 1) of result tile i is output n0 + 8 c + 2 i, + 1
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const __nv_bfloat16* row = b + (size_t)min(n0 + 8 * (g >> 1) + 2 * i + (g & 1), p.N - 1) * p.rank;
 #pragma unroll
-            for (int h = 0; h < (kW == 16 ? 2 : 1); ++h) {
+            for (int h = 0; h < kBQ; ++h) {
                 const __nv_bfloat16* from = row + min(kW * c + 8 * h, p.rank - (kW < 8 ? kW : 8));
                 if (kW == 2) bq[i][h] = make_uint4(__ldg(reinterpret_cast<const uint32_t*>(from)), 0u, 0u, 0u);
                 else if (kW == 4) {
@@ -159,13 +160,20 @@ __global__ void __launch_bounds__(32 * kUpWarps, 2) lora_batch_up_kernel(const L
                 } else bq[i][h] = __ldg(reinterpret_cast<const uint4*>(from));
             }
         }
-        const float scale = __ldg(p.scales + ad);
+    };
+    int n0 = (blockIdx.y * kUpWarps + warp) * 32;
+    const int stride = gridDim.y * kUpWarps * 32;
+    load(n0);
+    const float scale = __ldg(p.scales + (none ? 0 : ad));
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // t is written by the kernel before, which may still be running
+    if (!none) {
         for (int i = threadIdx.x; i < kMT * 16 * (kRank / 2); i += blockDim.x) {
             const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
             const float* t = p.t + (size_t)min(row0 + m, row1 - 1) * p.rank + min(j, p.rank - 2);
             float2 v = make_float2(0.f, 0.f);
+#pragma unroll 4
             for (int s = 0; s < p.slices; ++s) {
-                const float2 u = *reinterpret_cast<const float2*>(t + (size_t)s * p.M * p.rank);
+                const float2 u = __ldcg(reinterpret_cast<const float2*>(t + (size_t)s * p.M * p.rank));
                 v.x += u.x;
                 v.y += u.y;
             }
@@ -180,41 +188,52 @@ __global__ void __launch_bounds__(32 * kUpWarps, 2) lora_batch_up_kernel(const L
         }
     }
     __syncthreads();
-    if (n0 >= p.N) return;
+#pragma unroll 1
+    for (; n0 < p.N; n0 += stride) {
+        uint4 yn[kMT][2], bn[4][kBQ];
 #pragma unroll
-    for (int m = 0; m < kMT; ++m) {
-        float acc[4][4];
+        for (int m = 0; m < kMT; ++m) yn[m][0] = yv[m][0], yn[m][1] = yv[m][1];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
-        if (!none) {
+            for (int h = 0; h < kBQ; ++h) bn[i][h] = bq[i][h];
+        if (n0 + stride < p.N) load(n0 + stride);
+        const int n = n0 + 8 * c;      // this lane's 8 outputs (N is a multiple of 8: all or none of them exist)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
+        for (int m = 0; m < kMT; ++m) {
+            float acc[4][4];
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(frag + ((((m * kSteps + s) * 2) + part) * 32 + lane) * 4);
-                    const uint32_t a[4] = {v.x, v.y, kW == 2 ? 0u : v.z, kW == 2 ? 0u : v.w};
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
+            if (!none) {
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(frag + ((((m * kSteps + s) * 2) + part) * 32 + lane) * 4);
+                        const uint32_t a[4] = {v.x, v.y, kW == 2 ? 0u : v.z, kW == 2 ? 0u : v.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint4 q = bn[i][kW == 16 ? s >> 1 : 0];
+                            if (s & 1) mma16816(acc[i], a, q.z, q.w);
+                            else mma16816(acc[i], a, q.x, kW == 2 ? 0u : q.y);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = row0 + 16 * m + 8 * h + g;
+                if (row < row1 && n < p.N) {
+                    float o[8];
+                    unpack8(yn[m][h], o);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint4 q = bq[i][kW == 16 ? s >> 1 : 0];
-                        if (s & 1) mma16816(acc[i], a, q.z, q.w);
-                        else mma16816(acc[i], a, q.x, kW == 2 ? 0u : q.y);
+                        o[2 * i] += acc[i][2 * h];
+                        o[2 * i + 1] += acc[i][2 * h + 1];
                     }
+                    *reinterpret_cast<uint4*>(p.out + row * p.ldo + n) = pack8(o);
                 }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int row = row0 + 16 * m + 8 * h + g;
-            if (row < row1 && n < p.N) {
-                float o[8];
-                unpack8(yv[m][h], o);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    o[2 * i] += acc[i][2 * h];
-                    o[2 * i + 1] += acc[i][2 * h + 1];
-                }
-                *reinterpret_cast<uint4*>(p.out + row * p.ldo + n) = pack8(o);
             }
         }
     }
@@ -228,10 +247,11 @@ int lora_row_tiles(int M, int num_seqs, int rank) {
 }
 int lora_max_tiles(int M, int num_seqs, int rank) { return M / (16 * lora_row_tiles(M, num_seqs, rank)) + num_seqs; }
 
-// Slices of K for the first kernel: two blocks per SM where the row tiles alone are fewer, at least 256 columns each.
+// Slices of K for the first kernel: one round of two blocks per SM (a second round costs more than longer slices do), at
+// least 256 columns each.
 int lora_batch_slices(int M, int num_seqs, int rank, int K) {
     const int tiles = lora_max_tiles(M, num_seqs, rank);
-    int s = (2 * num_sms() + tiles - 1) / tiles;
+    int s = 2 * num_sms() / tiles;
     s = s < K / 256 ? s : K / 256;
     s = s < kMaxSlices ? s : kMaxSlices;
     return s < 1 ? 1 : s;
@@ -261,17 +281,33 @@ qil_status launch_lora_batch_add(const void* x, const void* a, const void* b, co
     p.slice_blocks = (blocks + p.slices - 1) / p.slices;
     p.slices = (blocks + p.slice_blocks - 1) / p.slice_blocks;
     const unsigned tiles = (unsigned)lora_max_tiles(M, num_seqs, rank);
-    const dim3 down(tiles, (unsigned)p.slices), up(tiles, (unsigned)((N + 32 * kUpWarps - 1) / (32 * kUpWarps)));
+    const int mt = lora_row_tiles(M, num_seqs, rank);
+    // second kernel: one round of blocks, or all the columns there are; with tiles of 16 rows a block's share is too small to
+    // be worth a loop
+    const unsigned groups = (unsigned)((N + 32 * kUpWarps - 1) / (32 * kUpWarps));
+    unsigned across = mt == 1 ? groups : (unsigned)(kUpBlocks * num_sms()) / tiles;
+    if (across < 1) across = 1;
+    if (across > groups) across = groups;
+    const dim3 down(tiles, (unsigned)p.slices), up(tiles, across);
+    cudaError_t e = cudaSuccess;
     auto go = [&](auto kd, auto ku) {
         kd<<<down, 32 * kDownWarps, 0, st>>>(p);
-        ku<<<up, 32 * kUpWarps, 0, st>>>(p);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = up;
+        cfg.blockDim = dim3(32 * kUpWarps);
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, ku, p);
     };
-    const int mt = lora_row_tiles(M, num_seqs, rank);
     if (rank <= 8) mt == 1 ? go(lora_batch_down_kernel<1, 1>, lora_batch_up_kernel<1, 1>) : go(lora_batch_down_kernel<4, 1>, lora_batch_up_kernel<4, 1>);
     else if (rank <= 16) mt == 1 ? go(lora_batch_down_kernel<1, 2>, lora_batch_up_kernel<1, 2>) : go(lora_batch_down_kernel<4, 2>, lora_batch_up_kernel<4, 2>);
     else if (rank <= 32) mt == 1 ? go(lora_batch_down_kernel<1, 4>, lora_batch_up_kernel<1, 4>) : go(lora_batch_down_kernel<4, 4>, lora_batch_up_kernel<4, 4>);
     else mt == 1 ? go(lora_batch_down_kernel<1, 8>, lora_batch_up_kernel<1, 8>) : go(lora_batch_down_kernel<2, 8>, lora_batch_up_kernel<2, 8>);
-    return launch_status();
+    return e == cudaSuccess ? launch_status() : QIL_ERR_CUDA;
 }
 
 }  // namespace qil
