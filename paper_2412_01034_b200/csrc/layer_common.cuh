@@ -42,6 +42,27 @@ __device__ __forceinline__ int request_of_row(const int* __restrict__ cu, int nu
     return b;
 }
 
+// The same with what a kernel needs next, in one trip to memory: the request's rows [lo, hi) and its number of cached
+// tokens.  False when no request holds the row.
+__device__ __forceinline__ bool request_at_row(const int* __restrict__ cu, const int* __restrict__ kv_len, int num_seqs, int total, int t,
+                                               int& seq, int& lo, int& hi, int& kv) {
+    const int lane = threadIdx.x & 31;
+    for (int base = 0; base < num_seqs; base += 32) {
+        const int b = min(base + lane, num_seqs - 1);
+        const int start = __ldg(cu + b), end = __ldg(cu + b + 1), len = __ldg(kv_len + b);
+        const unsigned past = __ballot_sync(0xffffffffu, base + lane < num_seqs && end > t);
+        if (past) {
+            const int who = __ffs(past) - 1;
+            seq = base + who;
+            lo = min(max(__shfl_sync(0xffffffffu, start, who), 0), total);
+            hi = min(max(__shfl_sync(0xffffffffu, end, who), lo), total);
+            kv = __shfl_sync(0xffffffffu, len, who);
+            return true;
+        }
+    }
+    return false;
+}
+
 // Packed rows are cut into tiles of `rows`, each request on its own (its last tile may be short): the request and the
 // first row of tile t, or false when there are fewer tiles.  All 32 lanes of a warp take part and get the same answer.
 __device__ __forceinline__ bool find_tile(const int* __restrict__ cu, int num_seqs, int total, int rows, int t, int& seq, int& row0, int& row1) {
