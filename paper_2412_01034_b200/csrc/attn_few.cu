@@ -56,16 +56,20 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
+    const int begin = split * p.chunk;
+    const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
+    // (the first tile's page and the length are on the way with the starts, not after them)
+    const int kv = __ldg(p.c.kv_len + seq);
+    int page = __ldg(table + min((begin + (int)(threadIdx.x >> 5) * kTile) >> p.page_shift, p.c.max_pages - 1));
     int row0, row1;
     request_rows(p.c.cu_q, seq, p.c.total_q, row0, row1);
     const int q_len = row1 - row0;
     if (q_len <= 0 || q_len * (long long)G > kFewRows) return;
-    const int rows = q_len * G, end = cache_end(p.c, seq), first_pos = __ldg(p.c.kv_len + seq) - q_len;
+    const int rows = q_len * G, end = cache_end(p.c, kv), first_pos = kv - q_len;
     const int parts = max(1, min((end + p.chunk - 1) / p.chunk, p.slots));
     if (split >= parts) return;
-    const int begin = split * p.chunk, stop = split + 1 == parts ? end : min(begin + p.chunk, end);
+    const int stop = split + 1 == parts ? end : min(begin + p.chunk, end);
     const int tiles = (stop - begin + kTile - 1) / kTile;
-    const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
 
     // visible tokens of this lane's two rows
     int see[2];
@@ -100,7 +104,6 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
         for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
 
     int ahead = warp;               // the next tile to fetch
-    int page = tiles > 0 ? page_of(ahead) : 0;
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
         if (ahead < tiles) {

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     // row r of tile i is new token (2 pair + i) tile_tokens + r / G, query head kvh G + r % G; `tokens` of them are the request's
     const int token0 = pair * 2 * p.tile_tokens;
     const int tokens[2] = {min(p.tile_tokens, q_hi - q_lo - token0), min(p.tile_tokens, q_hi - q_lo - token0 - p.tile_tokens)};
-    const int end = cache_end(p.c, seq), first_pos = __ldg(p.c.kv_len + seq) - (q_hi - q_lo);
+    const int kv = __ldg(p.c.kv_len + seq), end = cache_end(p.c, kv), first_pos = kv - (q_hi - q_lo);
     // cached tokens that a new token sees; tiles of them that row tile i needs, cut to this block's part of the cache
     auto visible = [&](int token) { return max(0, min(first_pos + token + 1, end)); };
     int need[2];

@@ -31,9 +31,7 @@ struct AttnParams {
 };
 
 // cached tokens that the table can name
-__device__ __forceinline__ int cache_end(const PagedCache& c, int seq) {
-    return min(max(__ldg(c.kv_len + seq), 0), c.max_pages * c.page_size);
-}
+__device__ __forceinline__ int cache_end(const PagedCache& c, int kv_len) { return min(max(kv_len, 0), c.max_pages * c.page_size); }
 
 __device__ __forceinline__ float fast_exp2(float x) {
     float y;
