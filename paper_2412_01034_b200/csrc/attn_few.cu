@@ -19,10 +19,10 @@ namespace {
 
 constexpr int kWarps = 4, kTile = 16;
 
-template <int kDim, bool kDeep>
+template <int kDim>
 struct FewShape {
     static constexpr int kTileBytes = kTile * kDim * 2;
-    static constexpr int kStages = (kDeep ? 6 : 3) * (128 / kDim);   // 96 KB a block, two blocks an SM; deep: 192 KB
+    static constexpr int kStages = 3 * (128 / kDim);   // 96 KB a block, two blocks an SM
     static constexpr int kWarpBytes = kStages * 2 * kTileBytes;
     static constexpr int kSmem = kWarps * kWarpBytes;
     static_assert(kWarps * kTile * kDim * 4 <= kSmem, "the warps' results fit where the rings were");
@@ -46,9 +46,9 @@ __device__ __forceinline__ float quad_sum(float v) {
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-template <int kDim, bool kDeep>
+template <int kDim>
 __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams p) {
-    using Shape = FewShape<kDim, kDeep>;
+    using Shape = FewShape<kDim>;
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kPieces = kDim / 8;   // 16-byte pieces of a row
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float s_m[kWarps][16], s_l[kWarps][16];
@@ -56,6 +56,8 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
+    // (the kernel for many rows reads nothing of this one's results: its blocks may come up as these leave)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int begin = split * p.chunk;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
     // (the first tile's page and the length are on the way with the starts, not after them)
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     }
     // a part: few_rows x kDim accumulators, then few_rows maxima and few_rows sums
     const size_t part_floats = (size_t)p.few_rows * (kDim + 2);
-    float* mine = p.parts + (((size_t)seq * p.c.num_kv_heads + kvh) * p.slots + split) * part_floats;
+    float* mine = p.few_parts + (((size_t)seq * p.c.num_kv_heads + kvh) * p.slots + split) * part_floats;
     for (int at = 2 * tid; at < rows * kDim; at += 2 * blockDim.x) *reinterpret_cast<float2*>(mine + at) = joined(at);
     if (tid < rows) {
         mine[p.few_rows * kDim + tid] = s_scale[0][tid];
@@ -291,23 +293,17 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     }
 }
 
-template <int kDim, bool kDeep>
+template <int kDim>
 qil_status go(const AttnParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
-    constexpr int kSmem = FewShape<kDim, kDeep>::kSmem;
-    if (!allow_smem(attn_few_kernel<kDim, kDeep>, kSmem, allowed)) return QIL_ERR_CUDA;
+    if (!allow_smem(attn_few_kernel<kDim>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
     const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)p.c.num_seqs);
-    attn_few_kernel<kDim, kDeep><<<grid, 32 * kWarps, kSmem, st>>>(p);
+    attn_few_kernel<kDim><<<grid, 32 * kWarps, FewShape<kDim>::kSmem, st>>>(p);
     return launch_status();
 }
 
 }  // namespace
 
-// Where every block can have an SM of its own, its rings take twice the tiles ahead.
-qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) {
-    const bool deep = (long long)p.slots * p.c.num_kv_heads * p.c.num_seqs <= num_sms();
-    if (p.c.head_dim == 128) return deep ? go<128, true>(p, st) : go<128, false>(p, st);
-    return deep ? go<64, true>(p, st) : go<64, false>(p, st);
-}
+qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) { return p.c.head_dim == 128 ? go<128>(p, st) : go<64>(p, st); }
 
 }  // namespace qil

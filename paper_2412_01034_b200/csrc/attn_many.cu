@@ -243,6 +243,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // Nothing here depends on the kernel before, but what comes after this launch may: its first block lasts until that
+    // kernel is complete.
+    if (p.after_few && blockIdx.x == 0 && blockIdx.z == 0 && warp == 3) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!found) {   // (the grid is sized for the most tiles that the requests could have)
         if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
         return;
@@ -516,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
             unsigned char* turn = smem + i * kTileBytes + (warp & 3) * (32 * kDim * 2);
             const int w_rows = my_tokens * G - 32 * (warp & 3);   // rows from the warp's first
             if (!whole && live)
-                *reinterpret_cast<float2*>(p.parts + (size_t)p.splits * items * kDim + 2 * ((size_t)blockIdx.z * items + item)) =
+                *reinterpret_cast<float2*>(p.many_parts + (size_t)p.splits * items * kDim + 2 * ((size_t)blockIdx.z * items + item)) =
                     make_float2(ref, sum);
             constexpr int kUnit = kDim * 2 / 16;   // 16-byte pieces of a row and turn: kDim bf16 or kDim / 2 fp32
             const int turns = whole ? 1 : 2, cols = kDim / turns;
@@ -559,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                     const size_t to = (size_t)__shfl_sync(0xffffffffu, item, rr);
                     if (rr >= w_rows) continue;
                     if (whole) *reinterpret_cast<uint4*>(p.out + to * kDim + 8 * at) = v;
-                    else *reinterpret_cast<uint4*>(p.parts + ((size_t)blockIdx.z * items + to) * kDim + h * cols + 4 * at) = v;
+                    else *reinterpret_cast<uint4*>(p.many_parts + ((size_t)blockIdx.z * items + to) * kDim + h * cols + 4 * at) = v;
                 }
                 __syncwarp();
             }
@@ -577,6 +581,7 @@ template <int kDim>
 __global__ void __launch_bounds__(128) attn_many_join_kernel(const AttnParams p) {
     constexpr int kPer = kDim / 32;
     const size_t items = (size_t)p.c.total_q * p.c.num_heads, at = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts
     if (at >= items) return;
     const int lane = threadIdx.x & 31, t = (int)(at / p.c.num_heads);
     const int seq = request_of_row(p.c.cu_q, p.c.num_seqs, t);
@@ -584,7 +589,7 @@ __global__ void __launch_bounds__(128) attn_many_join_kernel(const AttnParams p)
     int lo, hi;
     request_rows(p.c.cu_q, seq, p.c.total_q, lo, hi);
     if ((hi - lo) * p.G <= kFewRows) return;
-    const float2* stats = reinterpret_cast<const float2*>(p.parts + (size_t)p.splits * items * kDim);
+    const float2* stats = reinterpret_cast<const float2*>(p.many_parts + (size_t)p.splits * items * kDim);
     float most = -INFINITY, sum = 0.f, o[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) o[e] = 0.f;
@@ -593,7 +598,7 @@ __global__ void __launch_bounds__(128) attn_many_join_kernel(const AttnParams p)
         const float2 st = stats[s * items + at];
         if (st.y == 0.f) continue;
         const float f = fast_exp2(st.x - most);
-        const float* part = p.parts + (s * items + at) * kDim + lane * kPer;
+        const float* part = p.many_parts + (s * items + at) * kDim + lane * kPer;
         sum = fmaf(st.y, f, sum);
 #pragma unroll
         for (int e = 0; e < kPer; e += 2) {
@@ -661,12 +666,20 @@ qil_status go(const AttnParams& p, cudaStream_t st) {
     if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
     // (heads first, so that the long tiles of all heads start before the short ones of any)
     const dim3 grid((unsigned)((long long)p.c.num_kv_heads * (p.c.total_q / (2 * p.tile_tokens) + p.c.num_seqs)), 1u, (unsigned)p.splits);
-    attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mq, mk, mv, p);
-    if (p.splits > 1) {
-        const long long items = (long long)p.c.total_q * p.c.num_heads;
-        attn_many_join_kernel<kDim><<<(unsigned)((items + 3) / 4), 128, 0, st>>>(p);
+    cudaError_t e;
+    if (p.after_few) {
+        e = launch_early(attn_many_kernel<kDim>, grid, kThreads, kSmem, st, mq, mk, mv, p);
+    } else {
+        attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mq, mk, mv, p);
+        e = cudaGetLastError();
     }
-    return launch_status();
+    if (e == cudaSuccess && p.splits > 1) {
+        const long long items = (long long)p.c.total_q * p.c.num_heads;
+        e = launch_early(attn_many_join_kernel<kDim>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
+    }
+    if (e == cudaSuccess) return QIL_OK;
+    (void)cudaGetLastError();
+    return QIL_ERR_CUDA;
 }
 
 }  // namespace

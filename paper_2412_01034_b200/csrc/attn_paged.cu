@@ -14,7 +14,7 @@ namespace {
 struct AttnPlan {
     bool few, many;
     int chunk, slots, few_rows, splits;
-    size_t counter_bytes, part_floats;
+    size_t counter_bytes, few_floats, many_floats;
 };
 
 AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, int max_kv) {
@@ -36,7 +36,7 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
         const long long rows = (long long)max_q * G;
         pl.few_rows = (int)(rows < kFewRows ? rows : kFewRows);
         pl.counter_bytes = ((size_t)items * sizeof(int) + 255) & ~(size_t)255;
-        if (pl.slots > 1) pl.part_floats = (size_t)items * pl.slots * pl.few_rows * (D + 2);
+        if (pl.slots > 1) pl.few_floats = ((size_t)items * pl.slots * pl.few_rows * (D + 2) + 3) & ~(size_t)3;   // (16-byte stores behind them)
     }
     if (pl.many) {
         // The cache is split where the row tiles alone leave SMs idle, into parts of at least four tiles of 128 tokens.
@@ -44,10 +44,7 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
         long long s = sms / tiles;
         if (s > (max_kv + 511) / 512) s = (max_kv + 511) / 512;
         pl.splits = s < 1 ? 1 : (int)s;
-        if (pl.splits > 1) {
-            const size_t need = (size_t)pl.splits * total_q * H * (D + 2);
-            if (need > pl.part_floats) pl.part_floats = need;
-        }
+        if (pl.splits > 1) pl.many_floats = (size_t)pl.splits * total_q * H * (D + 2);
     }
     return pl;
 }
@@ -58,7 +55,7 @@ constexpr size_t kHeader = 256;   // status word
 
 size_t attn_paged_workspace(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int max_q_len, int max_kv_len) {
     const AttnPlan pl = plan_attn(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len);
-    return kHeader + pl.counter_bytes + pl.part_floats * sizeof(float);
+    return kHeader + pl.counter_bytes + (pl.few_floats + pl.many_floats) * sizeof(float);
 }
 
 qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const PagedCache& c, int max_q_len,
@@ -81,7 +78,9 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     char* base = static_cast<char*>(ws);
     p.status = reinterpret_cast<int*>(base);
     p.counters = reinterpret_cast<int*>(base + kHeader);
-    p.parts = reinterpret_cast<float*>(base + kHeader + pl.counter_bytes);
+    p.few_parts = reinterpret_cast<float*>(base + kHeader + pl.counter_bytes);
+    p.many_parts = p.few_parts + pl.few_floats;   // (the two kernels may run at the same time)
+    p.after_few = pl.few;
     if (pl.few) {
         const qil_status s = launch_attn_few(p, st);
         if (s != QIL_OK) return s;

@@ -27,7 +27,8 @@ struct AttnParams {
     int tile_tokens;     // many rows: new tokens of a row tile, kTileRows / G
     int* status;
     int* counters;       // [num_seqs][num_kv_heads] parts written so far, zero between launches
-    float* parts;
+    float *few_parts, *many_parts;
+    bool after_few;      // many rows: the launch follows one of the other kernel
 };
 
 // cached tokens that the table can name
@@ -55,6 +56,22 @@ inline bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
     }
     done.fetch_or(bit, std::memory_order_relaxed);
     return true;
+}
+
+// A launch whose blocks may come up while the kernel before it still runs (see griddepcontrol in the kernels).
+template <class Kernel, class... Args>
+inline cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 qil_status launch_attn_few(const AttnParams& p, cudaStream_t st);
