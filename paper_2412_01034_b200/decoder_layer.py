@@ -1,0 +1,112 @@
+"""One decoder layer of a Llama-2 style backbone (the OpenVLA language model, App. A.4.2) over quantised linears, for a batch
+of requests that are at different places: prompts, chunks of prompts and single tokens together.
+
+The linears are the library's (4-bit weight-only; the fused query / key / value projection optionally W8A8), and what lies
+between them runs on its layer operators: residual norm, rotary embedding with append to the paged cache, attention over
+the cache, low-rank adapters per request.  Weights are quantised on the device once; ``forward`` only enqueues kernels.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+
+import torch
+
+from . import api
+
+GROUP = 128
+
+
+@dataclass
+class Requests:
+    """A batch as the kernels read it (packed rows, lengths, pages, adapters) and the bounds that the host knows."""
+    cu_q: torch.Tensor          # int32 [B + 1]
+    kv_len: torch.Tensor        # int32 [B], the new tokens included
+    block_table: torch.Tensor   # int32 [B][max_pages]
+    adapter: torch.Tensor       # int32 [B], -1: none
+    max_q: int
+    max_kv: int
+
+    @staticmethod
+    def of(q_lens, kv_lens, tables, adapters, device="cuda") -> "Requests":
+        ints = lambda v: torch.tensor(v, dtype=torch.int32, device=device)  # noqa: E731
+        starts = [0]
+        for n in q_lens:
+            starts.append(starts[-1] + n)
+        width = max(1, max(len(t) for t in tables))
+        return Requests(ints(starts), ints(kv_lens), ints([list(t) + [0] * (width - len(t)) for t in tables]), ints(adapters),
+                        max(q_lens), max(kv_lens))
+
+
+class Linear4:
+    """A 4-bit weight-only linear on the canonical layout."""
+
+    def __init__(self, w):
+        self.N, self.K = w.shape
+        self.codes, self.scales, self.zeros = api.quantize_rtn_w4(w, GROUP)
+        self.packed = api.pack_w4(self.codes)
+
+    def __call__(self, x, workspace):
+        return api.linear_w4a16(x, self.packed, self.scales, self.zeros, self.N, GROUP, workspace=workspace)
+
+
+class DecoderLayer:
+    """weights: fp32 CUDA tensors norm1, norm2 [hidden], qkv [(H + 2 Hk) D][hidden], o [hidden][H D], gate, up [ffn][hidden],
+    down [hidden][ffn].  adapters: None or (a [n][r][hidden], b [n][(H + 2 Hk) D][r], scales [n]) beside the qkv projection."""
+
+    def __init__(self, weights, heads, kv_heads, head_dim, num_pages, page_size, max_pos, max_tokens, qkv_bits=4, adapters=None,
+                 eps=1e-5, theta=10000.0):
+        self.heads, self.kv_heads, self.head_dim, self.eps, self.qkv_bits = heads, kv_heads, head_dim, eps, qkv_bits
+        self.norm1, self.norm2 = (weights[n].to(torch.bfloat16) for n in ("norm1", "norm2"))
+        if qkv_bits == 8:
+            codes, scales, _ = api.quantize_rtn_w8(weights["qkv"], weights["qkv"].shape[1], symmetric=True)
+            self.qkv8 = (codes, scales.reshape(-1).contiguous())
+        else:
+            self.qkv = Linear4(weights["qkv"])
+        self.o, self.down = Linear4(weights["o"]), Linear4(weights["down"])
+        self.gate_up = Linear4(api.interleave_rows(weights["gate"], weights["up"]))
+        self.adapters = adapters
+        self.cos_sin = api.rope_table(max_pos, head_dim, theta)
+        self.k_cache, self.v_cache = api.new_kv_cache(num_pages, kv_heads, page_size, head_dim)
+        # one workspace for all linears of the layer (they run one after another), sized for the largest batch
+        size = 256
+        for M in {1, 8, 9, max_tokens}:
+            for lin in (self.o, self.down, self.gate_up) + (() if qkv_bits == 8 else (self.qkv,)):
+                size = max(size, api.linear_w4a16_workspace_size(M, lin.N, lin.K, GROUP))
+            size = max(size, api.linear_w4a16_swiglu_workspace_size(M, self.gate_up.N, self.gate_up.K, GROUP))
+        if qkv_bits == 8:
+            size = max(size, api.linear_w4a4_workspace_size(max_tokens, *weights["qkv"].shape))
+        self.workspace = api.new_workspace(size)
+        self.attn_workspace = None
+
+    def _qkv(self, h, residual, batch):
+        """The norm and the fused projection with the requests' adapters: (qkv, the residual stream)."""
+        if self.qkv_bits == 8:
+            x = torch.empty_like(h) if self.adapters else None   # the adapters read the norm in bf16
+            codes, scales, *rest = api.rmsnorm_a8(h, self.norm1, self.eps, residual=residual, out=x)
+            qkv = api.linear_w8a8(codes, scales, *self.qkv8, workspace=self.workspace)
+            residual = rest[0] if rest else h
+        else:
+            x = api.rmsnorm(h, self.norm1, self.eps, residual=residual)
+            x, residual = x if residual is not None else (x, h)
+            qkv = self.qkv(x, self.workspace)
+        if self.adapters:
+            a, b, scales = self.adapters
+            api.lora_batch_add(x, a, b, qkv, batch.cu_q, batch.adapter, scales)
+        return qkv, residual
+
+    def forward(self, h, residual, batch: Requests):
+        """h [T][hidden]: the layer's input (residual None) or the part of it that is still to be added to residual.
+        Returns the same pair for the next layer."""
+        qkv, residual = self._qkv(h, residual, batch)
+        q = api.rope_append(qkv, self.cos_sin, self.k_cache, self.v_cache, batch.cu_q, batch.kv_len, batch.block_table, self.heads)
+        need = api.attn_paged_workspace_size(q.shape[0], batch.kv_len.shape[0], self.heads, self.kv_heads, self.head_dim, batch.max_q,
+                                             batch.max_kv)
+        if self.attn_workspace is None or self.attn_workspace.numel() < need:
+            self.attn_workspace = api.new_workspace(need)
+        a = api.attn_paged(q, self.k_cache, self.v_cache, batch.cu_q, batch.kv_len, batch.block_table, batch.max_q, batch.max_kv,
+                           workspace=self.attn_workspace)
+        o = self.o(a.view(a.shape[0], -1), self.workspace)
+        x, residual = api.rmsnorm(o, self.norm2, self.eps, residual=residual)
+        g = api.linear_w4a16_swiglu(x, self.gate_up.packed, self.gate_up.scales, self.gate_up.zeros, self.gate_up.N, GROUP,
+                                    workspace=self.workspace)
+        return self.down(g, self.workspace), residual
