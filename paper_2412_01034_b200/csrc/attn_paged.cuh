@@ -58,22 +58,6 @@ inline bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
     return true;
 }
 
-// A launch whose blocks may come up while the kernel before it still runs (see griddepcontrol in the kernels).
-template <class Kernel, class... Args>
-inline cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 qil_status launch_attn_few(const AttnParams& p, cudaStream_t st);
 qil_status launch_attn_many(const AttnParams& p, cudaStream_t st);
 

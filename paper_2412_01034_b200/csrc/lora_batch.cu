@@ -17,7 +17,7 @@ namespace qil {
 
 namespace {
 
-constexpr int kDownWarps = 4, kUpWarps = 4, kUpBlocks = 3, kMaxSlices = 32;   // kUpBlocks: blocks of the second kernel per SM
+constexpr int kDownWarps = 4, kUpWarps = 4, kUpBlocks = 3, kMaxSlices = 32, kFusedWarps = 8, kCluster = 8;   // kUpBlocks: blocks of the second kernel per SM
 
 struct LoraParams {
     const __nv_bfloat16 *x, *a, *b, *y;
@@ -239,10 +239,162 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
     }
 }
 
-// Row tiles of 16 per block.  A tile wastes what its request does not fill, so a batch of single tokens takes tiles of 16;
-// prompts take 64 (32 at rank 64, for the accumulators' registers): the adapter is read once per tile.
+// Both products in one kernel, for tiles of 16 rows: a cluster of kCluster blocks takes a tile.  Each block multiplies by its
+// slice of K, the blocks add their parts through one another's shared memory, and each goes on to its share of the
+// outputs, whose y and B are on their way from the beginning: one launch, and t never goes to memory.
+template <int kNR>
+__global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1, 1) lora_batch_fused_kernel(const LoraParams p) {
+    constexpr int kRank = 8 * kNR, kW = kRank / 4, kSteps = kRank <= 16 ? 1 : kRank / 16, kBQ = kW == 16 ? 2 : 1;
+    __shared__ float part[kFusedWarps][16 * kRank];   // [warp][row][rank]; the block's part ends up in the first
+    __shared__ __align__(16) uint32_t frag[kSteps * 2 * 32 * 4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int tile = blockIdx.x / kCluster, mine = blockIdx.x % kCluster;
+    int seq, row0, row1;
+    if (!find_tile(p.cu, p.num_seqs, p.M, 16, tile, seq, row0, row1)) return;   // (the whole cluster)
+    const int ad = __ldg(p.adapter + seq);
+    const bool none = ad < 0 || ad >= p.num_adapters;
+    if (none && p.out == p.y) return;
+    const int use = none ? 0 : ad;
+    const __nv_bfloat16 *a = p.a + (size_t)use * p.rank * p.K, *b = p.b + (size_t)use * p.N * p.rank;
+    const __nv_bfloat16* xr[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) xr[h] = p.x + min(row0 + 8 * h + g, row1 - 1) * p.ldx;
+    // (rows, columns and rank elements that do not exist repeat others, as in the kernels above)
+    uint4 yv[2], bq[4][kBQ];
+    auto load = [&](int n0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            yv[h] = *reinterpret_cast<const uint4*>(p.y + min(row0 + 8 * h + g, row1 - 1) * p.ldy + min(n0 + 8 * c, p.N - 8));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat16* row = b + (size_t)min(n0 + 8 * (g >> 1) + 2 * i + (g & 1), p.N - 1) * p.rank;
+#pragma unroll
+            for (int h = 0; h < kBQ; ++h) {
+                const __nv_bfloat16* from = row + min(kW * c + 8 * h, p.rank - (kW < 8 ? kW : 8));
+                if (kW == 2) bq[i][h] = make_uint4(__ldg(reinterpret_cast<const uint32_t*>(from)), 0u, 0u, 0u);
+                else if (kW == 4) {
+                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(from));
+                    bq[i][h] = make_uint4(v.x, v.y, 0u, 0u);
+                } else bq[i][h] = __ldg(reinterpret_cast<const uint4*>(from));
+            }
+        }
+    };
+    const int groups = (p.N + 31) / 32, g0 = (int)((long long)groups * mine / kCluster), g1 = (int)((long long)groups * (mine + 1) / kCluster);
+    float acc[kNR][4];
+#pragma unroll
+    for (int n = 0; n < kNR; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
+    if (!none) {
+        const int blocks = (p.K + 31) / 32, last = (int)((long long)blocks * (mine + 1) / kCluster);
+#pragma unroll 2
+        for (int kb = (int)((long long)blocks * mine / kCluster) + warp; kb < last; kb += kFusedWarps) {
+            const int k = kb * 32 + c * 8, at = min(k, p.K - 8);
+            uint4 xv[2], av[kNR];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) xv[h] = __ldg(reinterpret_cast<const uint4*>(xr[h] + at));
+#pragma unroll
+            for (int n = 0; n < kNR; ++n) av[n] = __ldg(reinterpret_cast<const uint4*>(a + (size_t)min(8 * n + g, p.rank - 1) * p.K + at));
+            const uint32_t in = k < p.K ? 0xFFFFFFFFu : 0u;   // (A's repeated columns are finite or their row's result is not: zeros of x do)
+            const uint32_t a0[4] = {xv[0].x & in, xv[1].x & in, xv[0].y & in, xv[1].y & in};
+            const uint32_t a1[4] = {xv[0].z & in, xv[1].z & in, xv[0].w & in, xv[1].w & in};
+#pragma unroll
+            for (int n = 0; n < kNR; ++n) {
+                mma16816(acc[n], a0, av[n].x, av[n].y);
+                mma16816(acc[n], a1, av[n].z, av[n].w);
+            }
+        }
+    }
+    if (g0 + warp < g1) load((g0 + warp) * 32);
+#pragma unroll
+    for (int n = 0; n < kNR; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<float2*>(&part[warp][(g + 8 * h) * kRank + 8 * n + 2 * c]) = make_float2(acc[n][2 * h], acc[n][2 * h + 1]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * kRank; i += blockDim.x) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFusedWarps; ++w) v += part[w][i];
+        part[0][i] = v;
+    }
+    const uint32_t here = (uint32_t)__cvta_generic_to_shared(&part[0][0]);
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const float scale = __ldg(p.scales + use);
+    for (int i = threadIdx.x; i < 16 * (kRank / 2); i += blockDim.x) {
+        const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
+        float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int r = 0; r < kCluster; ++r) {
+            uint32_t there;
+            float2 u;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here + (uint32_t)(m * kRank + j) * 4u), "r"(r));
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(u.x), "=f"(u.y) : "r"(there) : "memory");
+            v.x += u.x;
+            v.y += u.y;
+        }
+        v.x = j < p.rank ? v.x * scale : 0.f;
+        v.y = j < p.rank ? v.y * scale : 0.f;
+        const uint32_t hi = pack2(v.x, v.y);
+        const uint32_t lo = pack2(v.x - __uint_as_float(hi << 16), v.y - __uint_as_float(hi & 0xFFFF0000u));
+        const int at = j % kW, step = at >> 2, reg = (m >> 3) + 2 * ((at & 3) >> 1);
+        uint32_t* f = frag + (step * 2 * 32 + (m & 7) * 4 + j / kW) * 4 + reg;
+        f[0] = hi;
+        f[32 * 4] = lo;
+    }
+    __syncthreads();
+    // (the others may still read this block's part: it stays until all have)
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    for (int n = g0 + warp; n < g1; n += kFusedWarps) {
+        uint4 yn[2] = {yv[0], yv[1]}, bn[4][kBQ];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < kBQ; ++h) bn[i][h] = bq[i][h];
+        if (n + kFusedWarps < g1) load((n + kFusedWarps) * 32);
+        float o4[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o4[i][e] = 0.f;
+        if (!none) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(frag + ((s * 2 + half) * 32 + lane) * 4);
+                    const uint32_t f[4] = {v.x, v.y, kW == 2 ? 0u : v.z, kW == 2 ? 0u : v.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 q = bn[i][kW == 16 ? s >> 1 : 0];
+                        if (s & 1) mma16816(o4[i], f, q.z, q.w);
+                        else mma16816(o4[i], f, q.x, kW == 2 ? 0u : q.y);
+                    }
+                }
+        }
+        const int col = n * 32 + 8 * c;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = row0 + 8 * h + g;
+            if (row < row1 && col < p.N) {
+                float o[8];
+                unpack8(yn[h], o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    o[2 * i] += o4[i][2 * h];
+                    o[2 * i + 1] += o4[i][2 * h + 1];
+                }
+                *reinterpret_cast<uint4*>(p.out + row * p.ldo + col) = pack8(o);
+            }
+        }
+    }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Row tiles of 16 per block.  A tile wastes what its request does not fill, so a batch of single tokens takes tiles of 16
+// (the fused kernel); prompts take 64 rows (32 at rank 64, for the accumulators' registers): the adapter is read once per tile.
 int lora_row_tiles(int M, int num_seqs, int rank) {
-    if (M <= 16 * num_seqs) return 1;
+    if (M <= 16LL * num_seqs) return 1;
     return rank > 32 ? 2 : 4;
 }
 int lora_max_tiles(int M, int num_seqs, int rank) { return M / (16 * lora_row_tiles(M, num_seqs, rank)) + num_seqs; }
@@ -260,6 +412,7 @@ int lora_batch_slices(int M, int num_seqs, int rank, int K) {
 }  // namespace
 
 size_t lora_batch_workspace(int M, int num_seqs, int rank) {
+    if (lora_row_tiles(M, num_seqs, rank) == 1) return 16;   // (t stays on the chip)
     return (size_t)lora_batch_slices(M, num_seqs, rank, 1 << 30) * M * rank * sizeof(float);
 }
 
@@ -276,37 +429,34 @@ qil_status launch_lora_batch_add(const void* x, const void* a, const void* b, co
     p.cu = cu_q; p.adapter = adapter; p.scales = scales;
     p.M = M; p.N = N; p.K = K; p.rank = rank; p.num_seqs = num_seqs; p.num_adapters = num_adapters;
     p.ldx = ldx; p.ldy = ldy; p.ldo = ldo;
+    const unsigned tiles = (unsigned)lora_max_tiles(M, num_seqs, rank);
+    if (lora_row_tiles(M, num_seqs, rank) == 1) {
+        auto go = [&](auto kernel) { kernel<<<tiles * kCluster, 32 * kFusedWarps, 0, st>>>(p); };
+        if (rank <= 8) go(lora_batch_fused_kernel<1>);
+        else if (rank <= 16) go(lora_batch_fused_kernel<2>);
+        else if (rank <= 32) go(lora_batch_fused_kernel<4>);
+        else go(lora_batch_fused_kernel<8>);
+        return launch_status();
+    }
     const int blocks = (K + 31) / 32;
     p.slices = lora_batch_slices(M, num_seqs, rank, K);
     p.slice_blocks = (blocks + p.slices - 1) / p.slices;
     p.slices = (blocks + p.slice_blocks - 1) / p.slice_blocks;
-    const unsigned tiles = (unsigned)lora_max_tiles(M, num_seqs, rank);
-    const int mt = lora_row_tiles(M, num_seqs, rank);
-    // second kernel: one round of blocks, or all the columns there are; with tiles of 16 rows a block's share is too small to
-    // be worth a loop
+    // second kernel: one round of blocks, or all the columns there are
     const unsigned groups = (unsigned)((N + 32 * kUpWarps - 1) / (32 * kUpWarps));
-    unsigned across = mt == 1 ? groups : (unsigned)(kUpBlocks * num_sms()) / tiles;
+    unsigned across = (unsigned)(kUpBlocks * num_sms()) / tiles;
     if (across < 1) across = 1;
     if (across > groups) across = groups;
     const dim3 down(tiles, (unsigned)p.slices), up(tiles, across);
     cudaError_t e = cudaSuccess;
     auto go = [&](auto kd, auto ku) {
         kd<<<down, 32 * kDownWarps, 0, st>>>(p);
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = up;
-        cfg.blockDim = dim3(32 * kUpWarps);
-        cfg.stream = st;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        e = cudaLaunchKernelEx(&cfg, ku, p);
+        e = launch_early(ku, up, 32 * kUpWarps, 0, st, p);
     };
-    if (rank <= 8) mt == 1 ? go(lora_batch_down_kernel<1, 1>, lora_batch_up_kernel<1, 1>) : go(lora_batch_down_kernel<4, 1>, lora_batch_up_kernel<4, 1>);
-    else if (rank <= 16) mt == 1 ? go(lora_batch_down_kernel<1, 2>, lora_batch_up_kernel<1, 2>) : go(lora_batch_down_kernel<4, 2>, lora_batch_up_kernel<4, 2>);
-    else if (rank <= 32) mt == 1 ? go(lora_batch_down_kernel<1, 4>, lora_batch_up_kernel<1, 4>) : go(lora_batch_down_kernel<4, 4>, lora_batch_up_kernel<4, 4>);
-    else mt == 1 ? go(lora_batch_down_kernel<1, 8>, lora_batch_up_kernel<1, 8>) : go(lora_batch_down_kernel<2, 8>, lora_batch_up_kernel<2, 8>);
+    if (rank <= 8) go(lora_batch_down_kernel<4, 1>, lora_batch_up_kernel<4, 1>);
+    else if (rank <= 16) go(lora_batch_down_kernel<4, 2>, lora_batch_up_kernel<4, 2>);
+    else if (rank <= 32) go(lora_batch_down_kernel<4, 4>, lora_batch_up_kernel<4, 4>);
+    else go(lora_batch_down_kernel<2, 8>, lora_batch_up_kernel<2, 8>);
     return e == cudaSuccess ? launch_status() : QIL_ERR_CUDA;
 }
 
