@@ -280,6 +280,8 @@ __global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1
         }
     };
     const int groups = (p.N + 31) / 32, g0 = (int)((long long)groups * mine / kCluster), g1 = (int)((long long)groups * (mine + 1) / kCluster);
+    load(min(g0 + warp, groups - 1) * 32);
+    const float scale = __ldg(p.scales + use);
     float acc[kNR][4];
 #pragma unroll
     for (int n = 0; n < kNR; ++n)
@@ -305,7 +307,6 @@ __global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1
             }
         }
     }
-    if (g0 + warp < g1) load((g0 + warp) * 32);
 #pragma unroll
     for (int n = 0; n < kNR; ++n)
 #pragma unroll
@@ -320,7 +321,6 @@ __global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1
     }
     const uint32_t here = (uint32_t)__cvta_generic_to_shared(&part[0][0]);
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    const float scale = __ldg(p.scales + use);
     for (int i = threadIdx.x; i < 16 * (kRank / 2); i += blockDim.x) {
         const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
         float2 v = make_float2(0.f, 0.f);
