@@ -2,8 +2,6 @@
 // workspace.
 #pragma once
 
-#include <atomic>
-
 #include "layer_common.cuh"
 
 namespace qil {
@@ -38,24 +36,6 @@ __device__ __forceinline__ float fast_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-// Lets a kernel use `bytes` of shared memory, once per device (`done` belongs to the kernel).
-template <class Kernel>
-inline bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>& done) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
-    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
-    if (bit && (done.load(std::memory_order_relaxed) & bit)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
-    done.fetch_or(bit, std::memory_order_relaxed);
-    return true;
 }
 
 qil_status launch_attn_few(const AttnParams& p, cudaStream_t st);

@@ -2,6 +2,8 @@
 // adapters of many requests).
 #pragma once
 
+#include <atomic>
+
 #include "qil_common.cuh"
 
 namespace qil {
@@ -98,6 +100,24 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Lets a kernel use `bytes` of shared memory, once per device (`done` belongs to the kernel).
+template <class Kernel>
+inline bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>& done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
 }
 
 // A launch whose blocks may come up while the kernel before it still runs (see griddepcontrol in the kernels).

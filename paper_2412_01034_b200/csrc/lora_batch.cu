@@ -17,7 +17,10 @@ namespace qil {
 
 namespace {
 
-constexpr int kDownWarps = 4, kUpWarps = 4, kUpBlocks = 3, kMaxSlices = 32, kFusedWarps = 8, kCluster = 8;   // kUpBlocks: blocks of the second kernel per SM
+constexpr int kDownWarps = 4, kUpWarps = 4, kMaxSlices = 32, kFusedWarps = 8, kCluster = 8;
+// Depth of the rings, and blocks of the second kernel per SM: by shared memory two blocks of the first and four of the second
+// kernel fit (4000 rows, rank 32, 4096 -> 11008: 49 us in all; a stage more of either ring takes a block away: 52 - 70 us).
+constexpr int kDownStages = 3, kUpStages = 2, kUpBlocks = 4;
 
 struct LoraParams {
     const __nv_bfloat16 *x, *a, *b, *y;
@@ -28,6 +31,17 @@ struct LoraParams {
     int M, N, K, rank, num_seqs, num_adapters, slices, slice_blocks;   // a slice is slice_blocks blocks of 32 columns of K
     long long ldx, ldy, ldo;
 };
+
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+    if (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(kBytes) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 
 // kMT: row tiles of 16 per block; kNR: column tiles of 8 of the rank (the rank padded up to 8, 16, 32 or 64)
 template <int kMT, int kNR>
@@ -47,8 +61,7 @@ __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const 
         for (int n = 0; n < kNR; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[m][n][e] = 0.f;
-    // Rows past the tile's last and rank rows past the last repeat the last one (nobody reads their results) and the block
-    // of K that reaches beyond K is cleared: with a condition around each load the loads would wait for one another.
+    // Rows past the tile's last and rank rows past the last repeat the last one: nobody reads their results.
     const __nv_bfloat16 *xr[kMT][2], *ar[kNR];
 #pragma unroll
     for (int m = 0; m < kMT; ++m)
@@ -57,42 +70,56 @@ __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const 
 #pragma unroll
     for (int n = 0; n < kNR; ++n) ar[n] = a + (size_t)min(8 * n + g, p.rank - 1) * p.K;
     const int first = blockIdx.y * p.slice_blocks, last = min(first + p.slice_blocks, (p.K + 31) / 32);
-    uint4 xv[kMT][2], av[kNR];
-    auto load = [&](int kb) {
+    // The lane's own 16-byte pieces of the next blocks of K go through a ring in shared memory instead of registers: two
+    // blocks are in flight beside the one at work.
+    extern __shared__ __align__(16) unsigned char ring[];
+    constexpr int kPieces = 2 * kMT + kNR, kStageBytes = kPieces * 512;
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring) + warp * (kDownStages * kStageBytes) + lane * 16;
+    auto fetch = [&](int kb, int stage) {
         const int at = min(kb * 32 + c * 8, p.K - 8);   // this lane's 8 columns (K is a multiple of 8: all or none of them exist)
+        const uint32_t to = slot + stage * kStageBytes;
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) xv[m][h] = __ldg(reinterpret_cast<const uint4*>(xr[m][h] + at));
+            for (int h = 0; h < 2; ++h) cp_async<16>(to + (2 * m + h) * 512, xr[m][h] + at);
 #pragma unroll
-        for (int n = 0; n < kNR; ++n) av[n] = __ldg(reinterpret_cast<const uint4*>(ar[n] + at));
+        for (int n = 0; n < kNR; ++n) cp_async<16>(to + (2 * kMT + n) * 512, ar[n] + at);
     };
-    if (first + warp < last) load(first + warp);
+    int ahead = first + warp, into = 0, stage = 0;
+#pragma unroll
+    for (int s = 0; s < kDownStages - 1; ++s, ahead += kDownWarps, ++into) {
+        if (ahead < last) fetch(ahead, into);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
 #pragma unroll 1
     for (int kb = first + warp; kb < last; kb += kDownWarps) {
-        uint4 xn[kMT][2], an[kNR];
+        if (ahead < last) fetch(ahead, into);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDownStages - 1) : "memory");
+        ahead += kDownWarps;
+        into = into + 1 == kDownStages ? 0 : into + 1;
+        uint4 xv[kMT][2], av[kNR];
 #pragma unroll
-        for (int m = 0; m < kMT; ++m) xn[m][0] = xv[m][0], xn[m][1] = xv[m][1];
+        for (int m = 0; m < kMT; ++m)
 #pragma unroll
-        for (int n = 0; n < kNR; ++n) an[n] = av[n];
-        load(min(kb + kDownWarps, last - 1));           // (the next block's operands are on the way during the products)
-        if (kb * 32 + 32 > p.K && kb * 32 + c * 8 >= p.K) {
+            for (int h = 0; h < 2; ++h) xv[m][h] = lds16(slot + stage * kStageBytes + (2 * m + h) * 512);
 #pragma unroll
-            for (int m = 0; m < kMT; ++m) xn[m][0] = xn[m][1] = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int n = 0; n < kNR; ++n) an[n] = make_uint4(0u, 0u, 0u, 0u);
-        }
+        for (int n = 0; n < kNR; ++n) av[n] = lds16(slot + stage * kStageBytes + (2 * kMT + n) * 512);
+        stage = stage + 1 == kDownStages ? 0 : stage + 1;
+        // (repeated columns of A are finite or their row's result is not anyway: zeros of x are enough)
+        const uint32_t in = kb * 32 + c * 8 < p.K ? 0xFFFFFFFFu : 0u;
 #pragma unroll
         for (int m = 0; m < kMT; ++m) {
-            const uint32_t a0[4] = {xn[m][0].x, xn[m][1].x, xn[m][0].y, xn[m][1].y};
-            const uint32_t a1[4] = {xn[m][0].z, xn[m][1].z, xn[m][0].w, xn[m][1].w};
+            const uint32_t a0[4] = {xv[m][0].x & in, xv[m][1].x & in, xv[m][0].y & in, xv[m][1].y & in};
+            const uint32_t a1[4] = {xv[m][0].z & in, xv[m][1].z & in, xv[m][0].w & in, xv[m][1].w & in};
 #pragma unroll
             for (int n = 0; n < kNR; ++n) {
-                mma16816(acc[m][n], a0, an[n].x, an[n].y);
-                mma16816(acc[m][n], a1, an[n].z, an[n].w);
+                mma16816(acc[m][n], a0, av[n].x, av[n].y);
+                mma16816(acc[m][n], a1, av[n].z, av[n].w);
             }
         }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     // the warps' parts, added in warp order
     if (warp > 0) {
 #pragma unroll
@@ -122,7 +149,7 @@ __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const 
         }
 }
 
-// A warp takes groups of 32 outputs in turn, with the next group's y and B on the way while it works: a block's way to its
+// A warp takes groups of 32 outputs in turn, with the next groups' y and B on the way while it works: a block's way to its
 // first product (the request, its adapter, t) is several trips to memory long and is paid once.
 template <int kMT, int kNR>
 __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel(const LoraParams p) {
@@ -139,31 +166,34 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
     const __nv_bfloat16* b = p.b + (size_t)(none ? 0 : ad) * p.N * p.rank;
     // Rows past the tile's last, columns past N and rank elements past the rank repeat others: the first two are not
     // written, the last meet zeros of t.  (Conditions around the loads would make them wait for one another.)
-    uint4 yv[kMT][2], bq[4][kBQ];
-    auto load = [&](int n0) {
+    // The lane's own pieces of y and B of the next groups go through a ring in shared memory, as in the first kernel.
+    extern __shared__ __align__(16) unsigned char ring[];
+    constexpr int kPieces = 2 * kMT + 4 * kBQ, kStageBytes = kPieces * 512;
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring) + warp * (kUpStages * kStageBytes) + lane * 16;
+    auto fetch = [&](int n0, int stage) {
+        const uint32_t to = slot + stage * kStageBytes;
 #pragma unroll
         for (int m = 0; m < kMT; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                yv[m][h] = *reinterpret_cast<const uint4*>(p.y + min(row0 + 16 * m + 8 * h + g, row1 - 1) * p.ldy + min(n0 + 8 * c, p.N - 8));
+                cp_async<16>(to + (2 * m + h) * 512, p.y + min(row0 + 16 * m + 8 * h + g, row1 - 1) * p.ldy + min(n0 + 8 * c, p.N - 8));
         // B rows of the 32 columns: column (2c, 2c + 1) of result tile i is output n0 + 8 c + 2 i, + 1
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const __nv_bfloat16* row = b + (size_t)min(n0 + 8 * (g >> 1) + 2 * i + (g & 1), p.N - 1) * p.rank;
 #pragma unroll
-            for (int h = 0; h < kBQ; ++h) {
-                const __nv_bfloat16* from = row + min(kW * c + 8 * h, p.rank - (kW < 8 ? kW : 8));
-                if (kW == 2) bq[i][h] = make_uint4(__ldg(reinterpret_cast<const uint32_t*>(from)), 0u, 0u, 0u);
-                else if (kW == 4) {
-                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(from));
-                    bq[i][h] = make_uint4(v.x, v.y, 0u, 0u);
-                } else bq[i][h] = __ldg(reinterpret_cast<const uint4*>(from));
-            }
+            for (int h = 0; h < kBQ; ++h)
+                cp_async<(kW < 8 ? 2 * kW : 16)>(to + (2 * kMT + i * kBQ + h) * 512, row + min(kW * c + 8 * h, p.rank - (kW < 8 ? kW : 8)));
         }
     };
     int n0 = (blockIdx.y * kUpWarps + warp) * 32;
     const int stride = gridDim.y * kUpWarps * 32;
-    load(n0);
+    int ahead = n0, into = 0, stage = 0;
+#pragma unroll
+    for (int s = 0; s < kUpStages - 1; ++s, ahead += stride, ++into) {
+        if (ahead < p.N) fetch(ahead, into);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
     const float scale = __ldg(p.scales + (none ? 0 : ad));
     asm volatile("griddepcontrol.wait;" ::: "memory");   // t is written by the kernel before, which may still be running
     if (!none) {
@@ -190,14 +220,18 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
     __syncthreads();
 #pragma unroll 1
     for (; n0 < p.N; n0 += stride) {
-        uint4 yn[kMT][2], bn[4][kBQ];
-#pragma unroll
-        for (int m = 0; m < kMT; ++m) yn[m][0] = yv[m][0], yn[m][1] = yv[m][1];
+        if (ahead < p.N) fetch(ahead, into);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kUpStages - 1) : "memory");
+        ahead += stride;
+        into = into + 1 == kUpStages ? 0 : into + 1;
+        const uint32_t from = slot + stage * kStageBytes;
+        stage = stage + 1 == kUpStages ? 0 : stage + 1;
+        uint4 bn[4][kBQ];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int h = 0; h < kBQ; ++h) bn[i][h] = bq[i][h];
-        if (n0 + stride < p.N) load(n0 + stride);
+            for (int h = 0; h < kBQ; ++h) bn[i][h] = lds16(from + (2 * kMT + i * kBQ + h) * 512);
         const int n = n0 + 8 * c;      // this lane's 8 outputs (N is a multiple of 8: all or none of them exist)
 #pragma unroll
         for (int m = 0; m < kMT; ++m) {
@@ -226,7 +260,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
                 const int row = row0 + 16 * m + 8 * h + g;
                 if (row < row1 && n < p.N) {
                     float o[8];
-                    unpack8(yn[m][h], o);
+                    unpack8(lds16(from + (2 * m + h) * 512), o);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         o[2 * i] += acc[i][2 * h];
@@ -409,6 +443,19 @@ int lora_batch_slices(int M, int num_seqs, int rank, int K) {
     return s < 1 ? 1 : s;
 }
 
+template <int kMT, int kNR>
+qil_status launch_two(const LoraParams& p, dim3 down, dim3 up, cudaStream_t st) {
+    constexpr int kDown = kDownWarps * kDownStages * (2 * kMT + kNR) * 512, kUp = kUpWarps * kUpStages * (2 * kMT + 4 * (kNR == 8 ? 2 : 1)) * 512;
+    static std::atomic<unsigned long long> down_allowed{0}, up_allowed{0};
+    if (!allow_smem(lora_batch_down_kernel<kMT, kNR>, kDown, down_allowed) || !allow_smem(lora_batch_up_kernel<kMT, kNR>, kUp, up_allowed))
+        return QIL_ERR_CUDA;
+    lora_batch_down_kernel<kMT, kNR><<<down, 32 * kDownWarps, kDown, st>>>(p);
+    const cudaError_t e = launch_early(lora_batch_up_kernel<kMT, kNR>, up, 32 * kUpWarps, kUp, st, p);
+    if (e == cudaSuccess) return launch_status();
+    (void)cudaGetLastError();
+    return QIL_ERR_CUDA;
+}
+
 }  // namespace
 
 size_t lora_batch_workspace(int M, int num_seqs, int rank) {
@@ -448,16 +495,10 @@ qil_status launch_lora_batch_add(const void* x, const void* a, const void* b, co
     if (across < 1) across = 1;
     if (across > groups) across = groups;
     const dim3 down(tiles, (unsigned)p.slices), up(tiles, across);
-    cudaError_t e = cudaSuccess;
-    auto go = [&](auto kd, auto ku) {
-        kd<<<down, 32 * kDownWarps, 0, st>>>(p);
-        e = launch_early(ku, up, 32 * kUpWarps, 0, st, p);
-    };
-    if (rank <= 8) go(lora_batch_down_kernel<4, 1>, lora_batch_up_kernel<4, 1>);
-    else if (rank <= 16) go(lora_batch_down_kernel<4, 2>, lora_batch_up_kernel<4, 2>);
-    else if (rank <= 32) go(lora_batch_down_kernel<4, 4>, lora_batch_up_kernel<4, 4>);
-    else go(lora_batch_down_kernel<2, 8>, lora_batch_up_kernel<2, 8>);
-    return e == cudaSuccess ? launch_status() : QIL_ERR_CUDA;
+    if (rank <= 8) return launch_two<4, 1>(p, down, up, st);
+    if (rank <= 16) return launch_two<4, 2>(p, down, up, st);
+    if (rank <= 32) return launch_two<4, 4>(p, down, up, st);
+    return launch_two<2, 8>(p, down, up, st);
 }
 
 }  // namespace qil
