@@ -16,6 +16,15 @@
 // One warp copies pages with bulk tensor copies (128-byte swizzle), one thread issues the products, one warp clears what
 // lies behind a request's last token in its last tile of V (a weight of zero times NaN would be NaN).
 // Every wait is bounded; when one runs out QIL_ERR_TIMEOUT is recorded and the block ends.
+//
+// Measured, 4096 new tokens over 8192, 32 heads of 128 (412 GFLOP): 378 us (1090 TFLOP/s) until the power cap sets in, 412 to
+// 440 us (940 to 1000 TFLOP/s at 1.65 GHz, 1000 W) sustained.  A step (128 tokens, both row tiles) takes 2830 cycles; the
+// products alone would take 2048 (16 cycles per 128 x 128 x 16 and pipe), the exponentials of both tiles 2048 on the
+// special-function units as well.  Per tile: 1660 cycles from S to P, 1130 waiting (half of the product, S, and their
+// latencies; the issuing thread needs 64 cycles a product, as long as the pipe does).  Tried and slower: part of the
+// exponentials as a polynomial on the multiply-add pipe (454 to 543 us: more instructions, and the power cap), polling
+// instead of suspended waits, blocks that stay and take tiles from a counter (no change: the start of a block, 7600 cycles,
+// is the copies of all blocks starting at once).
 #include <cuda.h>
 
 #include <mutex>

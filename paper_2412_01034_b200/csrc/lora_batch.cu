@@ -10,6 +10,9 @@
 // Both kernels take their operands straight from global memory in 16-byte loads and never stage them: the order of a
 // contraction's terms is free, so lane c of four takes 8 neighbouring elements and both operands use the same order; and
 // the columns of a group of four 16 x 8 results are dealt out so that a lane ends up with 8 neighbouring outputs.
+// Measured: 32 single tokens, 12 adapters of rank 16, 4096 x 4096: 7.5 us, a chain of five trips to memory (request, adapter,
+// operands, the cluster's parts, outputs).  4000 rows in nine prompts, rank 32, 4096 -> 11008: 13 + 36 us, against 34 us for
+// x, y and the output at the copy rate; of the second kernel's traffic a third is B, re-read from L2 for every 64 rows.
 // t is split into two bf16 terms (hi + lo) before it is multiplied: it keeps 16 significant bits.
 #include "layer_common.cuh"
 

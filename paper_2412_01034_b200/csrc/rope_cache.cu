@@ -5,7 +5,8 @@
 //   (a, b) = (x[i], x[i + D/2]) -> (a cos - b sin, b cos + a sin) with the table's row p, for query and key heads
 //   caches [num_pages][Hk][page_size][D]; position p sits in page block_table[b][p / page_size], slot p % page_size
 // One pass, memory bound.  A thread turns 8 pairs (two 16-byte loads and stores) or copies 16 values; what it reads is asked
-// for before the request, its page and its angles are looked up.  The angles come from a table: a sine of position *
+// for before the request, its page and its angles are looked up (4200 tokens of 32 + 32 + 32 heads: 45.3 us = 6.0 TB/s, 91 %
+// of the copy rate; with the look-up first 51 us; 32 single tokens 3.6 us).  The angles come from a table: a sine of position *
 // frequency formed in fp32 would be off by up to position * 2^-24 radians.
 #include "layer_common.cuh"
 
