@@ -43,7 +43,7 @@ def build_binding(force: bool = False) -> str:
                 os.path.join(base, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     cmd += [f"-isystem{i}" for i in includes] + [source, "-o", BINDING, "-L", os.path.join(base, "lib"), "-L", HERE, "-l:libqil.so",
-                                                 "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
+                                                 "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ltorch_cuda", "-Wl,-rpath,$ORIGIN"]
     subprocess.run(cmd, check=True)
     return BINDING
 
