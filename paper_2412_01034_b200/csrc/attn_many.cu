@@ -472,10 +472,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                     for (int c = 0; c < kTok; ++c)
                         if (c >= left) s[c] = 0xFF800000u;   // -inf
                 }
-                float top[2] = {-INFINITY, -INFINITY};
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < kTok; c += 2) top[(c >> 1) & 1] = max3(top[(c >> 1) & 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-                const float most = fmaxf(top[0], top[1]) * scale;
+                for (int c = 0; c < kTok; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
                 const bool raise = live && most > ref + kRaise;   // (also the first visible score: ref is -inf before it)
                 if (__any_sync(0xffffffffu, raise)) {
                     const float to = raise ? most : ref;
@@ -496,22 +496,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                     }
                 }
                 const float base = ref == -INFINITY ? 0.f : -ref;
-                float part[2] = {0.f, 0.f};
+                const unsigned long long scale2 = f2(scale, scale), base2 = f2(base, base);
+                unsigned long long acc[2] = {0ull, 0ull};
 #pragma unroll
                 for (int c = 0; c < kTok; c += 64) {
                     uint32_t w[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const float a = fast_exp2(fmaf(__uint_as_float(s[c + 2 * e]), scale, base));
-                        const float b = fast_exp2(fmaf(__uint_as_float(s[c + 2 * e + 1]), scale, base));
-                        part[0] += a;
-                        part[1] += b;
+                        float a, b;
+                        f2_split(f2_fma(f2(__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])), scale2, base2), a, b);
+                        a = fast_exp2(a);
+                        b = fast_exp2(b);
+                        acc[e & 1] = f2_add(acc[e & 1], f2(a, b));
                         w[e] = pack2(a, b);
                     }
                     tmem_st32(s_at + c / 2, w);
                     publish(c / 64);
                 }
-                sum += part[0] + part[1];
+                float a, b;
+                f2_split(f2_add(acc[0], acc[1]), a, b);
+                sum += a + b;
             }
         }
         // the rows' results

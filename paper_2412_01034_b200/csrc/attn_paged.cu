@@ -39,9 +39,12 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
         if (pl.slots > 1) pl.few_floats = ((size_t)items * pl.slots * pl.few_rows * (D + 2) + 3) & ~(size_t)3;   // (16-byte stores behind them)
     }
     if (pl.many) {
-        // The cache is split where the row tiles alone leave SMs idle, into parts of at least four tiles of 128 tokens.
-        const long long tiles = ((long long)total_q * G + 255) / 256 * Hk;
-        long long s = sms / tiles;
+        // The cache is split where the row tiles alone leave SMs idle, into parts of at least four tiles of 128 tokens.  The
+        // bounds give the least number of row tiles: all rows packed, or one tile for every request that has to be here.
+        const long long few = kFewRows / G, here = max_q > few ? (total_q - num_seqs * few + max_q - few - 1) / (max_q - few) : 0;
+        long long tiles = ((long long)total_q * G + 255) / 256;
+        if (tiles < here) tiles = here;
+        long long s = sms / (tiles * Hk);
         if (s > (max_kv + 511) / 512) s = (max_kv + 511) / 512;
         pl.splits = s < 1 ? 1 : (int)s;
         if (pl.splits > 1) pl.many_floats = (size_t)pl.splits * total_q * H * (D + 2);
