@@ -59,8 +59,8 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
-    // (the kernel for many rows reads nothing of this one's results: its blocks may come up as these leave)
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    wait_for_earlier_kernels();
+    let_next_kernel_start();   // (the kernel for many rows reads nothing of this one's results and runs beside it)
     const int begin = split * p.chunk;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
     // (the first tile's page and the length are on the way with the starts, not after them)
@@ -301,8 +301,7 @@ qil_status go(const AttnParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(attn_few_kernel<kDim>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
     const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)p.c.num_seqs);
-    attn_few_kernel<kDim><<<grid, 32 * kWarps, FewShape<kDim>::kSmem, st>>>(p);
-    return launch_status();
+    return launch_early(attn_few_kernel<kDim>, grid, 32 * kWarps, FewShape<kDim>::kSmem, st, p);
 }
 
 }  // namespace

@@ -200,6 +200,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     using Shape = ManyShape<kDim>;
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
+    // (behind the kernel for few rows: all of its blocks have seen the end of what came before)
+    if (!p.after_few) wait_for_earlier_kernels();
+    let_next_kernel_start();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.G, H = p.c.num_heads, kvh = blockIdx.x % p.c.num_kv_heads;
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -252,10 +255,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // Nothing here depends on the kernel before, but what comes after this launch may: its first block lasts until that
+    // Nothing here depends on the kernel for few rows, but what comes after this launch may: the first block lasts until that
     // kernel is complete.
-    if (p.after_few && blockIdx.x == 0 && blockIdx.z == 0 && warp == 3) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (p.after_few && blockIdx.x == 0 && blockIdx.z == 0 && warp == 3) wait_for_earlier_kernels();
     if (!found) {   // (the grid is sized for the most tiles that the requests could have)
         if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
         return;
@@ -594,7 +596,8 @@ template <int kDim>
 __global__ void __launch_bounds__(128) attn_many_join_kernel(const AttnParams p) {
     constexpr int kPer = kDim / 32;
     const size_t items = (size_t)p.c.total_q * p.c.num_heads, at = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts
+    wait_for_earlier_kernels();   // the parts
+    let_next_kernel_start();
     if (at >= items) return;
     const int lane = threadIdx.x & 31, t = (int)(at / p.c.num_heads);
     const int seq = request_of_row(p.c.cu_q, p.c.num_seqs, t);
@@ -679,20 +682,10 @@ qil_status go(const AttnParams& p, cudaStream_t st) {
     if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
     // (heads first, so that the long tiles of all heads start before the short ones of any)
     const dim3 grid((unsigned)((long long)p.c.num_kv_heads * (p.c.total_q / (2 * p.tile_tokens) + p.c.num_seqs)), 1u, (unsigned)p.splits);
-    cudaError_t e;
-    if (p.after_few) {
-        e = launch_early(attn_many_kernel<kDim>, grid, kThreads, kSmem, st, mq, mk, mv, p);
-    } else {
-        attn_many_kernel<kDim><<<grid, kThreads, kSmem, st>>>(mq, mk, mv, p);
-        e = cudaGetLastError();
-    }
-    if (e == cudaSuccess && p.splits > 1) {
-        const long long items = (long long)p.c.total_q * p.c.num_heads;
-        e = launch_early(attn_many_join_kernel<kDim>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
-    }
-    if (e == cudaSuccess) return QIL_OK;
-    (void)cudaGetLastError();
-    return QIL_ERR_CUDA;
+    const qil_status s = launch_early(attn_many_kernel<kDim>, grid, kThreads, kSmem, st, mq, mk, mv, p);
+    if (s != QIL_OK || p.splits == 1) return s;
+    const long long items = (long long)p.c.total_q * p.c.num_heads;
+    return launch_early(attn_many_join_kernel<kDim>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
 }
 
 }  // namespace

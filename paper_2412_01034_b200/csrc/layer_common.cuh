@@ -120,9 +120,16 @@ inline bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
     return true;
 }
 
-// A launch whose blocks may come up while the kernel before it still runs (see griddepcontrol in the kernels).
+// Every kernel of the layer operators is launched early: its blocks may come up while the kernel before it in the stream
+// finishes, which takes the gap between two short kernels (2.5 us) out of a chain of them.  A block's first act is to wait
+// until everything before is complete and visible; only then may the next kernel's blocks come up in turn, so that
+// nothing ever runs beside a kernel two places before it.  (No effect where the launch was an ordinary one.)
+__device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// An early launch, as described above.
 template <class Kernel, class... Args>
-inline cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+inline qil_status launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
@@ -133,7 +140,9 @@ inline cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t sm
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess) return QIL_OK;
+    (void)cudaGetLastError();
+    return QIL_ERR_CUDA;
 }
 
 // Internal launchers.

@@ -51,7 +51,8 @@ template <int kMT, int kNR>
 __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const LoraParams p) {
     __shared__ float part[kDownWarps - 1][kMT * kNR * 4 * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the second kernel's blocks may come up as these leave
+    wait_for_earlier_kernels();
+    let_next_kernel_start();   // (the second kernel reads what came before this one ahead of its own wait)
     int seq, row0, row1;
     if (!find_tile(p.cu, p.num_seqs, p.M, 16 * kMT, blockIdx.x, seq, row0, row1)) return;
     const int ad = __ldg(p.adapter + seq);
@@ -198,7 +199,8 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
     const float scale = __ldg(p.scales + (none ? 0 : ad));
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // t is written by the kernel before, which may still be running
+    wait_for_earlier_kernels();   // t is written by the first kernel, which may still be running
+    let_next_kernel_start();
     if (!none) {
         for (int i = threadIdx.x; i < kMT * 16 * (kRank / 2); i += blockDim.x) {
             const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
@@ -286,6 +288,8 @@ __global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1
     __shared__ __align__(16) uint32_t frag[kSteps * 2 * 32 * 4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int tile = blockIdx.x / kCluster, mine = blockIdx.x % kCluster;
+    wait_for_earlier_kernels();
+    let_next_kernel_start();
     int seq, row0, row1;
     if (!find_tile(p.cu, p.num_seqs, p.M, 16, tile, seq, row0, row1)) return;   // (the whole cluster)
     const int ad = __ldg(p.adapter + seq);
@@ -452,11 +456,8 @@ qil_status launch_two(const LoraParams& p, dim3 down, dim3 up, cudaStream_t st) 
     static std::atomic<unsigned long long> down_allowed{0}, up_allowed{0};
     if (!allow_smem(lora_batch_down_kernel<kMT, kNR>, kDown, down_allowed) || !allow_smem(lora_batch_up_kernel<kMT, kNR>, kUp, up_allowed))
         return QIL_ERR_CUDA;
-    lora_batch_down_kernel<kMT, kNR><<<down, 32 * kDownWarps, kDown, st>>>(p);
-    const cudaError_t e = launch_early(lora_batch_up_kernel<kMT, kNR>, up, 32 * kUpWarps, kUp, st, p);
-    if (e == cudaSuccess) return launch_status();
-    (void)cudaGetLastError();
-    return QIL_ERR_CUDA;
+    const qil_status s = launch_early(lora_batch_down_kernel<kMT, kNR>, down, 32 * kDownWarps, kDown, st, p);
+    return s != QIL_OK ? s : launch_early(lora_batch_up_kernel<kMT, kNR>, up, 32 * kUpWarps, kUp, st, p);
 }
 
 }  // namespace
@@ -481,12 +482,10 @@ qil_status launch_lora_batch_add(const void* x, const void* a, const void* b, co
     p.ldx = ldx; p.ldy = ldy; p.ldo = ldo;
     const unsigned tiles = (unsigned)lora_max_tiles(M, num_seqs, rank);
     if (lora_row_tiles(M, num_seqs, rank) == 1) {
-        auto go = [&](auto kernel) { kernel<<<tiles * kCluster, 32 * kFusedWarps, 0, st>>>(p); };
-        if (rank <= 8) go(lora_batch_fused_kernel<1>);
-        else if (rank <= 16) go(lora_batch_fused_kernel<2>);
-        else if (rank <= 32) go(lora_batch_fused_kernel<4>);
-        else go(lora_batch_fused_kernel<8>);
-        return launch_status();
+        auto go = [&](auto kernel) { return launch_early(kernel, dim3(tiles * kCluster), 32 * kFusedWarps, 0, st, p); };
+        if (rank <= 8) return go(lora_batch_fused_kernel<1>);
+        if (rank <= 16) return go(lora_batch_fused_kernel<2>);
+        return rank <= 32 ? go(lora_batch_fused_kernel<4>) : go(lora_batch_fused_kernel<8>);
     }
     const int blocks = (K + 31) / 32;
     p.slices = lora_batch_slices(M, num_seqs, rank, K);

@@ -22,6 +22,8 @@ __global__ void __launch_bounds__(kVec == 1 ? 256 : 1024) rmsnorm_kernel(const _
     __shared__ float s_sum[2][32], s_max[2][32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int nvec = K >> 3;
+    wait_for_earlier_kernels();
+    let_next_kernel_start();
     uint4 xv[kVec], rv[kVec], wv[kVec];
     // (threads past the row's end repeat its last vector and count for nothing: no condition around a load)
     auto load = [&](int row) {
@@ -122,15 +124,13 @@ qil_status launch_rmsnorm(const void* x, const void* residual, const void* weigh
     const long long room = (long long)num_sms() * (threads < 1024 ? 1024 / threads : 1);
     const unsigned grid = (unsigned)(M < room ? M : room);
     auto go = [&](auto kernel) {
-        kernel<<<grid, threads, 0, st>>>(
-            reinterpret_cast<const __nv_bfloat16*>(x), reinterpret_cast<const __nv_bfloat16*>(residual),
-            reinterpret_cast<const __nv_bfloat16*>(weight), reinterpret_cast<__nv_bfloat16*>(residual_out),
-            reinterpret_cast<__nv_bfloat16*>(y), qy, scales, M, K, eps);
+        return launch_early(kernel, dim3(grid), threads, 0, st, reinterpret_cast<const __nv_bfloat16*>(x),
+                            reinterpret_cast<const __nv_bfloat16*>(residual), reinterpret_cast<const __nv_bfloat16*>(weight),
+                            reinterpret_cast<__nv_bfloat16*>(residual_out), reinterpret_cast<__nv_bfloat16*>(y), qy, scales, M, K, eps);
     };
-    if (vec == 1) residual ? go(rmsnorm_kernel<1, true>) : go(rmsnorm_kernel<1, false>);
-    else if (vec == 2) residual ? go(rmsnorm_kernel<2, true>) : go(rmsnorm_kernel<2, false>);
-    else residual ? go(rmsnorm_kernel<4, true>) : go(rmsnorm_kernel<4, false>);
-    return launch_status();
+    if (vec == 1) return residual ? go(rmsnorm_kernel<1, true>) : go(rmsnorm_kernel<1, false>);
+    if (vec == 2) return residual ? go(rmsnorm_kernel<2, true>) : go(rmsnorm_kernel<2, false>);
+    return residual ? go(rmsnorm_kernel<4, true>) : go(rmsnorm_kernel<4, false>);
 }
 
 }  // namespace qil

@@ -22,6 +22,8 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __nv_bfloat
                                                                __nv_bfloat16* __restrict__ v_cache, PagedCache c, int max_pos, int pieces) {
     constexpr int kHalf = kDim / 2, kPer = kHalf / 8;   // pieces of 8 pairs per head, and as many of 16 values
     const int t = blockIdx.x, H = c.num_heads, Hk = c.num_kv_heads;
+    wait_for_earlier_kernels();
+    let_next_kernel_start();
     const int i = blockIdx.y * kThreads + threadIdx.x, piece = min(i, pieces - 1), head = piece / kPer, o = (piece % kPer) * 8;
     const bool turn = head < H + Hk;
     const __nv_bfloat16* src = qkv + ((size_t)t * (H + 2 * Hk) + head) * kDim + (turn ? o : 2 * o);
@@ -69,11 +71,11 @@ qil_status launch_rope_append(const void* qkv, const float* cos_sin, void* q_out
     const int pieces = (c.num_heads + 2 * c.num_kv_heads) * (c.head_dim / 16);
     const dim3 grid((unsigned)c.total_q, (unsigned)((pieces + kThreads - 1) / kThreads));
     auto go = [&](auto kernel) {
-        kernel<<<grid, kThreads, 0, st>>>(reinterpret_cast<const __nv_bfloat16*>(qkv), cos_sin, reinterpret_cast<__nv_bfloat16*>(q_out),
-                                          reinterpret_cast<__nv_bfloat16*>(k_cache), reinterpret_cast<__nv_bfloat16*>(v_cache), c, max_pos, pieces);
+        return launch_early(kernel, grid, kThreads, 0, st, reinterpret_cast<const __nv_bfloat16*>(qkv), cos_sin,
+                            reinterpret_cast<__nv_bfloat16*>(q_out), reinterpret_cast<__nv_bfloat16*>(k_cache),
+                            reinterpret_cast<__nv_bfloat16*>(v_cache), c, max_pos, pieces);
     };
-    c.head_dim == 128 ? go(rope_append_kernel<128>) : go(rope_append_kernel<64>);
-    return launch_status();
+    return c.head_dim == 128 ? go(rope_append_kernel<128>) : go(rope_append_kernel<64>);
 }
 
 }  // namespace qil

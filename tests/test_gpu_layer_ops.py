@@ -407,3 +407,95 @@ def test_every_operator_runs_on_the_stream_it_is_given(api):
         got_l = api.lora_batch_add(x, a, b, y, cu64, zero, scales, stream=s)
         s.synchronize()
         assert torch.equal(got, want) and torch.equal(got_o, want_o) and torch.equal(got_l, want_l)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# chains: the kernels come up early and wait for what is before them
+# ------------------------------------------------------------------------------------------------------------------
+class Chain:
+    """Each call reads what the call before it wrote, in place where that is possible; shapes short enough that launches, not
+    work, fill the time."""
+
+    def __init__(self, api, q_lens, kv_lens, seed):
+        g = gen(seed)
+        self.api, self.H, self.Hk, self.D, hidden = api, 8, 4, 64, 512
+        self.q_lens, self.T = q_lens, sum(q_lens)
+        self.table, _, pages = paged(g, kv_lens, 16)
+        self.kc, self.vc = draw(g, pages, self.Hk, 16, self.D), draw(g, pages, self.Hk, 16, self.D)
+        self.cu, self.kv, self.kv_lens = ints(starts(q_lens)), ints(kv_lens), kv_lens
+        self.h, self.residual, self.w = draw(g, self.T, hidden), draw(g, self.T, hidden), draw(g, hidden)
+        wide = (self.H + 2 * self.Hk) * self.D
+        self.a, self.b = draw(g, 2, 16, hidden, std=0.05), draw(g, 2, wide, 16, std=0.3)
+        self.scales, self.adapter = torch.tensor([0.5, -1.0], device="cuda"), ints([i % 3 - 1 for i in range(len(q_lens))])
+        self.cs = api.rope_table(max(kv_lens), self.D)
+        self.ws = api.new_workspace(api.attn_paged_workspace_size(self.T, len(q_lens), self.H, self.Hk, self.D, max(q_lens), max(kv_lens)))
+        self.lora_ws = api.new_workspace(api.lora_batch_workspace_size(self.T, len(q_lens), 16))
+        self.qkv, self.x = torch.empty(self.T, wide, dtype=torch.bfloat16, device="cuda"), torch.empty_like(self.h)
+        self.q, self.o = (torch.empty(self.T, self.H, self.D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.state = [self.h, self.residual, self.kc, self.vc]
+
+    def step(self, after=lambda: None):
+        api = self.api
+        api.rmsnorm(self.h, self.w, residual=self.residual, out=self.x, residual_out=self.residual)
+        after()
+        self.qkv.zero_()
+        after()
+        api.lora_batch_add(self.x, self.a, self.b, self.qkv, self.cu, self.adapter, self.scales, workspace=self.lora_ws)
+        after()
+        api.rope_append(self.qkv, self.cs, self.kc, self.vc, self.cu, self.kv, self.table, self.H, out=self.q)
+        after()
+        api.attn_paged(self.q, self.kc, self.vc, self.cu, self.kv, self.table, max(self.q_lens), max(self.kv_lens), out=self.o, workspace=self.ws)
+        after()
+        api.rmsnorm(self.o.view(self.T, -1), self.w, residual=self.residual, out=self.h, residual_out=self.residual)
+        after()
+
+
+CHAINS = [([1] * 5, [30, 1, 200, 77, 650]), ([70, 1, 1, 130], [700, 33, 500, 130]), ([200], [2000])]
+
+
+@pytest.mark.parametrize("case", range(len(CHAINS)))
+def test_chains_of_calls_equal_calls_one_by_one(api, case):
+    q_lens, kv_lens = CHAINS[case]
+    one, many = Chain(api, q_lens, kv_lens, 500 + case), Chain(api, q_lens, kv_lens, 500 + case)
+    for _ in range(20):
+        one.step(after=torch.cuda.synchronize)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        many.step()
+    torch.cuda.synchronize()
+    for a, b in zip(one.state, many.state):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    assert torch.isfinite(many.h).all()
+
+
+@pytest.mark.parametrize("case", range(len(CHAINS)))
+def test_a_captured_chain_replays(api, case):
+    q_lens, kv_lens = CHAINS[case]
+    one, many = Chain(api, q_lens, kv_lens, 600 + case), Chain(api, q_lens, kv_lens, 600 + case)
+    start = [t.clone() for t in many.state]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        many.step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        many.step()
+        many.step()
+    for t, v in zip(many.state, start):
+        t.copy_(v)
+    for _ in range(5):
+        graph.replay()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        one.step()
+    for a, b in zip(one.state, many.state):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_attn_paged_many_requests_of_every_kind(api):
+    """More requests than a warp looks at in one go, those with many rows and those with none anywhere among them."""
+    q_lens = [1] * 40 + [0] * 3 + [33, 1, 0, 5] + [1] * 30 + [130] + [2] * 5
+    kv_lens = [1 + (37 * i) % 150 for i in range(len(q_lens))]
+    kv_lens = [max(kv, q) for kv, q in zip(kv_lens, q_lens)]
+    args = attention_inputs(gen(90), q_lens, kv_lens, 4, 2, 64, 16)
+    check_attention(api, *args, q_lens, kv_lens)
