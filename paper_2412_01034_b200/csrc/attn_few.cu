@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
     wait_for_earlier_kernels();
-    let_next_kernel_start();   // (the kernel for many rows reads nothing of this one's results and runs beside it)
+    if (p.before_many) let_next_kernel_start();   // (the kernel for many rows reads nothing of this one's results and runs beside it)
     const int begin = split * p.chunk;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
     // (the first tile's page and the length are on the way with the starts, not after them)

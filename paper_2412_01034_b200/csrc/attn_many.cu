@@ -202,7 +202,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     extern __shared__ unsigned char smem_raw[];
     // (behind the kernel for few rows: all of its blocks have seen the end of what came before)
     if (!p.after_few) wait_for_earlier_kernels();
-    let_next_kernel_start();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.G, H = p.c.num_heads, kvh = blockIdx.x % p.c.num_kv_heads;
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -597,7 +596,6 @@ __global__ void __launch_bounds__(128) attn_many_join_kernel(const AttnParams p)
     constexpr int kPer = kDim / 32;
     const size_t items = (size_t)p.c.total_q * p.c.num_heads, at = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     wait_for_earlier_kernels();   // the parts
-    let_next_kernel_start();
     if (at >= items) return;
     const int lane = threadIdx.x & 31, t = (int)(at / p.c.num_heads);
     const int seq = request_of_row(p.c.cu_q, p.c.num_seqs, t);

@@ -83,6 +83,7 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     p.counters = reinterpret_cast<int*>(base + kHeader);
     p.few_parts = reinterpret_cast<float*>(base + kHeader + pl.counter_bytes);
     p.many_parts = p.few_parts + pl.few_floats;   // (the two kernels may run at the same time)
+    p.before_many = pl.many;
     p.after_few = pl.few;
     if (pl.few) {
         const qil_status s = launch_attn_few(p, st);

@@ -26,7 +26,7 @@ struct AttnParams {
     int* status;
     int* counters;       // [num_seqs][num_kv_heads] parts written so far, zero between launches
     float *few_parts, *many_parts;
-    bool after_few;      // many rows: the launch follows one of the other kernel
+    bool before_many, after_few;   // few rows: a launch of the other kernel follows; many rows: one came before
 };
 
 // cached tokens that the table can name

@@ -200,7 +200,6 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
     }
     const float scale = __ldg(p.scales + (none ? 0 : ad));
     wait_for_earlier_kernels();   // t is written by the first kernel, which may still be running
-    let_next_kernel_start();
     if (!none) {
         for (int i = threadIdx.x; i < kMT * 16 * (kRank / 2); i += blockDim.x) {
             const int m = i / (kRank / 2), j = 2 * (i % (kRank / 2));
@@ -289,7 +288,6 @@ __global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int tile = blockIdx.x / kCluster, mine = blockIdx.x % kCluster;
     wait_for_earlier_kernels();
-    let_next_kernel_start();
     int seq, row0, row1;
     if (!find_tile(p.cu, p.num_seqs, p.M, 16, tile, seq, row0, row1)) return;   // (the whole cluster)
     const int ad = __ldg(p.adapter + seq);

@@ -23,7 +23,6 @@ __global__ void __launch_bounds__(kVec == 1 ? 256 : 1024) rmsnorm_kernel(const _
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int nvec = K >> 3;
     wait_for_earlier_kernels();
-    let_next_kernel_start();
     uint4 xv[kVec], rv[kVec], wv[kVec];
     // (threads past the row's end repeat its last vector and count for nothing: no condition around a load)
     auto load = [&](int row) {

@@ -23,7 +23,6 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __nv_bfloat
     constexpr int kHalf = kDim / 2, kPer = kHalf / 8;   // pieces of 8 pairs per head, and as many of 16 values
     const int t = blockIdx.x, H = c.num_heads, Hk = c.num_kv_heads;
     wait_for_earlier_kernels();
-    let_next_kernel_start();
     const int i = blockIdx.y * kThreads + threadIdx.x, piece = min(i, pieces - 1), head = piece / kPer, o = (piece % kPer) * 8;
     const bool turn = head < H + Hk;
     const __nv_bfloat16* src = qkv + ((size_t)t * (H + 2 * Hk) + head) * kDim + (turn ? o : 2 * o);
