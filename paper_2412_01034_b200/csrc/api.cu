@@ -50,7 +50,7 @@ qil_status check_paged(const PagedCache& c) {
     // positions, rows of the cache and grid sizes are 32-bit numbers
     constexpr long long kMost = 0x7FFFFFFF;
     if ((long long)c.max_pages * c.page_size > kMost || (long long)c.num_pages * c.num_kv_heads * c.page_size > kMost ||
-        (long long)c.total_q * c.num_heads > kMost || c.num_seqs > 65535 || c.num_heads + 2LL * c.num_kv_heads > 4096)
+        (long long)c.total_q * c.num_heads > kMost || c.num_seqs > 65534 || c.num_heads + 2LL * c.num_kv_heads > 4096)
         return QIL_ERR_SHAPE;
     return QIL_OK;
 }

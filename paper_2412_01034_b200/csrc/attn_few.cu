@@ -59,8 +59,13 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
-    wait_for_earlier_kernels();
-    if (p.before_many) let_next_kernel_start();   // (the kernel for many rows reads nothing of this one's results and runs beside it)
+    // Behind the kernel for many rows, whose blocks have all seen the end of what came before, nothing is waited for: the two
+    // run side by side.  But what comes after this launch may need both, so one more block lasts until that kernel ends.
+    if (!p.both) wait_for_earlier_kernels();
+    if (seq == p.c.num_seqs) {
+        if (split == 0 && kvh == 0) wait_for_earlier_kernels();
+        return;
+    }
     const int begin = split * p.chunk;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
     // (the first tile's page and the length are on the way with the starts, not after them)
@@ -300,7 +305,7 @@ template <int kDim>
 qil_status go(const AttnParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(attn_few_kernel<kDim>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
-    const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)p.c.num_seqs);
+    const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)(p.c.num_seqs + p.both));
     return launch_early(attn_few_kernel<kDim>, grid, 32 * kWarps, FewShape<kDim>::kSmem, st, p);
 }
 

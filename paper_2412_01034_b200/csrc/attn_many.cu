@@ -200,8 +200,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     using Shape = ManyShape<kDim>;
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
-    // (behind the kernel for few rows: all of its blocks have seen the end of what came before)
-    if (!p.after_few) wait_for_earlier_kernels();
+    wait_for_earlier_kernels();
+    if (p.both) let_next_kernel_start();   // (the kernel for few rows fills the SMs that this one leaves)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.G, H = p.c.num_heads, kvh = blockIdx.x % p.c.num_kv_heads;
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -254,9 +254,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    // Nothing here depends on the kernel for few rows, but what comes after this launch may: the first block lasts until that
-    // kernel is complete.
-    if (p.after_few && blockIdx.x == 0 && blockIdx.z == 0 && warp == 3) wait_for_earlier_kernels();
     if (!found) {   // (the grid is sized for the most tiles that the requests could have)
         if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
         return;
@@ -680,14 +677,18 @@ qil_status go(const AttnParams& p, cudaStream_t st) {
     if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
     // (heads first, so that the long tiles of all heads start before the short ones of any)
     const dim3 grid((unsigned)((long long)p.c.num_kv_heads * (p.c.total_q / (2 * p.tile_tokens) + p.c.num_seqs)), 1u, (unsigned)p.splits);
-    const qil_status s = launch_early(attn_many_kernel<kDim>, grid, kThreads, kSmem, st, mq, mk, mv, p);
-    if (s != QIL_OK || p.splits == 1) return s;
-    const long long items = (long long)p.c.total_q * p.c.num_heads;
-    return launch_early(attn_many_join_kernel<kDim>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
+    return launch_early(attn_many_kernel<kDim>, grid, kThreads, kSmem, st, mq, mk, mv, p);
 }
 
 }  // namespace
 
 qil_status launch_attn_many(const AttnParams& p, cudaStream_t st) { return p.c.head_dim == 128 ? go<128>(p, st) : go<64>(p, st); }
+
+qil_status launch_attn_many_join(const AttnParams& p, cudaStream_t st) {
+    const long long items = (long long)p.c.total_q * p.c.num_heads;
+    const dim3 grid((unsigned)((items + 3) / 4));
+    return p.c.head_dim == 128 ? launch_early(attn_many_join_kernel<128>, grid, 128, 0, st, p)
+                               : launch_early(attn_many_join_kernel<64>, grid, 128, 0, st, p);
+}
 
 }  // namespace qil

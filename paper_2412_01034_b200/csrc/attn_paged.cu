@@ -83,13 +83,12 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     p.counters = reinterpret_cast<int*>(base + kHeader);
     p.few_parts = reinterpret_cast<float*>(base + kHeader + pl.counter_bytes);
     p.many_parts = p.few_parts + pl.few_floats;   // (the two kernels may run at the same time)
-    p.before_many = pl.many;
-    p.after_few = pl.few;
-    if (pl.few) {
-        const qil_status s = launch_attn_few(p, st);
-        if (s != QIL_OK) return s;
-    }
-    return pl.many ? launch_attn_many(p, st) : QIL_OK;
+    p.both = pl.few && pl.many;
+    qil_status s = QIL_OK;
+    if (pl.many) s = launch_attn_many(p, st);
+    if (s == QIL_OK && pl.few) s = launch_attn_few(p, st);
+    if (s == QIL_OK && pl.many && pl.splits > 1) s = launch_attn_many_join(p, st);
+    return s;
 }
 
 }  // namespace qil

@@ -26,7 +26,7 @@ struct AttnParams {
     int* status;
     int* counters;       // [num_seqs][num_kv_heads] parts written so far, zero between launches
     float *few_parts, *many_parts;
-    bool before_many, after_few;   // few rows: a launch of the other kernel follows; many rows: one came before
+    int both;            // both kernels are launched, many rows first
 };
 
 // cached tokens that the table can name
@@ -40,5 +40,6 @@ __device__ __forceinline__ float fast_exp2(float x) {
 
 qil_status launch_attn_few(const AttnParams& p, cudaStream_t st);
 qil_status launch_attn_many(const AttnParams& p, cudaStream_t st);
+qil_status launch_attn_many_join(const AttnParams& p, cudaStream_t st);
 
 }  // namespace qil
