@@ -10,8 +10,8 @@
 // Both kernels take their operands straight from global memory in 16-byte loads and never stage them: the order of a
 // contraction's terms is free, so lane c of four takes 8 neighbouring elements and both operands use the same order; and
 // the columns of a group of four 16 x 8 results are dealt out so that a lane ends up with 8 neighbouring outputs.
-// Measured: 32 single tokens, 12 adapters of rank 16, 4096 x 4096: 7.5 us, a chain of five trips to memory (request, adapter,
-// operands, the cluster's parts, outputs).  4000 rows in nine prompts, rank 32, 4096 -> 11008: 13 + 36 us, against 34 us for
+// Measured: 32 single tokens, 12 adapters of rank 16, 4096 x 4096: 6.0 us (7.5 cold), a chain of five trips to memory (request, adapter,
+// operands, the cluster's parts, outputs).  4000 rows in nine prompts, rank 32, 4096 -> 11008: 12 + 33 us, against 34 us for
 // x, y and the output at the copy rate; of the second kernel's traffic a third is B, re-read from L2 for every 64 rows.
 // t is split into two bf16 terms (hi + lo) before it is multiplied: it keeps 16 significant bits.
 #include "layer_common.cuh"
@@ -20,10 +20,11 @@ namespace qil {
 
 namespace {
 
-constexpr int kDownWarps = 4, kUpWarps = 4, kMaxSlices = 32, kFusedWarps = 8, kCluster = 8;
-// Depth of the rings, and blocks of the second kernel per SM: by shared memory two blocks of the first and four of the second
-// kernel fit (4000 rows, rank 32, 4096 -> 11008: 49 us in all; a stage more of either ring takes a block away: 52 - 70 us).
-constexpr int kDownStages = 3, kUpStages = 2, kUpBlocks = 4;
+constexpr int kDownWarps = 4, kUpWarps = 8, kMaxSlices = 32, kFusedWarps = 8, kCluster = 8;
+// Depth of the rings, and blocks of the second kernel per SM: by shared memory two blocks of either kernel fit an SM (4000
+// rows, rank 32, 4096 -> 11008: 45 us in all; a stage more of either ring takes a block away: 52 to 70 us; blocks of half the
+// size and twice as many: 47 us, shorter shares of the outputs per block: 50 to 57 us).
+constexpr int kDownStages = 3, kUpStages = 2, kUpBlocks = 2;
 
 struct LoraParams {
     const __nv_bfloat16 *x, *a, *b, *y;
