@@ -12,8 +12,10 @@
 // tensor pipe is idle most of the time here and the multiply-adds of up to 16 rows cost the same as those of one.
 // A page holds a multiple of 16 tokens, so a tile lies in one page.  Tokens behind the last one arrive as zeros (cp.async
 // with a source size of zero), so that whatever the page holds there never meets a weight of zero.
-// The warps' results are joined in shared memory.  Where a request has several blocks, each writes its part (fp32, with
-// maximum and sum) to the workspace, and the block that counts itself in last adds the parts in the order of the blocks.
+// The warps' results are joined in shared memory.  Where a request has several blocks, up to eight of them in a launch of
+// one round are a cluster and join their results through one another's shared memory, each a share of the outputs;
+// otherwise each writes its part (fp32, with maximum and sum) to the workspace, and the block that counts itself in last
+// adds the parts.  Either way in the order of the blocks.
 #include "attn_paged.cuh"
 
 namespace qil {
@@ -28,7 +30,7 @@ struct FewShape {
     static constexpr int kStages = 3 * (128 / kDim);   // 96 KB a block, two blocks an SM
     static constexpr int kWarpBytes = kStages * 2 * kTileBytes;
     static constexpr int kSmem = kWarps * kWarpBytes;
-    static_assert(kWarps * kTile * kDim * 4 <= kSmem, "the warps' results fit where the rings were");
+    static_assert((kWarps + 1) * kTile * kDim * 4 <= kSmem, "the warps' results and the block's fit where the rings were");
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
@@ -40,6 +42,16 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
 __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// a value at this address of another block's shared memory
+__device__ __forceinline__ float ld_block(uint32_t addr, int block) {
+    uint32_t there;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(block));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return v;
+}
 __device__ __forceinline__ float quad_max(float v) {
     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
     return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
@@ -49,7 +61,8 @@ __device__ __forceinline__ float quad_sum(float v) {
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-template <int kDim>
+// kTogether: the blocks of a request and key head are one cluster.
+template <int kDim, bool kTogether>
 __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams p) {
     using Shape = FewShape<kDim>;
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kPieces = kDim / 8;   // 16-byte pieces of a row
@@ -77,8 +90,9 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     if (q_len <= 0 || q_len * (long long)G > kFewRows) return;
     const int rows = q_len * G, end = cache_end(p.c, kv), first_pos = kv - q_len;
     const int parts = max(1, min((end + p.chunk - 1) / p.chunk, p.slots));
-    if (split >= parts) return;
-    const int stop = split + 1 == parts ? end : min(begin + p.chunk, end);
+    const bool idle = split >= parts;   // (more blocks than the request's tokens need)
+    if (idle && !kTogether) return;
+    const int stop = idle ? begin : split + 1 == parts ? end : min(begin + p.chunk, end);
     const int tiles = (stop - begin + kTile - 1) / kTile;
 
     // visible tokens of this lane's two rows
@@ -262,6 +276,39 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         *reinterpret_cast<uint32_t*>(p.out + ((size_t)(row0 + r / G) * H + kvh * G + r % G) * kDim + d) = pack2(v.x * inv, v.y * inv);
     };
+    if (kTogether) {
+        // every block's result behind the warps' ones; then each block joins its share of the outputs over all blocks
+        float* mine = reinterpret_cast<float*>(smem) + kWarps * kTile * kDim;
+        for (int at = 2 * tid; at < rows * kDim; at += 2 * blockDim.x) *reinterpret_cast<float2*>(mine + at) = joined(at);
+        cluster_arrive();
+        cluster_wait();
+        const uint32_t here = (uint32_t)__cvta_generic_to_shared(mine), stats = (uint32_t)__cvta_generic_to_shared(&s_scale[0][0]);
+        for (int at = 2 * (split * (int)blockDim.x + tid); at < rows * kDim; at += 2 * (int)(gridDim.x * blockDim.x)) {
+            const int r = at / kDim;
+            float top[kMostTogether], part[kMostTogether], most = -INFINITY, sum = 0.f;
+            float2 u[kMostTogether], v = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int s = 0; s < kMostTogether; ++s) {
+                const int from = min(s, parts - 1);   // (all on the way at once; the repeated ones do not count)
+                top[s] = ld_block(stats + 4 * r, from);
+                part[s] = ld_block(stats + 64 + 4 * r, from);
+                u[s].x = ld_block(here + 4 * at, from);
+                u[s].y = ld_block(here + 4 * at + 4, from);
+                most = fmaxf(most, top[s]);
+            }
+#pragma unroll
+            for (int s = 0; s < kMostTogether; ++s) {
+                const float f = s >= parts || top[s] == -INFINITY ? 0.f : fast_exp2(top[s] - most);
+                sum = fmaf(part[s], f, sum);
+                v.x = fmaf(u[s].x, f, v.x);
+                v.y = fmaf(u[s].y, f, v.y);
+            }
+            write(at, v, sum);
+        }
+        cluster_arrive();   // (nobody leaves while another block may read its shared memory)
+        cluster_wait();
+        return;
+    }
     if (parts == 1) {
         for (int at = 2 * tid; at < rows * kDim; at += 2 * blockDim.x) write(at, joined(at), s_scale[1][at / kDim]);
         return;
@@ -301,16 +348,20 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     }
 }
 
-template <int kDim>
+template <int kDim, bool kTogether>
 qil_status go(const AttnParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(attn_few_kernel<kDim>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
-    const dim3 grid((unsigned)p.slots, (unsigned)p.c.num_kv_heads, (unsigned)(p.c.num_seqs + p.both));
-    return launch_early(attn_few_kernel<kDim>, grid, 32 * kWarps, FewShape<kDim>::kSmem, st, p);
+    if (!allow_smem(attn_few_kernel<kDim, kTogether>, FewShape<kDim>::kSmem, allowed)) return QIL_ERR_CUDA;
+    const unsigned across = !kTogether ? (unsigned)p.slots : p.slots <= 2 ? 2u : p.slots <= 4 ? 4u : (unsigned)kMostTogether;
+    const dim3 grid(across, (unsigned)p.c.num_kv_heads, (unsigned)(p.c.num_seqs + p.both));
+    return launch_early_clusters(attn_few_kernel<kDim, kTogether>, kTogether ? across : 1u, grid, 32 * kWarps, FewShape<kDim>::kSmem, st, p);
 }
 
 }  // namespace
 
-qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) { return p.c.head_dim == 128 ? go<128>(p, st) : go<64>(p, st); }
+qil_status launch_attn_few(const AttnParams& p, cudaStream_t st) {
+    if (p.c.head_dim == 128) return p.together ? go<128, true>(p, st) : go<128, false>(p, st);
+    return p.together ? go<64, true>(p, st) : go<64, false>(p, st);
+}
 
 }  // namespace qil

@@ -9,7 +9,7 @@ namespace qil {
 // Query heads that share a key head are packed into the rows of one tile: row r of a request and key head h is new token
 // r / G, query head h G + r % G.  Requests of at most kFewRows rows (single tokens, short drafts) run on the kernel that
 // splits the cache over the GPU, the others on the tensor-memory kernel.
-constexpr int kFewRows = 16, kTileRows = 128;
+constexpr int kFewRows = 16, kTileRows = 128, kMostTogether = 8;
 
 struct AttnParams {
     const __nv_bfloat16 *q, *k, *v;
@@ -20,6 +20,7 @@ struct AttnParams {
     int page_shift;      // log2 of the page size
     int chunk;           // few rows: cached tokens of one block
     int slots;           // few rows: blocks per request and key head at most
+    int together;        // few rows: the blocks of a request and key head are one cluster
     int few_rows;        // few rows: rows of a part in the workspace
     int splits;          // many rows: parts of the cache
     int tile_tokens;     // many rows: new tokens of a row tile, kTileRows / G

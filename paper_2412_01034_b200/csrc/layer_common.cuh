@@ -128,22 +128,30 @@ inline bool allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>
 __device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// An early launch, as described above.
+// An early launch, as described above; in clusters of `cluster` blocks along x.
 template <class Kernel, class... Args>
-inline qil_status launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+inline qil_status launch_early_clusters(Kernel kernel, unsigned cluster, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess) return QIL_OK;
     (void)cudaGetLastError();
     return QIL_ERR_CUDA;
+}
+
+template <class Kernel, class... Args>
+inline qil_status launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+    return launch_early_clusters(kernel, 1u, grid, threads, smem, st, args...);
 }
 
 // Internal launchers.
