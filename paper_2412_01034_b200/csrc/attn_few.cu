@@ -2,8 +2,8 @@
 // short drafts.  Memory bound: every cached key and value of a request is read once per key head, 4 D bytes a token, and
 // the query rows are one 16-row operand.
 // Measured: 32 requests of up to 4099 tokens, 32 key heads of 128 (1.38 GB): 213 us from memory = 6.45 TB/s, 98 % of the copy
-// rate.  48 requests of up to 300 tokens: 39 us against 22 at the copy rate, one request over 287 tokens 7.4 us: there a
-// block's way to its first tile (lengths, page, keys: three trips to memory) is what counts.
+// rate.  48 requests of up to 300 tokens: 32 us against 23 at the copy rate; one token over 287: 5.1 us: there a block's way
+// to its first tile (lengths, page, keys: three trips to memory) is what counts.
 //
 // A block takes `chunk` cached tokens of one request and key head; its four warps take tiles of 16 tokens in turn and are
 // independent of one another: each has its own ring of tiles in shared memory (cp.async, 16-byte pieces, the pieces of a
