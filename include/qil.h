@@ -429,8 +429,9 @@ qil_status qil_rmsnorm(const void* x, const void* residual, const void* weight, 
  * request b sits in page block_table[b][j / page_size] (block_table [num_seqs][max_pages] int32), slot j % page_size.
  * kv_len [num_seqs] int32 counts a request's cached tokens, the new ones of this call among them: new token i of q_len
  * has position kv_len - q_len + i.  head_dim is 64 or 128, page_size 16, 32, 64 or 128, num_heads a multiple of
- * num_kv_heads; at most 65534 requests and 4096 heads of all kinds.  Pages named by the table are read and written only if they exist: what a page number outside
- * [0, num_pages) stands for is unspecified, but nothing outside the caches is touched.  Table entries past a request's
+ * num_kv_heads; at most 65534 requests and 4096 heads of all kinds.  Pages named by the table are read and written only if
+ * they exist: what a page number outside [0, num_pages) stands for is unspecified, but nothing outside the caches is
+ * touched.  Table entries past a request's
  * last token are not read as pages.
  *
  * qil_rope_append: rotary embedding of the new tokens' queries and keys, and the append of their keys and values.
