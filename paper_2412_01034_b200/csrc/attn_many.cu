@@ -37,6 +37,7 @@ namespace {
 
 constexpr int kRows = kTileRows, kTok = 128, kThreads = 384;
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+constexpr float kMostSum = 16384.f;   // 64 weights of 2^kRaise
 constexpr float kRaise = 8.f;   // log2 by which a score may exceed the reference maximum
 
 template <int kDim>
@@ -428,12 +429,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
             const bool edge = __any_sync(0xffffffffu, left < kTok);
             bool done = false;
             if (j > 0 && !edge) {
-                // Weights against the present reference while the tile's maximum is still being found: it hardly ever
-                // exceeds the reference by more than the limit, and the exponentials need not wait for it.  The first 64
-                // tokens' product starts while the other weights are computed.
+                // Weights against the present reference before the tile's maximum is known: it hardly ever exceeds the reference
+                // by more than the limit, and the exponentials need not wait for it.  The first 64 tokens' product starts while
+                // the other weights are computed, so for those the maximum is found beforehand; the first ones' sum says
+                // itself whether one of them was too large (a maximum of them as well cost 2 % of the time).
                 const unsigned long long scale2 = f2(scale, scale), base2 = f2(-ref, -ref);
                 unsigned long long acc[2] = {0ull, 0ull};
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float top[2] = {-INFINITY, -INFINITY};
                 auto weights = [&](int c, bool find) {
                     uint32_t w[32];
 #pragma unroll
@@ -443,23 +445,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                         f2_split(x, a, b);
                         a = fast_exp2(a);
                         b = fast_exp2(b);
-                        if (find) {
-                            top[e & 1] = max3(top[e & 1], __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
-                            top[2 + (e & 1)] = max3(top[2 + (e & 1)], __uint_as_float(s[64 + 2 * e]), __uint_as_float(s[64 + 2 * e + 1]));
-                        }
+                        if (find) top[e & 1] = max3(top[e & 1], __uint_as_float(s[64 + 2 * e]), __uint_as_float(s[64 + 2 * e + 1]));
                         acc[e & 1] = f2_add(acc[e & 1], f2(a, b));
                         w[e] = pack2(a, b);
                     }
                     tmem_st32(s_at + c / 2, w);
                 };
                 weights(0, true);
-                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
-                done = !__any_sync(0xffffffffu, live && !(most <= ref + kRaise));
+                float a, b;
+                f2_split(f2_add(acc[0], acc[1]), a, b);
+                done = !__any_sync(0xffffffffu, live && !(a + b <= kMostSum && fmaxf(top[0], top[1]) * scale <= ref + kRaise));
                 if (done) {
                     publish(0);
                     weights(64, false);
                     publish(1);
-                    float a, b;
                     f2_split(f2_add(acc[0], acc[1]), a, b);
                     sum += a + b;
                 }
