@@ -17,8 +17,8 @@
 // lies behind a request's last token in its last tile of V (a weight of zero times NaN would be NaN).
 // Every wait is bounded; when one runs out QIL_ERR_TIMEOUT is recorded and the block ends.
 //
-// Measured, 4096 new tokens over 8192, 32 heads of 128 (412 GFLOP): 378 us (1090 TFLOP/s) until the power cap sets in, 412 to
-// 440 us (940 to 1000 TFLOP/s at 1.65 GHz, 1000 W) sustained.  A step (128 tokens, both row tiles) takes 2830 cycles; the
+// Measured, 4096 new tokens over 8192, 32 heads of 128 (412 GFLOP): 368 us (1120 TFLOP/s) until the power cap sets in, 396 to
+// 430 us (960 to 1040 TFLOP/s at 1.65 GHz, 1000 W) sustained.  A step (128 tokens, both row tiles) takes 2830 cycles; the
 // products alone would take 2048 (32 of 128 x 128 x 16, 64 cycles each), and the exponentials of both tiles 2048 on the
 // special-function units as well.  Per tile: 1660 cycles from S to P, 1130 waiting (half of the product, S, and their
 // latencies; the issuing thread needs 64 cycles a product, as long as the pipe does).  Tried and slower: part of the

@@ -11,10 +11,14 @@ namespace qil {
 
 namespace {
 
+// The counters lie in the same place whatever the call's sizes are: they have to be zero between launches, and the parts of
+// one call must not lie where another call that shares the workspace has its counters.
+constexpr long long kCounters = 16384;
+
 struct AttnPlan {
     bool few, many, together;
     int chunk, slots, few_rows, splits;
-    size_t counter_bytes, few_floats, many_floats;
+    size_t few_floats, many_floats;
 };
 
 AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, int max_kv) {
@@ -43,11 +47,11 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
                 pl.together = max_kv > chunk;
             }
         }
+        if (items > kCounters) chunk = max_kv;   // (rows enough to fill the GPU many times over: one block each)
         pl.chunk = (int)chunk;
         pl.slots = (int)((max_kv + chunk - 1) / chunk);
         const long long rows = (long long)max_q * G;
         pl.few_rows = (int)(rows < kFewRows ? rows : kFewRows);
-        pl.counter_bytes = ((size_t)items * sizeof(int) + 255) & ~(size_t)255;
         if (pl.slots > 1 && !pl.together) pl.few_floats = ((size_t)items * pl.slots * pl.few_rows * (D + 2) + 3) & ~(size_t)3;   // (16-byte stores behind them)
     }
     if (pl.many) {
@@ -70,7 +74,7 @@ constexpr size_t kHeader = 256;   // status word
 
 size_t attn_paged_workspace(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int max_q_len, int max_kv_len) {
     const AttnPlan pl = plan_attn(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len);
-    return kHeader + pl.counter_bytes + (pl.few_floats + pl.many_floats) * sizeof(float);
+    return kHeader + kCounters * sizeof(int) + (pl.few_floats + pl.many_floats) * sizeof(float);
 }
 
 qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const PagedCache& c, int max_q_len,
@@ -94,7 +98,7 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     char* base = static_cast<char*>(ws);
     p.status = reinterpret_cast<int*>(base);
     p.counters = reinterpret_cast<int*>(base + kHeader);
-    p.few_parts = reinterpret_cast<float*>(base + kHeader + pl.counter_bytes);
+    p.few_parts = reinterpret_cast<float*>(base + kHeader + kCounters * sizeof(int));
     p.many_parts = p.few_parts + pl.few_floats;   // (the two kernels may run at the same time)
     p.both = pl.few && pl.many;
     qil_status s = QIL_OK;

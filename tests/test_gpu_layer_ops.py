@@ -291,6 +291,24 @@ def test_attn_paged_is_deterministic_and_its_workspace_is_reusable(api):
     assert int(ws[:4].view(torch.int32)[0]) == 0
 
 
+def test_attn_paged_workspace_of_calls_of_every_size(api):
+    """Calls with many and with few rows of the cache take turns on one workspace: the counters of one must not lie where
+    another keeps its parts."""
+    cases = [([1] * 5, [3000, 2500, 2900, 31, 2999], 32, 32), ([1], [20000], 1, 1), ([1] * 3, [2999] * 3, 64, 64), ([40, 1], [4000, 9], 2, 1)]
+    size = max(api.attn_paged_workspace_size(sum(q), len(q), H, Hk, 64, max(q), max(kv)) for q, kv, H, Hk in cases)
+    ws = api.new_workspace(size)
+    made = [attention_inputs(gen(180 + i), *c, 64, 64, poison=False) for i, c in enumerate(cases)]
+
+    def call(i, workspace):
+        (q, kc, vc, table, _), (q_lens, kv_lens, _, _) = made[i], cases[i]
+        return api.attn_paged(q, kc, vc, ints(starts(q_lens)), ints(kv_lens), table, max(q_lens), max(kv_lens), workspace=workspace)
+
+    want = [call(i, None) for i in range(len(cases))]
+    for i in (0, 1, 0, 3, 2, 1, 2, 0, 3, 0):
+        out = call(i, ws)
+        assert torch.equal(out, want[i]), i
+
+
 def test_attn_paged_bounds_may_be_loose(api):
     q_lens, kv_lens = [1, 2, 1], [100, 300, 7]
     q, kc, vc, table, tab = attention_inputs(gen(81), q_lens, kv_lens, 4, 4, 128, 16)
