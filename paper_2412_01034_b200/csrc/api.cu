@@ -316,7 +316,7 @@ qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cach
 }
 
 size_t qil_lora_batch_workspace_size(int M, int num_seqs, int rank) {
-    if (M <= 0 || num_seqs <= 0 || rank <= 0) return 0;
+    if (M <= 0 || M > (1 << 30) || num_seqs <= 0 || num_seqs > (1 << 24) || rank <= 0) return 0;
     return lora_batch_workspace(M, num_seqs, rank);
 }
 
@@ -328,7 +328,7 @@ qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const
         return QIL_ERR_SHAPE;
     if (ldx < K || ldy < N || ldo < N || ldx % 8 != 0 || ldy % 8 != 0 || ldo % 8 != 0 || (out == y && ldo != ldy)) return QIL_ERR_SHAPE;
     if (rank > 64) return QIL_ERR_UNSUPPORTED;
-    if ((N + 127) / 128 > 65535) return QIL_ERR_SHAPE;   // (grid size)
+    if ((N + 127) / 128 > 65535 || num_seqs > (1 << 24) || M > (1 << 30)) return QIL_ERR_SHAPE;   // (grid sizes)
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) || !aligned4(cu_q) ||
         !aligned4(adapter) || !aligned4(scales))
         return QIL_ERR_ALIGN;

@@ -96,6 +96,7 @@ def test_lora_batch_validation(lib):
     need = lib.qil_lora_batch_workspace_size(4, 2, 8)
     assert need > 0 and f(nbytes=need - 1) == 5 and f(ws=None) == 5 and f(ws=U) == 3
     assert lib.qil_lora_batch_workspace_size(0, 1, 8) == 0
+    assert f(num_seqs=(1 << 24) + 1) == 2 and f(M=(1 << 30) + 1) == 2
 
 
 def test_the_binding_refuses_wrong_tensors():
