@@ -450,7 +450,7 @@ qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, v
  * cached tokens 0 ... p of its request:
  *     out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,   k_j, v_j of key head h / (num_heads / num_kv_heads)
  *   A token that sees nothing (kv_len < q_len) gets zeros.  q, out [total_q][num_heads][head_dim].
- *   What lies in the caches behind a request's last token, be it infinite or NaN, has no influence.
+ *   What lies in the caches behind the tokens that a token sees, be it infinite or NaN, has no influence on it.
  *   max_q_len, max_kv_len: bounds on the requests' q_len and kv_len that the host knows.  They choose how the work is
  *   split; a request that exceeds them gets unspecified results.
  *   workspace: qil_attn_paged_workspace_size() bytes, zero-filled once; calls that share it must not overlap.  Its first

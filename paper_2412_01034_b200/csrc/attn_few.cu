@@ -12,6 +12,8 @@
 // tensor pipe is idle most of the time here and the multiply-adds of up to 16 rows cost the same as those of one.
 // A page holds a multiple of 16 tokens, so a tile lies in one page.  Tokens behind the last one arrive as zeros (cp.async
 // with a source size of zero), so that whatever the page holds there never meets a weight of zero.
+// Of several new tokens the earlier ones must not see the later ones' values: tiles that hold such values are looked through,
+// and those with an infinity or a NaN are added token by token.
 // The warps' results are joined in shared memory.  Where a request has several blocks, up to eight of them in a launch of
 // one round are a cluster and join their results through one another's shared memory, each a share of the outputs;
 // otherwise each writes its part (fp32, with maximum and sum) to the workspace, and the block that counts itself in last
@@ -41,6 +43,16 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
 }
 __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 lds_pair(uint32_t addr) {   // two bf16
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -213,14 +225,47 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] *= keep[e >> 1];
         }
+        // A value that some row must not see and that is infinite or NaN stays out of that row (the products of a tile would
+        // add zero times it): such a tile's weights and values are multiplied one token after the other.
+        bool apart = false;
+        if (tok + kTile > all_see && all_see < stop) {
 #pragma unroll
-        for (int n = 0; n < kDim / 16; ++n) {
-            // matrices: tokens 0-7 / 8-15 at columns 16 n, then the same at 16 n + 8, transposed
-            const int piece = 2 * n + lhalf;
-            uint32_t b[4];
-            ldsm4t(b, vt + lrow * (kDim * 2) + ((piece & ~7) | ((piece ^ lrow) & 7)) * 16);
-            mma16816(o[2 * n], pa, b[0], b[1]);
-            mma16816(o[2 * n + 1], pa, b[2], b[3]);
+            for (int j = 0; j < kTile * kPieces / 32; ++j) {
+                const int piece = j * 32 + lane, r = piece / kPieces, o8 = piece % kPieces;
+                if (tok + r >= all_see) apart |= any_not_finite(lds128(vt + r * (kDim * 2) + ((o8 & ~7) | ((o8 ^ r) & 7)) * 16));
+            }
+            apart = __any_sync(0xffffffffu, apart);
+        }
+        if (apart) {
+#pragma unroll 1
+            for (int t = 0; t < kTile; ++t) {
+                float w[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float even = t < 8 ? s[0][2 * h] : s[1][2 * h], odd = t < 8 ? s[0][2 * h + 1] : s[1][2 * h + 1];
+                    w[h] = __shfl_sync(0xffffffffu, t & 1 ? odd : even, (lane & ~3) | ((t & 7) >> 1));
+                }
+#pragma unroll
+                for (int n = 0; n < kDim / 8; ++n) {
+                    const float2 v = lds_pair(vt + t * (kDim * 2) + ((n & ~7) | ((n ^ t) & 7)) * 16 + 4 * c);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (tok + t < see[h]) {
+                            o[n][2 * h] = fmaf(w[h], v.x, o[n][2 * h]);
+                            o[n][2 * h + 1] = fmaf(w[h], v.y, o[n][2 * h + 1]);
+                        }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < kDim / 16; ++n) {
+                // matrices: tokens 0-7 / 8-15 at columns 16 n, then the same at 16 n + 8, transposed
+                const int piece = 2 * n + lhalf;
+                uint32_t b[4];
+                ldsm4t(b, vt + lrow * (kDim * 2) + ((piece & ~7) | ((piece ^ lrow) & 7)) * 16);
+                mma16816(o[2 * n], pa, b[0], b[1]);
+                mma16816(o[2 * n + 1], pa, b[2], b[3]);
+            }
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
         into = into + 1 == kStages ? 0 : into + 1;

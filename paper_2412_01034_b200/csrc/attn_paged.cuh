@@ -39,6 +39,15 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return y;
 }
 
+// one of eight bf16 is infinite or NaN
+__device__ __forceinline__ bool any_not_finite(uint4 v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7F800000u) == 0x7F800000u || (w[e] & 0x7F80u) == 0x7F80u;
+    return any;
+}
+
 qil_status launch_attn_few(const AttnParams& p, cudaStream_t st);
 qil_status launch_attn_many(const AttnParams& p, cudaStream_t st);
 qil_status launch_attn_many_join(const AttnParams& p, cudaStream_t st);

@@ -291,6 +291,33 @@ def test_attn_paged_is_deterministic_and_its_workspace_is_reusable(api):
     assert int(ws[:4].view(torch.int32)[0]) == 0
 
 
+@pytest.mark.parametrize("q_len,kv,H,Hk,D,page", [(6, 300, 4, 2, 128, 16), (16, 16, 3, 3, 64, 32), (5, 4100, 3, 1, 128, 64), (16, 700, 2, 2, 64, 16),
+                                                  (300, 500, 2, 2, 128, 16), (280, 280, 4, 1, 64, 64), (70, 70, 6, 2, 128, 128), (130, 6100, 2, 1, 128, 64)])
+@pytest.mark.parametrize("scale", [None, -0.1, 0.0])
+def test_attn_paged_values_that_are_not_finite_stay_out_of_earlier_tokens(api, q_len, kv, H, Hk, D, page, scale):
+    """A new token's value holds a NaN and an infinity, the last one's key is infinite: the new tokens before them are as if
+    they were not there, the others get them in their columns (the last one everywhere)."""
+    q, kc, vc, table, tab = attention_inputs(gen(90 + q_len + D), [q_len], [kv], H, Hk, D, page)
+    bad = kv - q_len + q_len // 2
+    vc[tab[0, bad // page], :, bad % page, 5] = float("nan")
+    vc[tab[0, bad // page], :, bad % page, D - 3] = float("inf")
+    kc[tab[0, (kv - 1) // page], :, (kv - 1) % page] = float("inf")
+    got = f64(api.attn_paged(q, kc, vc, ints([0, q_len]), ints([kv]), table, q_len, kv, scale=scale))
+    s = D ** -0.5 if scale is None else scale
+    with np.errstate(all="ignore"):
+        want, spread, absdot = np_layer.attn(f64(q), np_layer.gather_cache(f64(kc), tab[0], kv), np_layer.gather_cache(f64(vc), tab[0], kv), kv - q_len, s)
+    before, n = kv - 1 - (kv - q_len), q_len // 2
+    weight = BF16_HALF_ULP + 2 * (D + 4) * 2.0 ** -24 * absdot[:before, :, None] + 2.0 ** -14
+    clean = np.ones(D, dtype=bool)
+    clean[[5, D - 3]] = False
+    tol = BF16_HALF_ULP * np.abs(want[:before]) + weight * spread[:before] + 1e-30
+    assert_within(got[:n], want[:n], tol[:n])
+    assert_within(got[n:before][:, :, clean], want[n:before][:, :, clean], tol[n:][:, :, clean])
+    assert not np.isfinite(got[n:][:, :, ~clean]).any()
+    if s != 0.0:
+        assert not np.isfinite(got[before]).any()
+
+
 def test_attn_paged_workspace_of_calls_of_every_size(api):
     """Calls with many and with few rows of the cache take turns on one workspace: the counters of one must not lie where
     another keeps its parts."""
