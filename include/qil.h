@@ -191,7 +191,8 @@ qil_status qil_lora_side_add(const void* x, const void* a, const void* b, void* 
  * == 0) gate and up products stay in fp32 until the result is rounded to bf16
  * once; on all other shapes the linear is computed as by qil_linear_w4a16 into
  * the workspace (bf16) and a second kernel applies the activation.
- * workspace: qil_linear_w4a16_swiglu_workspace_size() bytes, zero-filled once.
+ * workspace: qil_linear_w4a16_swiglu_workspace_size() bytes, zero-filled once; calls of
+ * this function and of qil_linear_w4a16, of any shapes, may take turns on one workspace.
  * Errors: NULL, SHAPE (also odd N), ALIGN, WORKSPACE, UNSUPPORTED, CUDA.
  * ---------------------------------------------------------------------- */
 size_t qil_linear_w4a16_swiglu_workspace_size(int M, int N, int K, int group_size);

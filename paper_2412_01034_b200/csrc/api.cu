@@ -214,9 +214,13 @@ qil_status qil_linear_w4a16(const void* x, const uint32_t* qweight, const void* 
     return launch_w4a16_general(x, qweight, scales, zeros, y, M, N, K, group_size, S(stream));
 }
 
-// Bytes of the plain linear's workspace, rounded so that the bf16 scratch of the unfused path can follow it.
+// Where the bf16 scratch of the unfused path begins: behind the plain linear's workspace, and behind the split-K counters
+// that other shapes have in the same workspace even where this shape has none (a call's scratch must not lie where another
+// call expects zeros, so that one workspace, zero-filled once, serves calls of every shape).
 static size_t swiglu_tmp_offset(int M, int N, int K, int group_size) {
-    return (qil_linear_w4a16_workspace_size(M, N, K, group_size) + 255) / 256 * 256;
+    const size_t plain = qil_linear_w4a16_workspace_size(M, N, K, group_size);
+    const size_t counters = w4a16_skinny_ws_offset() + w4a16_skinny_counter_bytes();
+    return ((plain > counters ? plain : counters) + 255) / 256 * 256;
 }
 
 size_t qil_linear_w4a16_swiglu_workspace_size(int M, int N, int K, int group_size) {
