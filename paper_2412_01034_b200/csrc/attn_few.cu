@@ -101,6 +101,9 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     const int q_len = row1 - row0;
     if (q_len <= 0 || q_len * (long long)G > kFewRows) return;
     const int rows = q_len * G, end = cache_end(p.c, kv), first_pos = kv - q_len;
+    // A part in the workspace has room for the rows of max_q_len tokens: a request with more of them (the bound was wrong) is
+    // left out, it would write over its neighbours' parts and past the workspace.
+    if (!kTogether && p.slots > 1 && rows > p.few_rows) return;
     const int parts = max(1, min((end + p.chunk - 1) / p.chunk, p.slots));
     const bool idle = split >= parts;   // (more blocks than the request's tokens need)
     if (idle && !kTogether) return;
