@@ -302,8 +302,8 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
     if (tid < 16) {
         float most = s_m[0][tid], sum = 0.f;
         for (int w = 1; w < kWarps; ++w) most = fmaxf(most, s_m[w][tid]);
-        for (int w = 0; w < kWarps; ++w)
-            if (s_m[w][tid] != -INFINITY) sum += s_l[w][tid] * fast_exp2(s_m[w][tid] - most);
+        // (a maximum of -inf: the warp has seen nothing, its sum is zero; or only scores that are NaN, and so is its sum)
+        for (int w = 0; w < kWarps; ++w) sum += s_l[w][tid] * (s_m[w][tid] == -INFINITY ? 0.f : fast_exp2(s_m[w][tid] - most));
         s_scale[0][tid] = most;
         s_scale[1][tid] = sum;
     }
@@ -385,8 +385,7 @@ __global__ void __launch_bounds__(32 * kWarps) attn_few_kernel(const AttnParams 
         for (int s = 0; s < parts; ++s) {
             const float* q = first + s * part_floats;
             const float ms = __ldcg(q + p.few_rows * kDim + r);
-            if (ms == -INFINITY) continue;
-            const float f = fast_exp2(ms - most);
+            const float f = ms == -INFINITY ? 0.f : fast_exp2(ms - most);   // (times zeros, or a NaN that stays one)
             const float2 u = __ldcg(reinterpret_cast<const float2*>(q + at));
             sum = fmaf(__ldcg(q + p.few_rows * (kDim + 1) + r), f, sum);
             v.x = fmaf(u.x, f, v.x);

@@ -34,3 +34,37 @@ def test_attn_paged_more_new_tokens_than_the_bound(api, q_lens, kv_lens, max_q):
     ones = [min(n, 1) for n in q_lens]
     few = q[:sum(ones)]
     check_attention(api, few, kc, vc, table, tab, ones, kv_lens, workspace=ws)
+
+
+# (requests, heads, key heads, dim, new tokens, cached tokens): the ways in which a request's parts are joined
+JOINS = {"one_block": (1, 4, 2, 128, 1, 90), "cluster": (1, 8, 2, 128, 3, 700), "workspace": (8, 32, 32, 64, 1, 1000), "workspace_drafts": (9, 32, 32, 128, 4, 1500),
+         "prompt": (2, 8, 2, 64, 70, 300), "prompt_parts": (1, 4, 2, 128, 60, 3000)}
+
+
+@pytest.mark.parametrize("how", list(JOINS))
+def test_attn_paged_nan_queries(api, how):  # noqa: F811
+    """A query with a NaN gives NaN, on every way through the kernels; nothing else does."""
+    B, H, Hk, D, n, kv = JOINS[how]
+    q_lens, kv_lens = [n] * B, [kv - 3 * b for b in range(B)]
+    q, kc, vc, table, _ = attention_inputs(gen(710), q_lens, kv_lens, H, Hk, D, 64)
+    call = lambda: api.attn_paged(q, kc, vc, ints(starts(q_lens)), ints(kv_lens), table, n, kv)  # noqa: E731
+    want, bad = call(), torch.zeros(B * n, H, dtype=torch.bool, device="cuda")
+    assert torch.isfinite(want).all()
+    for t, h in ((0, H - 1), (B * n - 1, 0), (B * n // 2, H // 2)):
+        q[t, h, (5 * t + h) % D] = float("nan")
+        bad[t, h] = True
+    got = call()
+    assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("B,H,D,chunk,max_kv", [(8, 32, 64, 896, 1000), (9, 32, 128, 1472, 1500), (40, 8, 64, 2048, 2100), (1, 2, 128, 128, 188)])
+def test_attn_paged_a_nan_key_alone_in_its_part(api, B, H, D, chunk, max_kv):  # noqa: F811
+    """The last cached token, which may be the only one of a block's part (parts of `chunk` tokens), has a key with a NaN: whoever sees it gets NaN."""
+    for kv in (chunk, chunk + 1, chunk + 2):
+        kv_lens = [kv] + [max_kv] * (B - 1)
+        q, kc, vc, table, tab = attention_inputs(gen(720), [1] * B, kv_lens, H, H, D, 64)
+        kc[tab[0, (kv - 1) // 64], 1, (kv - 1) % 64, 7] = float("nan")
+        got = api.attn_paged(q, kc, vc, ints(starts([1] * B)), ints(kv_lens), table, 1, max_kv)
+        bad = torch.zeros(B, H, dtype=torch.bool, device="cuda")
+        bad[0, 1] = True
+        assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all(), kv
