@@ -453,7 +453,7 @@ qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, v
  *   A token that sees nothing (kv_len < q_len) gets zeros.  q, out [total_q][num_heads][head_dim].
  *   What lies in the caches behind the tokens that a token sees, be it infinite or NaN, has no influence on it.
  *   max_q_len, max_kv_len: bounds on the requests' q_len and kv_len that the host knows.  They choose how the work is
- *   split; a request that exceeds them gets unspecified results (nothing but its own rows of out is affected).
+ *   split; a request that exceeds them gets unspecified results, the others keep theirs.
  *   workspace: qil_attn_paged_workspace_size() bytes, zero-filled once; calls that share it must not overlap.  Its first
  *   int is a status word (QIL_ERR_TIMEOUT if a bounded device-side wait ran out; see qil_device_status).
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also a scale that is not finite, and more than 128 heads to a key head),

@@ -27,8 +27,10 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
     const long long sms = num_sms();
     if (max_q > total_q) max_q = total_q;
     pl.many = (long long)max_q * G > kFewRows;
-    // every request has more than kFewRows rows if the others at their longest leave more for it
-    pl.few = !(((long long)total_q - (long long)(num_seqs - 1) * max_q) * G > kFewRows);
+    // Every request has more than kFewRows rows if the others at their longest leave more for it.  (More than max_q left says
+    // that the bound is wrong, and nothing about any one request.)
+    const long long least = (long long)total_q - (long long)(num_seqs - 1) * max_q;
+    pl.few = least * G <= kFewRows || least > max_q;
     if (pl.few) {
         // Two blocks fit an SM, and one round of blocks is best: each of 2048 tokens at most (the requests' lengths differ).
         // Where it gives a row of the cache (a request and key head) at least two blocks, up to eight of 128 tokens or more

@@ -68,3 +68,15 @@ def test_attn_paged_a_nan_key_alone_in_its_part(api, B, H, D, chunk, max_kv):  #
         bad = torch.zeros(B, H, dtype=torch.bool, device="cuda")
         bad[0, 1] = True
         assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all(), kv
+
+
+@pytest.mark.parametrize("q_lens,kv_lens,max_q,H,Hk", [([1, 40, 2], [90, 300, 7], 2, 4, 4), ([3, 100, 1, 9], [33, 500, 300, 9], 9, 8, 2), ([50, 120], [50, 130], 50, 4, 4)])
+def test_attn_paged_one_request_beyond_the_bound(api, q_lens, kv_lens, max_q, H, Hk):  # noqa: F811
+    """More rows in all than the bound on each allows: the requests that keep to it have their results."""
+    q, kc, vc, table, tab = attention_inputs(gen(730), q_lens, kv_lens, H, Hk, 64, 16)
+    want = check_attention(api, q, kc, vc, table, tab, q_lens, kv_lens)
+    cu, out = starts(q_lens), torch.full_like(q, 77.0)
+    api.attn_paged(q, kc, vc, ints(cu), ints(kv_lens), table, max_q, max(kv_lens), out=out)
+    for b, n in enumerate(q_lens):
+        if n <= max_q:
+            np.testing.assert_allclose(f64(out[cu[b]:cu[b + 1]]), f64(want[cu[b]:cu[b + 1]]), atol=2.0 ** -6, err_msg=str(b))
