@@ -164,10 +164,15 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
     __shared__ __align__(16) uint32_t frag[kMT * kSteps * 2 * 32 * 4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     int seq, row0, row1;
-    if (!find_tile(p.cu, p.num_seqs, p.M, 16 * kMT, blockIdx.x, seq, row0, row1)) return;
-    const int ad = __ldg(p.adapter + seq);
+    // Blocks without work leave at once, all but one: what comes after this launch waits for it alone, so it has to last until
+    // the first kernel ends even if no request has an adapter.
+    const bool found = find_tile(p.cu, p.num_seqs, p.M, 16 * kMT, blockIdx.x, seq, row0, row1);
+    const int ad = found ? __ldg(p.adapter + seq) : -1;
     const bool none = ad < 0 || ad >= p.num_adapters;
-    if (none && p.out == p.y) return;
+    if (!found || (none && p.out == p.y)) {
+        if (blockIdx.x == 0 && blockIdx.y == 0) wait_for_earlier_kernels();
+        return;
+    }
     const __nv_bfloat16* b = p.b + (size_t)(none ? 0 : ad) * p.N * p.rank;
     // Rows past the tile's last, columns past N and rank elements past the rank repeat others: the first two are not
     // written, the last meet zeros of t.  (Conditions around the loads would make them wait for one another.)

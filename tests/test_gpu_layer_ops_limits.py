@@ -80,3 +80,30 @@ def test_attn_paged_one_request_beyond_the_bound(api, q_lens, kv_lens, max_q, H,
     for b, n in enumerate(q_lens):
         if n <= max_q:
             np.testing.assert_allclose(f64(out[cu[b]:cu[b + 1]]), f64(want[cu[b]:cu[b + 1]]), atol=2.0 ** -6, err_msg=str(b))
+
+
+def test_lora_batch_without_adapters_in_a_chain(api):  # noqa: F811
+    """Prompts of which none has an adapter, in place (the second kernel has nothing to do), between work that changes what the
+    call before and after reads: adapters, rows and workspace.  As in calls one by one."""
+    g = gen(740)
+    q_lens, K, N, r, n = [300, 17, 200, 90], 2048, 1024, 32, 2
+    M, cu = sum(q_lens), ints(starts(q_lens))
+    a, b, scales = draw(g, n, r, K, std=K ** -0.5), draw(g, n, N, r), torch.tensor([0.5, -1.0], device="cuda")
+    picks = [ints(p) for p in ([-1] * 4, [0, -1, 1, 0], [-1, 2, 7, -5], [1, 1, 0, -1])]
+    x0, y0 = draw(g, M, K), draw(g, M, N)
+    size = api.lora_batch_workspace_size(M, len(q_lens), r)
+
+    def chain(after):
+        x, y, ad, ws = x0.clone(), y0.clone(), picks[0].clone(), api.new_workspace(size)
+        for i in range(24):
+            ad.copy_(picks[i % 4])
+            after()
+            api.lora_batch_add(x, a, b, y, cu, ad, scales, workspace=ws)
+            after()
+            ws.fill_(0xFF)
+            x.mul_(-1.0)
+            after()
+        return y
+
+    want = chain(torch.cuda.synchronize)
+    assert torch.equal(chain(lambda: None), want) and torch.isfinite(want).all() and not torch.equal(want, y0)
