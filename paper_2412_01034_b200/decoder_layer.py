@@ -49,6 +49,18 @@ class Linear4:
         return api.linear_w4a16(x, self.packed, self.scales, self.zeros, self.N, GROUP, workspace=workspace)
 
 
+def linear_workspace_size(max_tokens, linears, gate_up, linears8=()):
+    """Bytes that serve batches of 1 ... max_tokens rows through the 4-bit linears, the gated MLP and the W8A8 linears of these
+    (N, K).  Every row count is asked for: the prefill GEMM's need grows and shrinks with the tiles that the rows are cut into
+    (at 4096 x 11008, 280 rows need more than 1000 do), and with less it falls back to whole tiles on part of the GPU."""
+    size = 256
+    for M in range(1, max_tokens + 1):
+        size = max(size, api.linear_w4a16_swiglu_workspace_size(M, *gate_up, GROUP),
+                   *(api.linear_w4a16_workspace_size(M, N, K, GROUP) for N, K in linears),
+                   *(api.linear_w4a4_workspace_size(M, N, K) for N, K in linears8))
+    return size
+
+
 class DecoderLayer:
     """weights: fp32 CUDA tensors norm1, norm2 [hidden], qkv [(H + 2 Hk) D][hidden], o [hidden][H D], gate, up [ffn][hidden],
     down [hidden][ffn].  adapters: None or (a [n][r][hidden], b [n][(H + 2 Hk) D][r], scales [n]) beside the qkv projection."""
@@ -67,15 +79,10 @@ class DecoderLayer:
         self.adapters = adapters
         self.cos_sin = api.rope_table(max_pos, head_dim, theta)
         self.k_cache, self.v_cache = api.new_kv_cache(num_pages, kv_heads, page_size, head_dim)
-        # one workspace for all linears of the layer (they run one after another), sized for the largest batch
-        size = 256
-        for M in {1, 8, 9, max_tokens}:
-            for lin in (self.o, self.down, self.gate_up) + (() if qkv_bits == 8 else (self.qkv,)):
-                size = max(size, api.linear_w4a16_workspace_size(M, lin.N, lin.K, GROUP))
-            size = max(size, api.linear_w4a16_swiglu_workspace_size(M, self.gate_up.N, self.gate_up.K, GROUP))
-        if qkv_bits == 8:
-            size = max(size, api.linear_w4a4_workspace_size(max_tokens, *weights["qkv"].shape))
-        self.workspace = api.new_workspace(size)
+        # one workspace for all linears of the layer (they run one after another)
+        self.workspace = api.new_workspace(linear_workspace_size(
+            max_tokens, [(lin.N, lin.K) for lin in (self.o, self.down) + (() if qkv_bits == 8 else (self.qkv,))],
+            (self.gate_up.N, self.gate_up.K), [tuple(weights["qkv"].shape)] if qkv_bits == 8 else []))
         self.attn_workspace = None
 
     def _qkv(self, h, residual, batch):

@@ -56,3 +56,17 @@ def test_linears_and_the_gated_mlp_take_turns_on_one_workspace():
         for name in ("o", "gate_up", "odd", "down", "gate_up", "o", "down"):
             assert torch.equal(calls[M, name](ws), want[M, name]), (M, name)
     assert int(ws[:4].view(torch.int32)[0]) == 0
+
+
+@pytest.mark.parametrize("max_tokens", [1, 7, 8, 200, 300, 512, 768, 1024])
+def test_the_decoder_layers_workspace_serves_every_row_count(lib, max_tokens):
+    """No batch of up to max_tokens rows needs more than the layer has (the GEMM would take a slower way without a word)."""
+    from paper_2412_01034_b200 import decoder_layer
+    hidden, ffn, qkv = 4096, 11008, 12288
+    size = decoder_layer.linear_workspace_size(max_tokens, [(hidden, hidden), (hidden, ffn), (qkv, hidden)], (2 * ffn, hidden))
+    for M in range(1, max_tokens + 1):
+        for N, K in ((hidden, hidden), (hidden, ffn), (qkv, hidden)):
+            assert lib.qil_linear_w4a16_workspace_size(M, N, K, 128) <= size, (M, N, K)
+        assert lib.qil_linear_w4a16_swiglu_workspace_size(M, 2 * ffn, hidden, 128) <= size, M
+    with8 = decoder_layer.linear_workspace_size(max_tokens, [(hidden, hidden)], (2 * ffn, hidden), [(qkv, hidden)])
+    assert with8 >= lib.qil_linear_w4a4_workspace_size(max_tokens, qkv, hidden)
