@@ -454,10 +454,12 @@ qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, v
  *   What lies in the caches behind the tokens that a token sees, be it infinite or NaN, has no influence on it.
  *   max_q_len, max_kv_len: bounds on the requests' q_len and kv_len that the host knows.  They choose how the work is
  *   split; a request that exceeds them gets unspecified results, the others keep theirs.
- *   workspace: qil_attn_paged_workspace_size() bytes, zero-filled once; calls that share it must not overlap.  Its first
+ *   workspace: qil_attn_paged_workspace_size() bytes, the first QIL_ATTN_PAGED_ZEROED_BYTES of them zero-filled once (status
+ *   word and counters; the parts behind them need no initialisation); calls that share it must not overlap.  Its first
  *   int is a status word (QIL_ERR_TIMEOUT if a bounded device-side wait ran out; see qil_device_status).
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also a scale that is not finite, and more than 128 heads to a key head),
  *   WORKSPACE, CUDA. */
+#define QIL_ATTN_PAGED_ZEROED_BYTES 65792u
 size_t qil_attn_paged_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim,
                                      int max_q_len, int max_kv_len);
 qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const int* cu_q,

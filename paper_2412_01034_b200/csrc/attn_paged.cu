@@ -71,6 +71,7 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
 }
 
 constexpr size_t kHeader = 256;   // status word
+static_assert(kHeader + kCounters * sizeof(int) == QIL_ATTN_PAGED_ZEROED_BYTES, "what has to be zero before the first call");
 
 }  // namespace
 

@@ -81,9 +81,13 @@ qil_stream_t stream_of(const Tensor& t) {
     if (dev != c10::cuda::current_device()) throw std::invalid_argument("qil: the tensors are not on the current device");
     return reinterpret_cast<qil_stream_t>(c10::cuda::getCurrentCUDAStream(dev).stream());
 }
-// a caller's workspace, or a new zero-filled one
-Tensor workspace_of(PyObject* o, size_t bytes, const Tensor& like) {
-    if (o == Py_None) return at::zeros({(int64_t)std::max<size_t>(bytes, 16)}, like.options().dtype(c10::kByte));
+// a caller's workspace, or a new one whose first `zeroed` bytes are zero (the rest needs no initialisation)
+Tensor workspace_of(PyObject* o, size_t bytes, size_t zeroed, const Tensor& like) {
+    if (o == Py_None) {
+        const Tensor t = at::detail::empty_cuda({(int64_t)std::max<size_t>(bytes, 16)}, c10::kByte, like.device(), std::nullopt);
+        if (zeroed && bytes) t.narrow(0, 0, (int64_t)std::min(zeroed, bytes)).zero_();
+        return t;
+    }
     const Tensor& t = tensor(o, "workspace");
     if (!t.is_cuda() || !t.is_contiguous()) throw std::invalid_argument("qil: the workspace has to be a contiguous CUDA tensor");
     return t;
@@ -203,7 +207,7 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* po = arg(out, "out", c10::kBFloat16, {T, heads, c.dim});
         const size_t bytes = a[10] != Py_None ? 0 : qil_attn_paged_workspace_size(size32(T), size32(c.seqs), size32(heads), size32(c.kv_heads),
                                                                                   size32(c.dim), max_q, max_kv);
-        const Tensor ws = workspace_of(a[10], bytes, q);
+        const Tensor ws = workspace_of(a[10], bytes, QIL_ATTN_PAGED_ZEROED_BYTES, q);
         const qil_status s = qil_attn_paged(pq, c.k, c.v, po, c.cu, c.len, c.table, size32(T), size32(c.seqs), size32(heads),
                                             size32(c.kv_heads), size32(c.dim), size32(c.page), size32(c.pages), size32(c.width), max_q, max_kv,
                                             (float)scale, ws.data_ptr(), ws.nbytes(), stream_of(q));
@@ -229,7 +233,7 @@ PyObject* lora_batch_add(PyObject*, PyObject* const* p, Py_ssize_t n) {
         int* ad = static_cast<int*>(arg(adapter, "adapter", c10::kInt, {seqs}));
         float* sc = static_cast<float*>(arg(tensor(p[6], "scales"), "scales", c10::kFloat, {count}));
         const size_t bytes = p[8] != Py_None ? 0 : qil_lora_batch_workspace_size(size32(M), size32(seqs), size32(r));
-        const Tensor ws = workspace_of(p[8], bytes, x);
+        const Tensor ws = workspace_of(p[8], bytes, 0, x);
         const qil_status s = qil_lora_batch_add(px, pa, pb, py, po, cu, ad, sc, size32(M), size32(N), size32(K), size32(r), size32(seqs),
                                                 size32(count), ldx, ldy, ldo, ws.data_ptr(), ws.nbytes(), stream_of(x));
         return s != QIL_OK ? PyLong_FromLong(s) : wrap(out);

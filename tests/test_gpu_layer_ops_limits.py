@@ -107,3 +107,35 @@ def test_lora_batch_without_adapters_in_a_chain(api):  # noqa: F811
 
     want = chain(torch.cuda.synchronize)
     assert torch.equal(chain(lambda: None), want) and torch.isfinite(want).all() and not torch.equal(want, y0)
+
+
+def dirty_memory():
+    """What the allocator hands out next is full of 0xFF."""
+    torch.cuda.empty_cache()
+    for n in (1 << 8, 1 << 12, 1 << 16, 1 << 18, 1 << 20, 1 << 22, 1 << 24, 1 << 26):
+        block = [torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        del block
+
+
+def test_calls_without_a_workspace_clear_what_has_to_be_zero_and_no_more(api):  # noqa: F811
+    """In memory that others have used: the results stand, and nothing but the counters of the attention is filled."""
+    g = gen(750)
+    q_lens, kv_lens = [1] * 8 + [60], [1000 - 7 * i for i in range(8)] + [4000]
+    q, kc, vc, table, tab = attention_inputs(g, q_lens, kv_lens, 32, 32, 64, 64)
+    attn = (q, kc, vc, ints(starts(q_lens)), ints(kv_lens), table, 60, 4000)
+    M, K, N, r = 340, 2048, 1024, 64
+    x, y, a, b = draw(g, M, K), draw(g, M, N), draw(g, 1, r, K, std=K ** -0.5), draw(g, 1, N, r)
+    lora = (x, a, b, y, ints([0, M]), ints([0]), torch.ones(1, device="cuda"))
+    out = torch.empty_like(y)
+    want_l = api.lora_batch_add(*lora, out=torch.empty_like(y), workspace=api.new_workspace(api.lora_batch_workspace_size(M, 1, r)))
+    want = check_attention(api, q, kc, vc, table, tab, q_lens, kv_lens,
+                           workspace=api.new_workspace(api.attn_paged_workspace_size(sum(q_lens), 9, 32, 32, 64, 60, 4000)))
+    for _ in range(3):
+        dirty_memory()
+        assert torch.equal(api.attn_paged(*attn), want) and torch.equal(api.lora_batch_add(*lora, out=out), want_l)
+    # the fills that the calls enqueue
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA], acc_events=True) as prof:
+        api.lora_batch_add(*lora, out=out)
+        torch.cuda.synchronize()
+    names = [e.key for e in prof.key_averages()]
+    assert not [n for n in names if "fill" in n.lower() or "memset" in n.lower()], names
