@@ -63,7 +63,9 @@ def linear_workspace_size(max_tokens, linears, gate_up, linears8=()):
 
 class DecoderLayer:
     """weights: fp32 CUDA tensors norm1, norm2 [hidden], qkv [(H + 2 Hk) D][hidden], o [hidden][H D], gate, up [ffn][hidden],
-    down [hidden][ffn].  adapters: None or (a [n][r][hidden], b [n][(H + 2 Hk) D][r], scales [n]) beside the qkv projection."""
+    down [hidden][ffn].  adapters: None or (a [n][r][hidden], b [n][(H + 2 Hk) D][r], scales [n]) beside the qkv projection.
+    The caches and workspaces are the layer's own: its calls belong on one stream, or have to be ordered by the caller.
+    Steps may be captured in CUDA graphs."""
 
     def __init__(self, weights, heads, kv_heads, head_dim, num_pages, page_size, max_pos, max_tokens, qkv_bits=4, adapters=None,
                  eps=1e-5, theta=10000.0):
@@ -83,7 +85,27 @@ class DecoderLayer:
         self.workspace = api.new_workspace(linear_workspace_size(
             max_tokens, [(lin.N, lin.K) for lin in (self.o, self.down) + (() if qkv_bits == 8 else (self.qkv,))],
             (self.gate_up.N, self.gate_up.K), [tuple(weights["qkv"].shape)] if qkv_bits == 8 else []))
-        self.attn_workspace = None
+        # the adapters' need is greatest for one request with all the rows (more requests: fewer slices of K)
+        self.max_tokens = max_tokens
+        self.lora_workspace = adapters and torch.empty(
+            max(16, *(api.lora_batch_workspace_size(M, 1, adapters[0].shape[1]) for M in range(1, max_tokens + 1))), dtype=torch.uint8, device="cuda")
+        self._attn_workspaces = []
+
+    def _attn_workspace(self, tokens, requests, max_q, max_kv):
+        """The attention's workspace for such a batch: the newest one if it is large enough, or a larger one.  The older ones
+        stay (each is at least twice the one before), because a captured graph may hold them."""
+        need = api.attn_paged_workspace_size(tokens, requests, self.heads, self.kv_heads, self.head_dim, max_q, max_kv)
+        held = self._attn_workspaces[-1].numel() if self._attn_workspaces else 0
+        if held < need:
+            if torch.cuda.is_current_stream_capturing():
+                return None   # (one of the graph's own: what is cleared in a capture is only cleared when the graph runs)
+            self._attn_workspaces.append(api.new_workspace(max(need, 2 * held)))
+        return self._attn_workspaces[-1]
+
+    def reserve(self, tokens, requests, max_q, max_kv):
+        """Makes room for batches of up to this many new tokens and requests with these bounds, so that ``forward`` need not
+        (before a capture, say).  Batches that differ in shape may need more than a larger one: reserve each kind."""
+        self._attn_workspace(tokens, requests, max_q, max_kv)
 
     def _qkv(self, h, residual, batch):
         """The norm and the fused projection with the requests' adapters: (qkv, the residual stream)."""
@@ -98,7 +120,8 @@ class DecoderLayer:
             qkv = self.qkv(x, self.workspace)
         if self.adapters:
             a, b, scales = self.adapters
-            api.lora_batch_add(x, a, b, qkv, batch.cu_q, batch.adapter, scales)
+            api.lora_batch_add(x, a, b, qkv, batch.cu_q, batch.adapter, scales,
+                               workspace=self.lora_workspace if x.shape[0] <= self.max_tokens else None)
         return qkv, residual
 
     def forward(self, h, residual, batch: Requests):
@@ -106,12 +129,8 @@ class DecoderLayer:
         Returns the same pair for the next layer."""
         qkv, residual = self._qkv(h, residual, batch)
         q = api.rope_append(qkv, self.cos_sin, self.k_cache, self.v_cache, batch.cu_q, batch.kv_len, batch.block_table, self.heads)
-        need = api.attn_paged_workspace_size(q.shape[0], batch.kv_len.shape[0], self.heads, self.kv_heads, self.head_dim, batch.max_q,
-                                             batch.max_kv)
-        if self.attn_workspace is None or self.attn_workspace.numel() < need:
-            self.attn_workspace = api.new_workspace(need)
         a = api.attn_paged(q, self.k_cache, self.v_cache, batch.cu_q, batch.kv_len, batch.block_table, batch.max_q, batch.max_kv,
-                           workspace=self.attn_workspace)
+                           workspace=self._attn_workspace(q.shape[0], batch.kv_len.shape[0], batch.max_q, batch.max_kv))
         o = self.o(a.view(a.shape[0], -1), self.workspace)
         x, residual = api.rmsnorm(o, self.norm2, self.eps, residual=residual)
         g = api.linear_w4a16_swiglu(x, self.gate_up.packed, self.gate_up.scales, self.gate_up.zeros, self.gate_up.N, GROUP,
