@@ -17,6 +17,7 @@ F32, BF16, F16 = 0, 1, 2
 LAYOUT_CANONICAL, LAYOUT_TILE16, LAYOUT_STREAM128 = 0, 1, 3
 DEP_PREVIOUS = 1
 DEP_NEVER = 2
+ERR_TIMEOUT = 7
 ERR_RANGE = 8
 
 _DT = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -163,6 +164,16 @@ def linear_w4a16_workspace_size(M: int, N: int, K: int, group_size: int) -> int:
 def new_workspace(nbytes: int, device="cuda"):
     """A zero-filled workspace of at least ``nbytes`` bytes (zero-filling is required once)."""
     return torch.zeros(max(int(nbytes), 16), dtype=torch.uint8, device=device)
+
+
+def check_workspace(workspace, stream=None) -> None:
+    """Waits for the stream and raises QilError if a kernel that used the workspace has recorded a failure in its first int (a
+    bounded device-side wait that ran out, ERR_TIMEOUT: the outputs of that call are unspecified; zero-fill the workspace
+    before it is used again).  A call that makes its own workspace leaves nothing to ask."""
+    _need_cuda(workspace)
+    out = C.c_int(0)
+    _check(_lib.load().qil_device_status(_ptr(workspace), C.byref(out), _stream(stream)))
+    _check(out.value)
 
 
 def linear_w4a16(x, qweight, scales, zeros, N: int, group_size: int, layout: int = LAYOUT_CANONICAL, out=None,
@@ -413,7 +424,8 @@ def attn_paged_workspace_size(total_q: int, num_seqs: int, num_heads: int, num_k
 def attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len: int, max_kv_len: int, scale: float | None = None,
                out=None, workspace=None, stream=None):
     """Causal attention of the new tokens q [T][H][D] of all requests over the paged cache (which holds them already).
-    max_q_len, max_kv_len bound the requests' lengths; scale defaults to D ** -0.5."""
+    max_q_len, max_kv_len bound the requests' lengths; scale defaults to D ** -0.5.  With a workspace of the caller's,
+    check_workspace tells whether a device-side wait ran out."""
     return _call("attn_paged", stream, q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
 
 

@@ -107,6 +107,11 @@ class DecoderLayer:
         (before a capture, say).  Batches that differ in shape may need more than a larger one: reserve each kind."""
         self._attn_workspace(tokens, requests, max_q, max_kv)
 
+    def check(self):
+        """Waits for the current stream and raises QilError if a kernel of an earlier step has recorded a failure."""
+        for workspace in (self.workspace, *self._attn_workspaces):
+            api.check_workspace(workspace)
+
     def _qkv(self, h, residual, batch):
         """The norm and the fused projection with the requests' adapters: (qkv, the residual stream)."""
         if self.qkv_bits == 8:

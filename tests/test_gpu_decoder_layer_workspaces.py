@@ -97,3 +97,23 @@ def test_adapters_of_every_row_count_have_room(n):
     many, x = batch(normal, [n // 5] * 4 + [n - n // 5 * 4], [max(n, 1)] * 5)
     h, r = layer.forward(x, None, many)
     assert torch.isfinite(h).all()
+
+
+def test_recorded_failures_are_seen():
+    """A status word that a kernel has set (here: the test) is raised, by the function and by the layer."""
+    from paper_2412_01034_b200 import api
+    ws = api.new_workspace(1 << 10)
+    api.check_workspace(ws)
+    ws[:4].view(torch.int32).fill_(api.ERR_TIMEOUT)
+    with pytest.raises(api.QilError, match="timed out"):
+        api.check_workspace(ws)
+    layer, normal = make()
+    b, x = batch(normal, [60, 1], [900, 30])
+    layer.forward(x, None, b)
+    layer.check()
+    for held in (layer.workspace, layer._attn_workspaces[0]):
+        held[:4].view(torch.int32).fill_(api.ERR_TIMEOUT)
+        with pytest.raises(api.QilError, match="timed out"):
+            layer.check()
+        held[:4].zero_()
+        layer.check()
