@@ -11,6 +11,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
 
@@ -108,14 +109,33 @@ Tensor fresh(const Tensor& x, Sizes shape, c10::ScalarType type) {
 }
 PyObject* wrap(const Tensor& t) { return THPVariable_Wrap(t); }
 
+// every tensor among the arguments has to be on the first one's device (a kernel would take any address)
+void need_one_device(PyObject* const* args, std::initializer_list<const char*> names) {
+    const Tensor* first = nullptr;
+    const char* first_name = nullptr;
+    for (const char* name : names) {
+        PyObject* o = *args++;
+        if (!THPVariable_Check(o)) continue;
+        const Tensor& t = THPVariable_Unpack(o);
+        if (!first) {
+            first = &t;
+            first_name = name;
+        } else if (t.device() != first->device()) {
+            throw std::invalid_argument(std::string("qil: ") + name + " is on " + t.device().str() + ", " + first_name + " on " +
+                                        first->device().str());
+        }
+    }
+}
+
 // C++ exceptions end here
 template <class F>
-PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F body) {
-    if (got != want) {
-        PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, got);
+PyObject* guarded(PyObject* const* args, Py_ssize_t got, std::initializer_list<const char*> names, F body) {
+    if (got != (Py_ssize_t)names.size()) {
+        PyErr_Format(PyExc_TypeError, "expected %zu arguments, got %zd", names.size(), got);
         return nullptr;
     }
     try {
+        need_one_device(args, names);
         return body();
     } catch (const std::invalid_argument& e) {
         PyErr_SetString(PyExc_ValueError, e.what());
@@ -129,7 +149,7 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F body) {
 
 // rmsnorm(x, weight, eps, residual, out, residual_out, a8)
 PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 7, [&]() -> PyObject* {
+    return guarded(a, n, {"x", "weight", "eps", "residual", "out", "residual_out", "a8"}, [&]() -> PyObject* {
         const Tensor& x = tensor(a[0], "x", 2);
         const int64_t M = x.size(0), K = x.size(1);
         void* px = arg(x, "x", c10::kBFloat16, {M, K});
@@ -179,7 +199,7 @@ struct Paged {
 
 // rope_append(qkv, cos_sin, k_cache, v_cache, cu_q, kv_len, block_table, num_heads, out)
 PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 9, [&]() -> PyObject* {
+    return guarded(a, n, {"qkv", "cos_sin", "k_cache", "v_cache", "cu_q", "kv_len", "block_table", "num_heads", "out"}, [&]() -> PyObject* {
         const Tensor &qkv = tensor(a[0], "qkv", 2), &cs = tensor(a[1], "cos_sin", 2);
         const Paged c(a + 2);
         const int64_t heads = whole(a[7]), T = qkv.size(0);
@@ -196,7 +216,8 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
 PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 11, [&]() -> PyObject* {
+    return guarded(a, n, {"q", "k_cache", "v_cache", "cu_q", "kv_len", "block_table", "max_q_len", "max_kv_len", "scale", "out",
+                          "workspace"}, [&]() -> PyObject* {
         const Tensor& q = tensor(a[0], "q", 3);
         const Paged c(a + 1);
         const int64_t T = q.size(0), heads = q.size(1);
@@ -217,7 +238,7 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // lora_batch_add(x, a, b, y, cu_q, adapter, scales, out, workspace)
 PyObject* lora_batch_add(PyObject*, PyObject* const* p, Py_ssize_t n) {
-    return guarded(n, 9, [&]() -> PyObject* {
+    return guarded(p, n, {"x", "a", "b", "y", "cu_q", "adapter", "scales", "out", "workspace"}, [&]() -> PyObject* {
         const Tensor &x = tensor(p[0], "x", 2), &b = tensor(p[2], "b", 3), &y = tensor(p[3], "y", 2);
         const int64_t M = x.size(0), K = x.size(1), count = b.size(0), N = b.size(1), r = b.size(2);
         const Tensor& adapter = tensor(p[5], "adapter", 1);

@@ -13,3 +13,31 @@ def built():
 def test_check_workspace_refuses_what_is_no_workspace():
     with pytest.raises(ValueError):
         api.check_workspace(torch.zeros(64, dtype=torch.uint8))
+
+
+def shapes():
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    cache = dict(k_cache=bf(3, 2, 16, 64), v_cache=bf(3, 2, 16, 64), cu_q=i32(3), kv_len=i32(2), block_table=i32(2, 4))
+    return {
+        "rmsnorm": dict(x=bf(2, 8), weight=bf(8), residual=bf(2, 8), out=bf(2, 8), residual_out=bf(2, 8)),
+        "rmsnorm_a8": dict(x=bf(2, 8), weight=bf(8), residual=bf(2, 8), out=bf(2, 8), residual_out=bf(2, 8)),
+        "rope_append": dict(qkv=bf(2, 512), cos_sin=torch.zeros(4, 64), **cache, num_heads=4, out=bf(2, 4, 64)),
+        "attn_paged": dict(q=bf(2, 4, 64), **cache, max_q_len=1, max_kv_len=16, out=bf(2, 4, 64), workspace=torch.zeros(1 << 20, dtype=torch.uint8)),
+        "lora_batch_add": dict(x=bf(2, 8), a=bf(1, 8, 8), b=bf(1, 16, 8), y=bf(2, 16), cu_q=i32(2), adapter=i32(1), scales=torch.zeros(1), out=bf(2, 16),
+                               workspace=torch.zeros(1 << 10, dtype=torch.uint8)),
+    }
+
+
+@pytest.mark.parametrize("op", list(shapes()))
+def test_tensors_of_another_device_are_refused(op):
+    """Each tensor in turn is on a device that is not the first one's: refused by name, before an address is taken."""
+    args = shapes()[op]
+    first = next(iter(args))
+    for name, value in args.items():
+        if name == first or not isinstance(value, torch.Tensor):
+            continue
+        with pytest.raises(ValueError, match=f"{name} is on meta, {first} on cpu"):
+            getattr(api, op)(**dict(args, **{name: value.to("meta")}))
+    with pytest.raises(ValueError, match="CUDA"):
+        getattr(api, op)(**args)
