@@ -70,7 +70,7 @@ void* arg_rows(const Tensor& t, const char* name, int64_t rows, int64_t cols, lo
     need_type_and_shape(t, name, c10::kBFloat16, {rows, cols});
     if (!t.is_cuda() || (cols > 1 && t.stride(1) != 1))
         throw std::invalid_argument(std::string("qil: the rows of ") + name + " have to be contiguous, on a CUDA device");
-    stride = rows > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), cols);
+    stride = rows > 1 ? t.stride(0) : cols;   // (the stride of a single row says nothing)
     return t.data_ptr();
 }
 int size32(int64_t n) {

@@ -139,3 +139,22 @@ def test_calls_without_a_workspace_clear_what_has_to_be_zero_and_no_more(api):  
         torch.cuda.synchronize()
     names = [e.key for e in prof.key_averages()]
     assert not [n for n in names if "fill" in n.lower() or "memset" in n.lower()], names
+
+
+def test_lora_batch_single_rows_of_tensors_of_any_width(api):  # noqa: F811
+    """One row of a matrix whose rows are no multiple of 8 long: the stride is of no account."""
+    g = gen(760)
+    K, N = 256, 128
+    a, b, scales = draw(g, 1, 8, K, std=K ** -0.5), draw(g, 1, N, 8), torch.ones(1, device="cuda")
+    x, y = draw(g, 1, K), draw(g, 1, N)
+    want = api.lora_batch_add(x, a, b, y, ints([0, 1]), ints([0]), scales, out=torch.empty_like(y))
+    for pad in (4, 13):
+        wide_x, wide_y, wide_o = (torch.zeros(3, n + pad, dtype=torch.bfloat16, device="cuda") for n in (K, N, N))
+        wide_x[:1, :K], wide_y[:1, :N] = x, y
+        out = wide_o[:1, :N]
+        api.lora_batch_add(wide_x[:1, :K], a, b, wide_y[:1, :N], ints([0, 1]), ints([0]), scales, out=out)
+        assert torch.equal(out, want) and not wide_o[1:].any() and not wide_o[:, N:].any()
+        api.lora_batch_add(wide_x[:1, :K], a, b, wide_y[:1, :N], ints([0, 1]), ints([0]), scales)
+        assert torch.equal(wide_y[:1, :N], want) and not wide_y[1:].any() and not wide_y[:, N:].any()
+        with pytest.raises(api.QilError):
+            api.lora_batch_add(wide_x[:2, :K], a, b, draw(g, 2, N), ints([0, 2]), ints([0]), scales)
