@@ -49,7 +49,8 @@ qil_status check_paged(const PagedCache& c) {
     if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128) return QIL_ERR_UNSUPPORTED;
     // positions, rows of the cache and grid sizes are 32-bit numbers
     constexpr long long kMost = 0x7FFFFFFF;
-    if ((long long)c.max_pages * c.page_size > kMost || (long long)c.num_pages * c.num_kv_heads * c.page_size > kMost ||
+    constexpr long long kAhead = 4096;   // (tokens that the kernels may count past a request's last)
+    if ((long long)c.max_pages * c.page_size > kMost - kAhead || (long long)c.num_pages * c.num_kv_heads * c.page_size > kMost ||
         (long long)c.total_q * c.num_heads > kMost || c.num_seqs > 65534 || c.num_heads + 2LL * c.num_kv_heads > 4096)
         return QIL_ERR_SHAPE;
     return QIL_OK;
@@ -271,7 +272,7 @@ qil_status qil_lora_side_add(const void* x, const void* a, const void* b, void* 
 qil_status qil_rmsnorm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, int8_t* qy, float* scales,
                        int M, int K, float eps, qil_stream_t stream) {
     if (!x || !weight || (!y && !qy) || (qy && !scales) || (residual_out && !residual)) return QIL_ERR_NULL;
-    if (M <= 0 || K <= 0 || K % 8 != 0) return QIL_ERR_SHAPE;
+    if (M <= 0 || M > 0x7FFF0000 || K <= 0 || K % 8 != 0) return QIL_ERR_SHAPE;   // (a block counts one grid past the last row)
     if (!rmsnorm_supported(K) || !(eps >= 0.f)) return QIL_ERR_UNSUPPORTED;
     if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(residual_out) || !aligned16(y) || !aligned16(qy) ||
         !aligned4(scales))
@@ -332,7 +333,7 @@ qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const
         return QIL_ERR_SHAPE;
     if (ldx < K || ldy < N || ldo < N || ldx % 8 != 0 || ldy % 8 != 0 || ldo % 8 != 0 || (out == y && ldo != ldy)) return QIL_ERR_SHAPE;
     if (rank > 64) return QIL_ERR_UNSUPPORTED;
-    if ((N + 127) / 128 > 65535 || num_seqs > (1 << 24) || M > (1 << 30)) return QIL_ERR_SHAPE;   // (grid sizes)
+    if (N > 65535 * 128 || K > (1 << 30) || num_seqs > (1 << 24) || M > (1 << 30)) return QIL_ERR_SHAPE;   // (grid sizes, 32-bit counts)
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(y) || !aligned16(out) || !aligned16(workspace) || !aligned4(cu_q) ||
         !aligned4(adapter) || !aligned4(scales))
         return QIL_ERR_ALIGN;

@@ -63,7 +63,7 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
         long long tiles = ((long long)total_q * G + 255) / 256;
         if (tiles < here) tiles = here;
         long long s = sms / (tiles * Hk);
-        if (s > (max_kv + 511) / 512) s = (max_kv + 511) / 512;
+        if (s > (max_kv + 511LL) / 512) s = (max_kv + 511LL) / 512;
         pl.splits = s < 1 ? 1 : (int)s;
         if (pl.splits > 1) pl.many_floats = (size_t)pl.splits * total_q * H * (D + 2);
     }

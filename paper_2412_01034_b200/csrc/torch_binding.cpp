@@ -74,7 +74,7 @@ void* arg_rows(const Tensor& t, const char* name, int64_t rows, int64_t cols, lo
     return t.data_ptr();
 }
 int size32(int64_t n) {
-    if (n > 0x7FFFFFFF) throw std::invalid_argument("qil: a size exceeds 32 bits");
+    if (n > 0x7FFFFFFF || n < -0x7FFFFFFF) throw std::invalid_argument("qil: a size exceeds 32 bits");
     return (int)n;
 }
 qil_stream_t stream_of(const Tensor& t) {

@@ -41,3 +41,22 @@ def test_tensors_of_another_device_are_refused(op):
             getattr(api, op)(**dict(args, **{name: value.to("meta")}))
     with pytest.raises(ValueError, match="CUDA"):
         getattr(api, op)(**args)
+
+
+A = 0x10000   # an aligned address that is never read
+
+
+def test_sizes_near_32_bits_are_refused():
+    """Where a kernel's counts would pass 2^31 the call is refused as a bad shape (on a machine without a GPU a launch would
+    give another status)."""
+    from paper_2412_01034_b200 import _lib
+    lib, big = _lib.load(), 1 << 50
+    assert lib.qil_rmsnorm(A, None, A, None, A, None, None, 0x7FFFFFFF, 8, 1e-5, None) == 2
+    for n in (0x7FFFFFF8, 65535 * 128 + 8):
+        assert lib.qil_lora_batch_add(A, A, A, A, A, A, A, A, 4, n, 32, 8, 2, 3, 32, n, n, A, big, None) == 2
+    k = 0x7FFFFFF8
+    assert lib.qil_lora_batch_add(A, A, A, A, A, A, A, A, 4, 16, k, 8, 2, 3, k, 16, 16, A, big, None) == 2
+    sizes = (4, 2, 4, 2, 64, 128, 8, (1 << 24) - 1)
+    assert lib.qil_rope_append(*[A] * 8, *sizes, 32, None) == 2
+    assert lib.qil_attn_paged(*[A] * 7, *sizes, 4, 64, 0.1, A, big, None) == 2
+    assert lib.qil_attn_paged_workspace_size(4, 2, 4, 2, 64, 4, 0x7FFFFFFF) >= lib.qil_attn_paged_workspace_size(4, 2, 4, 2, 64, 4, 1 << 30) > 0

@@ -158,3 +158,13 @@ def test_lora_batch_single_rows_of_tensors_of_any_width(api):  # noqa: F811
         assert torch.equal(wide_y[:1, :N], want) and not wide_y[1:].any() and not wide_y[:, N:].any()
         with pytest.raises(api.QilError):
             api.lora_batch_add(wide_x[:2, :K], a, b, draw(g, 2, N), ints([0, 2]), ints([0]), scales)
+
+
+def test_attn_paged_bounds_are_not_cut_to_32_bits(api):  # noqa: F811
+    q, kc, vc, table, _ = attention_inputs(gen(770), [1], [20], 4, 4, 64, 16)
+    for max_q, max_kv in ((1 - 2 ** 32, 20), (1 + 2 ** 32, 20), (1, 20 - 2 ** 32), (1, 20 + 2 ** 32)):
+        with pytest.raises(ValueError, match="32 bits"):
+            api.attn_paged(q, kc, vc, ints([0, 1]), ints([20]), table, max_q, max_kv)
+    for max_q, max_kv in ((-1, 20), (0, 20), (1, 0)):
+        with pytest.raises(api.QilError):
+            api.attn_paged(q, kc, vc, ints([0, 1]), ints([20]), table, max_q, max_kv, workspace=api.new_workspace(1 << 20))
