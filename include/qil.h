@@ -473,6 +473,8 @@ qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cach
  *   a [num_adapters][rank][K]   b [num_adapters][N][rank]   scales [num_adapters] fp32   adapter [num_seqs] int32
  *   A request whose adapter is not in [0, num_adapters) has none: out = y.
  *   The inner product is fp32 in the workspace and enters the second product with 16 significant bits.
+ *   An element of A or B that is infinite or NaN leaves the outputs that it enters infinite or NaN, which of the two is
+ *   unspecified.
  *   K, N, rank and the strides multiples of 8, rank <= 64 (UNSUPPORTED above; pad smaller ranks with zeros).
  *   workspace: qil_lora_batch_workspace_size() bytes, no initialisation needed.
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA. */

@@ -47,6 +47,16 @@ __device__ __forceinline__ uint4 lds16(uint32_t addr) {
     return v;
 }
 
+// Two values as sums of two bf16 terms each.  What is finite stays so (a value beyond bf16's largest has that as its first
+// term), and an infinity has no second term: inf - inf would make the product NaN.
+__device__ __forceinline__ void split2(float2 v, uint32_t& hi, uint32_t& lo) {
+    constexpr float kMost = 3.3895313892515355e38f;   // (2 - 2^-7) 2^127
+    const auto first = [](float x) { return fabsf(x) > kMost && fabsf(x) < INFINITY ? copysignf(kMost, x) : x; };
+    const auto rest = [](float x, float h) { return fabsf(x) == INFINITY ? 0.f : x - h; };
+    hi = pack2(first(v.x), first(v.y));
+    lo = pack2(rest(v.x, __uint_as_float(hi << 16)), rest(v.y, __uint_as_float(hi & 0xFFFF0000u)));
+}
+
 // kMT: row tiles of 16 per block; kNR: column tiles of 8 of the rank (the rank padded up to 8, 16, 32 or 64)
 template <int kMT, int kNR>
 __global__ void __launch_bounds__(32 * kDownWarps) lora_batch_down_kernel(const LoraParams p) {
@@ -219,8 +229,8 @@ __global__ void __launch_bounds__(32 * kUpWarps, kUpBlocks) lora_batch_up_kernel
             }
             v.x = j < p.rank ? v.x * scale : 0.f;
             v.y = j < p.rank ? v.y * scale : 0.f;
-            const uint32_t hi = pack2(v.x, v.y);
-            const uint32_t lo = pack2(v.x - __uint_as_float(hi << 16), v.y - __uint_as_float(hi & 0xFFFF0000u));
+            uint32_t hi, lo;
+            split2(v, hi, lo);
             const int at = j % kW, step = at >> 2, reg = ((m & 15) >> 3) + 2 * ((at & 3) >> 1);
             uint32_t* f = frag + ((((m >> 4) * kSteps + step) * 2) * 32 + (m & 7) * 4 + j / kW) * 4 + reg;
             f[0] = hi;
@@ -380,8 +390,8 @@ __global__ void __launch_bounds__(32 * kFusedWarps) __cluster_dims__(kCluster, 1
         }
         v.x = j < p.rank ? v.x * scale : 0.f;
         v.y = j < p.rank ? v.y * scale : 0.f;
-        const uint32_t hi = pack2(v.x, v.y);
-        const uint32_t lo = pack2(v.x - __uint_as_float(hi << 16), v.y - __uint_as_float(hi & 0xFFFF0000u));
+        uint32_t hi, lo;
+        split2(v, hi, lo);
         const int at = j % kW, step = at >> 2, reg = (m >> 3) + 2 * ((at & 3) >> 1);
         uint32_t* f = frag + (step * 2 * 32 + (m & 7) * 4 + j / kW) * 4 + reg;
         f[0] = hi;

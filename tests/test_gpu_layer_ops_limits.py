@@ -168,3 +168,28 @@ def test_attn_paged_bounds_are_not_cut_to_32_bits(api):  # noqa: F811
     for max_q, max_kv in ((-1, 20), (0, 20), (1, 0)):
         with pytest.raises(api.QilError):
             api.attn_paged(q, kc, vc, ints([0, 1]), ints([20]), table, max_q, max_kv, workspace=api.new_workspace(1 << 20))
+
+
+@pytest.mark.parametrize("q_lens", [[1, 3, 2], [40, 100, 33]])
+@pytest.mark.parametrize("r", [8, 16, 24, 32, 64])
+def test_lora_batch_inner_products_beyond_bf16(api, q_lens, r):  # noqa: F811
+    """Inner products that are infinite, or finite and larger than bf16's largest number, enter the second product as such."""
+    g = gen(780 + r)
+    K, N, M, cu = 264, 72, sum(q_lens), starts(q_lens)
+    x, y = draw(g, M, K), draw(g, M, N)
+    a, b = draw(g, 1, r, K, std=K ** -0.5), draw(g, 1, N, r).abs() * 2.0 ** -70
+    a[0, :, 5], a[0, :, 77] = 3.38953139e38, 1e36
+    x[:, 5] = x[:, 77] = 0
+    big, inf = cu[1], cu[2] - 1
+    x[big] = 0
+    x[big, 5] = x[big, 77] = 1.0      # 3.3995e38: fp32 holds it, bf16 rounds it to infinity
+    x[inf, 100] = float("inf")
+    a[0, :, 100] = 0.5
+    out = api.lora_batch_add(x, a, b, y, ints(cu), ints([0] * len(q_lens)), torch.ones(1, device="cuda"), out=torch.empty_like(y))
+    t = f64(x[big:big + 1]) @ f64(a[0]).T
+    assert (t > 3.3896e38).all() and (t < 3.4028e38).all()
+    want = f64(y[big:big + 1]) + t @ f64(b[0]).T
+    got = f64(out)
+    assert np.all(np.abs(got[big] - want) <= (2.0 ** -8 + (K + 2 * r + 8) * 2.0 ** -24 + 2.0 ** -16) * np.abs(want))
+    assert np.all(got[inf] == np.inf)
+    assert np.all(np.isfinite(np.delete(got, inf, axis=0)))
