@@ -415,6 +415,8 @@ qil_status qil_linear_int_batch(const qil_igemm_desc* descs /*host*/, int count,
  *     h = x + residual (h = x if residual is null);  residual_out = bf16(h)
  *     v = h / sqrt(sum_k h_k^2 / K + eps) * weight
  *     y = bf16(v);  s = max |v| / 127 (0 -> 1), qy = clamp(rint(v / s), -128, 127)
+ *   A row with max |h weight| <= 2^-119 (1.5e-36) counts as zeros in s and qy; where max |v| is below 127 * 2^-126 but
+ *   max |h weight| is not (rows of 1e9 and more on weights of 1e-36 and less), qy is unspecified.
  *   The norm is taken of the fp32 sum, not of residual_out.  qy and scales are
  *   the operands of qil_linear_w8a8; a code may differ by one from the formula's
  *   where v / s is within fp32 rounding of a half.

@@ -193,3 +193,40 @@ def test_lora_batch_inner_products_beyond_bf16(api, q_lens, r):  # noqa: F811
     assert np.all(np.abs(got[big] - want) <= (2.0 ** -8 + (K + 2 * r + 8) * 2.0 ** -24 + 2.0 ** -16) * np.abs(want))
     assert np.all(got[inf] == np.inf)
     assert np.all(np.isfinite(np.delete(got, inf, axis=0)))
+
+
+@pytest.mark.parametrize("K", [64, 4096, 20000])
+@pytest.mark.parametrize("x_std,w_std,eps", [(1e-35, 1.0, 1e-5), (2e-37, 1.0, 1e-5), (1e-37, 1.0, 1e-5), (1e-36, 1e-2, 1e-5), (1.0, 1e-35, 1e-5), (1e-18, 1e-20, 1e-6),
+                                             (1e-17, 3e-18, 1e-6)])
+@pytest.mark.parametrize("with_residual", [False, True])
+def test_rmsnorm_codes_of_tiny_rows(api, K, x_std, w_std, eps, with_residual):  # noqa: F811
+    """Rows near the end of fp32's range: their codes are those of the formula, or, below the stated limit, those of zeros.  (The
+    sum x + residual and the product with the weight round to fp32, 2^-23 of the largest, or to multiples of 2^-149.)"""
+    from oracle import np_layer
+    g = gen(790 + K)
+    x, w = draw(g, 9, K, std=x_std), draw(g, K, std=w_std)
+    r = draw(g, 9, K, std=x_std) if with_residual else None
+    v, h = np_layer.rmsnorm(f64(x), f64(w), eps, None if r is None else f64(r))
+    top = np.abs(h * f64(w)).max(axis=1)
+    both = torch.empty_like(x)
+    codes, scales, *_ = api.rmsnorm_a8(x, w, eps, residual=r, out=both)
+    s, got, codes = np_layer.a8_scale(v), f64(scales), f64(codes)
+    zero, full = top < 2.0 ** -119 * (1 - 2.0 ** -20), top > 2.0 ** -119 * (1 + 2.0 ** -20)
+    assert not codes[zero].any() and np.all(got[zero] == 1)
+    assert np.all(np.abs(got - s)[full] <= 2.0 ** -17 * s[full])
+    assert np.all(np.abs(codes - v / s[:, None])[full] <= 0.5 + 127 * (2.0 ** -16 + 2.0 ** -149 / top[full, None]))
+    assert np.all(np.abs(f64(both) - v) <= (2.0 ** -8 + 2.0 ** -16) * np.abs(v) + 2.0 ** -134)
+
+
+@pytest.mark.parametrize("K", [64, 4096, 20000])
+def test_rmsnorm_nan_rows_have_nan_scales(api, K):  # noqa: F811
+    """A NaN anywhere in a row, or everywhere, shows in the row's scale and norm; the other rows are as without it."""
+    g = gen(800 + K)
+    x, w = draw(g, 4, K), draw(g, K)
+    _, want = api.rmsnorm_a8(x, w)
+    y = api.rmsnorm(x, w)
+    x[1], x[3, K // 2] = float("nan"), float("nan")
+    both = torch.empty_like(x)
+    _, scales = api.rmsnorm_a8(x, w, out=both)
+    assert torch.isnan(scales[[1, 3]]).all() and torch.equal(scales[[0, 2]], want[[0, 2]])
+    assert torch.isnan(both[[1, 3]]).all() and torch.equal(both[[0, 2]], y[[0, 2]])
