@@ -50,11 +50,11 @@ class Linear4:
 
 
 def linear_workspace_size(max_tokens, linears, gate_up, linears8=()):
-    """Bytes that serve batches of 1 ... max_tokens rows through the 4-bit linears, the gated MLP and the W8A8 linears of these
+    """Bytes that serve batches of 1 ... max_tokens rows (and of up to 9) through the 4-bit linears, the gated MLP and the W8A8 linears of these
     (N, K).  Every row count is asked for: the prefill GEMM's need grows and shrinks with the tiles that the rows are cut into
     (at 4096 x 11008, 280 rows need more than 1000 do), and with less it falls back to whole tiles on part of the GPU."""
     size = 256
-    for M in range(1, max_tokens + 1):
+    for M in range(1, max(max_tokens, 9) + 1):   # (more rows than max_tokens run too, but the gated MLP's scratch has to be there)
         size = max(size, api.linear_w4a16_swiglu_workspace_size(M, *gate_up, GROUP),
                    *(api.linear_w4a16_workspace_size(M, N, K, GROUP) for N, K in linears),
                    *(api.linear_w4a4_workspace_size(M, N, K) for N, K in linears8))

@@ -7,14 +7,14 @@ pytestmark = pytest.mark.gpu
 HIDDEN, HEADS, DIM, FFN, PAGE, WIDTH = 512, 8, 64, 768, 16, 72
 
 
-def make(adapters=True):
+def make(adapters=True, max_tokens=256):
     from paper_2412_01034_b200.decoder_layer import DecoderLayer
     g = torch.Generator(device="cuda").manual_seed(3)
     normal = lambda std, *s: torch.randn(s, generator=g, device="cuda") * std  # noqa: E731
     w = {"norm1": 1 + normal(0.1, HIDDEN), "norm2": 1 + normal(0.1, HIDDEN), "qkv": normal(0.04, 3 * HEADS * DIM, HIDDEN),
          "o": normal(0.04, HIDDEN, HEADS * DIM), "gate": normal(0.04, FFN, HIDDEN), "up": normal(0.04, FFN, HIDDEN), "down": normal(0.04, HIDDEN, FFN)}
     ad = (normal(HIDDEN ** -0.5, 3, 8, HIDDEN).bfloat16(), normal(0.3, 3, 3 * HEADS * DIM, 8).bfloat16(), torch.tensor([0.5, 1.0, -0.7], device="cuda"))
-    layer = DecoderLayer(w, HEADS, HEADS, DIM, num_pages=40 * WIDTH, page_size=PAGE, max_pos=1152, max_tokens=256, adapters=ad if adapters else None)
+    layer = DecoderLayer(w, HEADS, HEADS, DIM, num_pages=40 * WIDTH, page_size=PAGE, max_pos=1152, max_tokens=max_tokens, adapters=ad if adapters else None)
     for c in (layer.k_cache, layer.v_cache):
         c.normal_(generator=g)
     return layer, normal
@@ -117,3 +117,14 @@ def test_recorded_failures_are_seen():
             layer.check()
         held[:4].zero_()
         layer.check()
+
+
+def test_more_rows_than_the_layer_was_made_for():
+    """A layer for one row takes batches of 2 to 40: as a layer with room for them, up to the order of the GEMMs' sums."""
+    small, normal = make(max_tokens=1)
+    large, _ = make(max_tokens=256)
+    for n in (2, 7, 8, 9, 40):
+        b, x = batch(normal, [n], [n])
+        got, want = both(small.forward(x, None, b)), both(large.forward(x, None, b))
+        assert float((got.float() - want.float()).abs().max()) <= 2.0 ** -5 * float(want.float().abs().max()), n
+    small.check()

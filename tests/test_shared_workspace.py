@@ -70,3 +70,13 @@ def test_the_decoder_layers_workspace_serves_every_row_count(lib, max_tokens):
         assert lib.qil_linear_w4a16_swiglu_workspace_size(M, 2 * ffn, hidden, 128) <= size, M
     with8 = decoder_layer.linear_workspace_size(max_tokens, [(hidden, hidden)], (2 * ffn, hidden), [(qkv, hidden)])
     assert with8 >= lib.qil_linear_w4a4_workspace_size(max_tokens, qkv, hidden)
+
+
+@pytest.mark.parametrize("max_tokens", [1, 2, 5])
+def test_layers_made_for_a_few_rows_take_what_the_unfused_gated_mlp_takes(lib, max_tokens):
+    """The row counts of the unfused form (up to 8) always have room for its scratch, which is a must; the GEMM above has a way
+    without its parts."""
+    from paper_2412_01034_b200 import decoder_layer
+    size = decoder_layer.linear_workspace_size(max_tokens, [(4096, 4096), (4096, 11008), (12288, 4096)], (22016, 4096))
+    for M in range(1, 10):
+        assert lib.qil_linear_w4a16_swiglu_workspace_size(M, 22016, 4096, 128) <= size, M
