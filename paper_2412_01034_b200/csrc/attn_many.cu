@@ -13,6 +13,9 @@
 // The maximum that the weights refer to is only raised when a row's score exceeds it by more than 2^8; the sums stay
 // far from fp32's limits and bf16 rounds relatively, so nothing is lost, and O_i is rescaled (by the group itself, between
 // products) a few times instead of once per tile.
+// The weights are bf16 because V is (a product's operands have one type); a second term for their lower bits would add half
+// of the products' time to a kernel that waits for them.  Outputs are off by 0.0019 to 0.0023 of their size, 0.0017 of which
+// are their own rounding.
 // One warp copies pages with bulk tensor copies (128-byte swizzle), one thread issues the products, one warp clears what
 // lies behind a request's last token in its last tile of V (a weight of zero times NaN would be NaN).
 // A row of a new token that comes before one whose value is infinite or NaN meets that value all the same: rows whose results

@@ -7,8 +7,9 @@
 //   2. out = y + scale t B^T, one pass over y.
 // Rows are cut into tiles per request, so that a tile has one adapter.  The products run on mma.sync (16 x 8 x 16): with a
 // rank of 8 to 64 against two streams of K or N elements per row, a multiply costs nothing next to its operands' bytes.
-// Both kernels take their operands straight from global memory in 16-byte loads and never stage them: the order of a
-// contraction's terms is free, so lane c of four takes 8 neighbouring elements and both operands use the same order; and
+// A lane fetches its own operands in 16-byte pieces and no other lane reads them, so that nothing is rearranged (single tokens:
+// into registers; prompts: through a ring of the lane's own pieces in shared memory, which holds more in flight).  The order
+// of a contraction's terms is free: lane c of four takes 8 neighbouring elements and both operands use the same order; and
 // the columns of a group of four 16 x 8 results are dealt out so that a lane ends up with 8 neighbouring outputs.
 // Measured: 32 single tokens, 12 adapters of rank 16, 4096 x 4096: 6.0 us (7.5 cold), a chain of five trips to memory (request, adapter,
 // operands, the cluster's parts, outputs).  4000 rows in nine prompts, rank 32, 4096 -> 11008: 12 + 33 us, against 34 us for

@@ -123,7 +123,8 @@ qil_status launch_rmsnorm(const void* x, const void* residual, const void* weigh
     const int threads = ((nvec + vec - 1) / vec + 31) / 32 * 32;
     // One round of blocks, which take the rows in turn (64 registers a thread: 1024 threads per SM).  8192 rows of 4096 with
     // residual and int8 output: 41.3 us = 5.7 TB/s, 87 % of the copy rate (one vector a thread took 2 us more, one block per
-    // row 12 us more); a single row 2.9 us.
+    // row 12 us more); a single row 2.9 us.  Rows of more than 16384 take four vectors a thread, whose registers spill (72 to 76
+    // bytes a thread, and no next row on the way): 1024 rows of 32768 49 us = 4.8 TB/s.
     const long long room = (long long)num_sms() * (threads < 1024 ? 1024 / threads : 1);
     const unsigned grid = (unsigned)(M < room ? M : room);
     auto go = [&](auto kernel) {

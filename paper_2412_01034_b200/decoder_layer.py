@@ -50,9 +50,10 @@ class Linear4:
 
 
 def linear_workspace_size(max_tokens, linears, gate_up, linears8=()):
-    """Bytes that serve batches of 1 ... max_tokens rows (and of up to 9) through the 4-bit linears, the gated MLP and the W8A8 linears of these
-    (N, K).  Every row count is asked for: the prefill GEMM's need grows and shrinks with the tiles that the rows are cut into
-    (at 4096 x 11008, 280 rows need more than 1000 do), and with less it falls back to whole tiles on part of the GPU."""
+    """Bytes that serve batches of 1 ... max_tokens rows (and of up to 9) through the 4-bit linears, the gated MLP and the W8A8
+    linears of these (N, K).  Every row count is asked for: the prefill GEMM's need grows and shrinks with the tiles that the rows
+    are cut into (at 4096 x 11008, 280 rows need more than 1000 do), and with less it falls back to whole tiles on part of the
+    GPU."""
     size = 256
     for M in range(1, max(max_tokens, 9) + 1):   # (more rows than max_tokens run too, but the gated MLP's scratch has to be there)
         size = max(size, api.linear_w4a16_swiglu_workspace_size(M, *gate_up, GROUP),
@@ -87,8 +88,10 @@ class DecoderLayer:
             (self.gate_up.N, self.gate_up.K), [tuple(weights["qkv"].shape)] if qkv_bits == 8 else []))
         # the adapters' need is greatest for one request with all the rows (more requests: fewer slices of K)
         self.max_tokens = max_tokens
-        self.lora_workspace = adapters and torch.empty(
-            max(16, *(api.lora_batch_workspace_size(M, 1, adapters[0].shape[1]) for M in range(1, max_tokens + 1))), dtype=torch.uint8, device="cuda")
+        self.lora_workspace = None
+        if adapters:
+            need = max(api.lora_batch_workspace_size(M, 1, adapters[0].shape[1]) for M in range(1, max_tokens + 1))
+            self.lora_workspace = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
         self._attn_workspaces = []
 
     def _attn_workspace(self, tokens, requests, max_q, max_kv):
