@@ -474,6 +474,52 @@ qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cach
                           int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages, int max_q_len,
                           int max_kv_len, float scale, void* workspace, size_t workspace_bytes, qil_stream_t stream);
 
+/* The quantised paged cache: keys and values in 8 or 4 bits, quantised round-to-nearest as they are written (Sec. 2.1; the
+ * paper quantises the backbone's linears, the cache is this library's use of the same quantiser), with one scale per token and
+ * key head.  Pages, tables, lengths and limits are those of the bf16 cache above.
+ *   bits 8: codes  [num_pages][num_kv_heads][page_size][head_dim] int8
+ *           scales [num_pages][num_kv_heads][page_size] bf16
+ *           a = max |v|; s = bf16_rn(a / 127); q = clamp(rint(v / s), -128, 127); a code stands for q s
+ *   bits 4: codes  [num_pages][num_kv_heads][page_size][head_dim / 8] uint32, packed like qil_pack_w4's canonical words
+ *           scales [num_pages][num_kv_heads][page_size][2] bf16: scale and zero point
+ *           lo = min(0, min v), hi = max(0, max v); s = bf16_rn((hi - lo) / 15); z = clamp(rint(-lo / s), 0, 15);
+ *           q = clamp(rint(v / s) + z, 0, 15); a code stands for (q - z) s
+ *   over the head_dim values v of a token's head, with fp32 operations rounded one by one (divisions IEEE, rint to even).
+ *   A head with s < 2^-126 counts as zeros (s = 1).  Where a value is not finite, or s is not, s = NaN and all codes are zero:
+ *   the head reads as NaN.  (A head within 2^-7 of bf16's largest number may read as infinite.)
+ *
+ * qil_rope_append_q: qil_rope_append into such a cache.  Keys are quantised as they leave the rotation in fp32: two products
+ *   and a sum, each rounded (so do the queries, whose fp32 results are then rounded to bf16).
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED (also bits), CUDA. */
+qil_status qil_rope_append_q(const void* qkv, const float* cos_sin, void* q_out, void* k_codes, void* v_codes, void* k_scales,
+                             void* v_scales, int bits, const int* cu_q, const int* kv_len, const int* block_table, int total_q,
+                             int num_seqs, int num_heads, int num_kv_heads, int head_dim, int page_size, int num_pages,
+                             int max_pages, int max_pos, qil_stream_t stream);
+
+/* qil_kv_read_q: the last cached tokens of every request as bf16 rows, bf16_rn of what the codes stand for: rows cu[b] ...
+ *   cu[b + 1] - 1 of k_out and v_out [total_rows][num_kv_heads][head_dim] are the tokens that end at kv_len[b] (with cu[b + 1] -
+ *   cu[b] = kv_len[b], all of them; with the new tokens' cu, what an append has just written).  Rows whose token or page does
+ *   not exist are zeros, rows of no request stay as they are.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, CUDA. */
+qil_status qil_kv_read_q(const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales, int bits,
+                         void* k_out, void* v_out, const int* cu, const int* kv_len, const int* block_table, int total_rows,
+                         int num_seqs, int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages,
+                         qil_stream_t stream);
+
+/* qil_attn_paged_q: qil_attn_paged over such a cache (arguments, bounds and workspace as there, with a size of its own; the
+ *   two may take turns on one workspace that is large enough for either).  Of a request with at most 16 query rows (new tokens x
+ *   query heads of a key head) scores and sums take the codes exactly and round a weight times its value's scale to bf16 (2^-9 of
+ *   it); of one with more the values (q - z) s are rounded to bf16 as qil_kv_read_q gives them, and the weights to bf16.
+ *   A head that reads as NaN makes the results of the tokens that see it NaN and has no influence on others.
+ * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA. */
+size_t qil_attn_paged_q_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int bits,
+                                       int max_q_len, int max_kv_len);
+qil_status qil_attn_paged_q(const void* q, const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales,
+                            int bits, void* out, const int* cu_q, const int* kv_len, const int* block_table, int total_q,
+                            int num_seqs, int num_heads, int num_kv_heads, int head_dim, int page_size, int num_pages,
+                            int max_pages, int max_q_len, int max_kv_len, float scale, void* workspace, size_t workspace_bytes,
+                            qil_stream_t stream);
+
 /* qil_lora_batch_add: the low-rank side path (qil_lora_side_add) for a batch whose requests bring their own adapters:
  *     out[m][n] = bf16( y[m][n] + scales[a] sum_j (sum_k x[m][k] A[a][j][k]) B[a][n][j] ),  a = adapter[request of row m]
  *   x [M][K] with row stride ldx   y, out [M][N] with row strides ldy, ldo (out may be y itself, with the same stride)

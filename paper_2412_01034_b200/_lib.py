@@ -24,6 +24,10 @@ SIGNATURES = {
     "qil_rope_append": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _i, _vp]),
     "qil_attn_paged_workspace_size": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
     "qil_attn_paged": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i, C.c_float, _vp, _sz, _vp]),
+    "qil_rope_append_q": (_i, [_vp] * 7 + [_i] + [_vp] * 3 + [_i] * 9 + [_vp]),
+    "qil_kv_read_q": (_i, [_vp] * 4 + [_i] + [_vp] * 5 + [_i] * 7 + [_vp]),
+    "qil_attn_paged_q_workspace_size": (_sz, [_i] * 8),
+    "qil_attn_paged_q": (_i, [_vp] * 5 + [_i] + [_vp] * 4 + [_i] * 10 + [C.c_float, _vp, _sz, _vp]),
     "qil_lora_batch_workspace_size": (_sz, [_i, _i, _i]),
     "qil_lora_batch_add": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, C.c_longlong, C.c_longlong,
                                 C.c_longlong, _vp, _sz, _vp]),

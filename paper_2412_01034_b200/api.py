@@ -7,6 +7,7 @@ turned into an exception.  All arithmetic runs in the CUDA kernels.
 from __future__ import annotations
 
 import ctypes as C
+from typing import NamedTuple
 
 import torch
 
@@ -427,6 +428,53 @@ def attn_paged(q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len: int, m
     max_q_len, max_kv_len bound the requests' lengths; scale defaults to D ** -0.5.  With a workspace of the caller's,
     check_workspace tells whether a device-side wait ran out."""
     return _call("attn_paged", stream, q, k_cache, v_cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
+
+
+class QuantCache(NamedTuple):
+    """A paged cache in 8 bits (k, v int8 [pages][Hk][page][D], scales bf16 [pages][Hk][page]) or 4 bits (k, v int32 words
+    [pages][Hk][page][D / 8], packed like pack_w4's; scales [pages][Hk][page][2]: scale and zero point)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @property
+    def bits(self) -> int:
+        return 8 if self.k.dtype == torch.int8 else 4
+
+
+def new_kv_cache_q(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, bits: int = 8, device="cuda") -> QuantCache:
+    """An empty quantised cache (all zeros)."""
+    if bits not in (4, 8):
+        _check(4)
+    shape = (num_pages, num_kv_heads, page_size)
+    codes = [torch.zeros(shape + ((head_dim,) if bits == 8 else (head_dim // 8,)), dtype=torch.int8 if bits == 8 else torch.int32, device=device)
+             for _ in range(2)]
+    scales = [torch.zeros(shape + (() if bits == 8 else (2,)), dtype=torch.bfloat16, device=device) for _ in range(2)]
+    return QuantCache(*codes, *scales)
+
+
+def rope_append_q(qkv, cos_sin, cache: QuantCache, cu_q, kv_len, block_table, num_heads: int, out=None, stream=None):
+    """rope_append into a quantised cache: keys (turned, fp32) and values are quantised as they are written.  Returns the rotated
+    queries [T][H][D] in bf16; the cache is updated."""
+    return _call("rope_append_q", stream, qkv, cos_sin, *cache, cu_q, kv_len, block_table, num_heads, out)
+
+
+def kv_read_q(cache: QuantCache, cu, kv_len, block_table, total_rows: int, out=(None, None), stream=None):
+    """The last cu[b + 1] - cu[b] cached tokens of every request b (its kv_len[b]-th is the last) as bf16 rows: (k, v), each
+    [total_rows][Hk][D]; out: a pair of tensors to write to."""
+    return _call("kv_read_q", stream, *cache, cu, kv_len, block_table, total_rows, *out)
+
+
+def attn_paged_q_workspace_size(total_q: int, num_seqs: int, num_heads: int, num_kv_heads: int, head_dim: int, bits: int, max_q_len: int,
+                                max_kv_len: int) -> int:
+    return int(_lib.load().qil_attn_paged_q_workspace_size(total_q, num_seqs, num_heads, num_kv_heads, head_dim, bits, max_q_len, max_kv_len))
+
+
+def attn_paged_q(q, cache: QuantCache, cu_q, kv_len, block_table, max_q_len: int, max_kv_len: int, scale: float | None = None, out=None,
+                 workspace=None, stream=None):
+    """attn_paged over a quantised cache: the codes are read as they are, once per key head."""
+    return _call("attn_paged_q", stream, q, *cache, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
 
 
 def lora_batch_workspace_size(M: int, num_seqs: int, rank: int) -> int:

@@ -3,6 +3,7 @@
 
 #include <cmath>
 
+#include "kv_quant.cuh"
 #include "layer_common.cuh"
 
 namespace qil {
@@ -56,6 +57,21 @@ qil_status check_paged(const PagedCache& c) {
     return QIL_OK;
 }
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+QuantCache quant_cache(const void* k, const void* v, const void* ks, const void* vs, int bits) {
+    return {const_cast<void*>(k), const_cast<void*>(v), static_cast<__nv_bfloat16*>(const_cast<void*>(ks)),
+            static_cast<__nv_bfloat16*>(const_cast<void*>(vs)), bits};
+}
+// a quantised cache and the packed requests that use it
+qil_status check_quant(const QuantCache& kv, const PagedCache& c) {
+    if (!kv.k || !kv.v || !kv.ks || !kv.vs || !c.cu_q || !c.kv_len || !c.block_table) return QIL_ERR_NULL;
+    const qil_status s = check_paged(c);
+    if (s != QIL_OK) return s;
+    if (kv.bits != 4 && kv.bits != 8) return QIL_ERR_UNSUPPORTED;
+    if (!aligned16(kv.k) || !aligned16(kv.v) || !aligned16(kv.ks) || !aligned16(kv.vs) || !aligned4(c.cu_q) || !aligned4(c.kv_len) ||
+        !aligned4(c.block_table))
+        return QIL_ERR_ALIGN;
+    return QIL_OK;
+}
 inline bool pack_layout_ok(int l) { return l == QIL_LAYOUT_CANONICAL || l == QIL_LAYOUT_TILE16; }
 }  // namespace
 
@@ -318,6 +334,58 @@ qil_status qil_attn_paged(const void* q, const void* k_cache, const void* v_cach
     if (!workspace || workspace_bytes < attn_paged_workspace(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len))
         return QIL_ERR_WORKSPACE;
     return launch_attn_paged(q, k_cache, v_cache, out, c, max_q_len, max_kv_len, scale, workspace, S(stream));
+}
+
+qil_status qil_rope_append_q(const void* qkv, const float* cos_sin, void* q_out, void* k_codes, void* v_codes, void* k_scales,
+                             void* v_scales, int bits, const int* cu_q, const int* kv_len, const int* block_table, int total_q,
+                             int num_seqs, int num_heads, int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages,
+                             int max_pos, qil_stream_t stream) {
+    if (!qkv || !cos_sin || !q_out) return QIL_ERR_NULL;
+    const PagedCache c = {cu_q, kv_len, block_table, total_q, num_seqs, num_heads, num_kv_heads, head_dim, page_size, num_pages, max_pages};
+    const QuantCache kv = quant_cache(k_codes, v_codes, k_scales, v_scales, bits);
+    const qil_status s = check_quant(kv, c);
+    if (s != QIL_OK) return s;
+    if (max_pos <= 0) return QIL_ERR_SHAPE;
+    if (!aligned16(qkv) || !aligned16(cos_sin) || !aligned16(q_out)) return QIL_ERR_ALIGN;
+    return launch_rope_append_q(qkv, cos_sin, q_out, kv, c, max_pos, S(stream));
+}
+
+qil_status qil_kv_read_q(const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales, int bits, void* k_out,
+                         void* v_out, const int* cu, const int* kv_len, const int* block_table, int total_rows, int num_seqs,
+                         int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages, qil_stream_t stream) {
+    if (!k_out || !v_out) return QIL_ERR_NULL;
+    const PagedCache c = {cu, kv_len, block_table, total_rows, num_seqs, num_kv_heads, num_kv_heads, head_dim, page_size, num_pages, max_pages};
+    const QuantCache kv = quant_cache(k_codes, v_codes, k_scales, v_scales, bits);
+    const qil_status s = check_quant(kv, c);
+    if (s != QIL_OK) return s;
+    if (!aligned16(k_out) || !aligned16(v_out)) return QIL_ERR_ALIGN;
+    return launch_kv_read_q(kv, c, k_out, v_out, S(stream));
+}
+
+size_t qil_attn_paged_q_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int bits, int max_q_len,
+                                       int max_kv_len) {
+    if (total_q <= 0 || num_seqs <= 0 || num_heads <= 0 || num_kv_heads <= 0 || num_heads % num_kv_heads != 0 || head_dim <= 0 ||
+        (bits != 4 && bits != 8) || max_q_len <= 0 || max_kv_len <= 0)
+        return 0;
+    return attn_paged_q_workspace(total_q, num_seqs, num_heads, num_kv_heads, head_dim, bits, max_q_len, max_kv_len);
+}
+
+qil_status qil_attn_paged_q(const void* q, const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales, int bits,
+                            void* out, const int* cu_q, const int* kv_len, const int* block_table, int total_q, int num_seqs, int num_heads,
+                            int num_kv_heads, int head_dim, int page_size, int num_pages, int max_pages, int max_q_len, int max_kv_len,
+                            float scale, void* workspace, size_t workspace_bytes, qil_stream_t stream) {
+    if (!q || !out) return QIL_ERR_NULL;
+    const PagedCache c = {cu_q, kv_len, block_table, total_q, num_seqs, num_heads, num_kv_heads, head_dim, page_size, num_pages, max_pages};
+    const QuantCache kv = quant_cache(k_codes, v_codes, k_scales, v_scales, bits);
+    const qil_status s = check_quant(kv, c);
+    if (s != QIL_OK) return s;
+    if (max_q_len <= 0 || max_kv_len <= 0) return QIL_ERR_SHAPE;
+    if (!std::isfinite(scale) || num_heads / num_kv_heads > 128) return QIL_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return QIL_ERR_ALIGN;
+    if (!workspace ||
+        workspace_bytes < attn_paged_q_workspace(total_q, num_seqs, num_heads, num_kv_heads, head_dim, bits, max_q_len, max_kv_len))
+        return QIL_ERR_WORKSPACE;
+    return launch_attn_paged_q(q, kv, out, c, max_q_len, max_kv_len, scale, workspace, S(stream));
 }
 
 size_t qil_lora_batch_workspace_size(int M, int num_seqs, int rank) {

@@ -35,13 +35,13 @@
 
 #include <mutex>
 
-#include "attn_paged.cuh"
+#include "attn_paged_q.cuh"
 
 namespace qil {
 
 namespace {
 
-constexpr int kRows = kTileRows, kTok = 128, kThreads = 384;
+constexpr int kRows = kTileRows, kTok = 128;
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 constexpr float kMostSum = 16384.f;   // 64 weights of 2^kRaise
 constexpr float kRaise = 8.f;   // log2 by which a score may exceed the reference maximum
@@ -201,10 +201,33 @@ __device__ __forceinline__ bool find_pair(const PagedCache& c, int G, int tokens
     return false;
 }
 
-template <int kDim>
-__global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                                                               const __grid_constant__ CUtensorMap map_v, const AttnParams p) {
+// Codes as bf16 values of the cache, one rounding each: eight of them (16 bytes of the result).
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint4 values_of_bytes(uint32_t a, uint32_t b, uint32_t scale2) {
+    const auto pair = [&](uint32_t w, uint32_t pick) { return bf2_mul(bytes02(__byte_perm(w, 0u, pick)), scale2); };
+    return make_uint4(pair(a, 0x4140), pair(a, 0x4342), pair(b, 0x4140), pair(b, 0x4342));
+}
+__device__ __forceinline__ uint4 values_of_nibbles(uint32_t w, uint32_t zero2, uint32_t scale2) {   // zero2: 128 + zero point, twice
+    uint32_t x[4];   // elements (e, e + 4)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = bf2_mul(bf2_sub(plus128<0x000F000Fu>(w >> (4 * e)), zero2), scale2);
+    return make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+}
+
+// Threads: warp 0 copies, warp 1 issues the products, warp 2 clears (warp 3 idles); with a quantised cache four more warps
+// decode it into the operands' tiles; then the two softmax groups.
+template <int kBits>
+constexpr int kThreadsOf = kBits == 16 ? 384 : 512;
+
+template <int kDim, int kBits>
+__global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                         const __grid_constant__ CUtensorMap map_v, const AttnParams p, const QuantCache kvq) {
     using Shape = ManyShape<kDim>;
+    constexpr int kGroups = kBits == 16 ? 4 : 8;   // the first warp of the softmax groups
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
     wait_for_earlier_kernels();
@@ -228,8 +251,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
         mbar_init(v_raw, 1);                    // the copy of a V tile whose last tokens are still to be cleared
         mbar_init(drain, 1);
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(k_full + 8 * s, 1);
-            mbar_init(v_full + 8 * s, 1);
+            mbar_init(k_full + 8 * s, kBits == 16 ? 1 : 4);   // a copy, or the decoding warps
+            mbar_init(v_full + 8 * s, kBits == 16 ? 1 : 4);
             mbar_init(k_free + 8 * s, 1);       // commit after the last S of a K tile
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -267,8 +290,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
     }
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp == 0) {
+        if constexpr (kBits == 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (kBits != 16 && warp == 0) {
+            // ---------------- queries (the decoding warps take care of the cache) ----------------
+            if (lane < 2 && (lane ? n1 : n0) > 0) {
+                mbar_expect_tx(q_full + 8 * lane, (uint32_t)(p.tile_tokens * G * kDim * 2));
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+                    tma_load_3d(sq + lane * kTileBytes + h * kHalfBytes, &map_q, h * 64, kvh * G, q_lo + token0 + lane * p.tile_tokens,
+                                q_full + 8 * lane);
+                (void)mbar_wait(q_full + 8 * lane, 0);   // (not in flight when the block retires)
+            }
+        } else if (warp == 0) {
             // ---------------- copies: lane = (page of the tile, half of the head's columns) ----------------
             const int page_rows = p.c.page_size, per_tile = kTok / page_rows;
             const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
@@ -384,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                 tc_commit(drain);
                 if (!mbar_wait(drain, 0)) ok = false;
             }
-        } else if (warp == 2 && tail >= 0 && tail < n) {
+        } else if (kBits == 16 && warp == 2 && tail >= 0 && tail < n) {
             // ---------------- the last tile of V: tokens that do not exist become zeros ----------------
             const int s = tail % kStages;
             ok = mbar_wait(v_raw, 0);
@@ -399,10 +433,106 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
                 if (lane == 0) mbar_arrive(v_full + 8 * s);
             }
         }
+    } else if (warp < kGroups) {
+        // ---------------- codes to bf16 operand tiles: 32 tokens a warp ----------------
+        // A 16-byte piece of codes a lane and turn; its values go to shared memory in the operands' swizzle, the order of a
+        // lane's pieces chosen so that eight lanes meet all banks.  The codes of the next tile are on the way meanwhile.
+        if constexpr (kBits != 16) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+            constexpr int kRowBytes = kDim * kBits / 8, kAcross = kRowBytes / 16, kDown = 32 / kAcross, kTurns = 32 / kDown;
+            constexpr int kOut = kBits == 8 ? 2 : 4;   // 16-byte pieces of values of a piece of codes
+            const int across = lane % kAcross, down = lane / kAcross, first = 32 * (warp - 4);
+            const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
+            // the row of the cache where this lane's token of tile j lies, or -1
+            auto row_of = [&](int j) {
+                const int tok = (j0 + j) * kTok + first + lane;
+                if (j >= n || tok >= end) return -1;
+                const int page = __ldg(table + (tok >> p.page_shift));
+                return page < 0 || page >= p.c.num_pages ? -1 : (page * p.c.num_kv_heads + kvh) * p.c.page_size + (tok & (p.c.page_size - 1));
+            };
+            auto load = [&](uint4 (&w)[kTurns], const void* codes, int row) {
+#pragma unroll
+                for (int x = 0; x < kTurns; ++x) {
+                    const int from = __shfl_sync(0xffffffffu, row, x * kDown + down);
+                    w[x] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(codes) + (size_t)max(from, 0) * kRowBytes) + across);
+                }
+            };
+            auto parameter = [&](const __nv_bfloat16* scales, int row) -> uint32_t {   // scale, zero point above it
+                if (row < 0) return 0u;   // (zeros)
+                return kBits == 8 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(scales) + row) : __ldg(reinterpret_cast<const uint32_t*>(scales) + row);
+            };
+            auto store = [&](const uint4 (&w)[kTurns], uint32_t par, uint32_t tile) {
+#pragma unroll
+                for (int x = 0; x < kTurns; ++x) {
+                    const uint32_t mine = __shfl_sync(0xffffffffu, par, x * kDown + down);
+                    const uint32_t scale2 = __byte_perm(mine, mine, 0x1010);
+                    uint4 f[kOut];
+                    if (kBits == 8) {
+                        f[0] = values_of_bytes(w[x].x, w[x].y, scale2);
+                        f[1] = values_of_bytes(w[x].z, w[x].w, scale2);
+                    } else {
+                        uint32_t zero2 = __byte_perm(mine, mine, 0x3232);
+                        asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(zero2) : "r"(0x43004300u));
+                        f[0] = values_of_nibbles(w[x].x, zero2, scale2);
+                        f[1] = values_of_nibbles(w[x].y, zero2, scale2);
+                        f[kOut - 2] = values_of_nibbles(w[x].z, zero2, scale2);
+                        f[kOut - 1] = values_of_nibbles(w[x].w, zero2, scale2);
+                    }
+                    const int r = first + x * kDown + down, at = across * kOut, half = at / 8;
+#pragma unroll
+                    for (int k = 0; k < kOut; ++k) {
+                        const int turn = kDim == 64 || half == 0 ? k : k ^ (kOut / 2);   // (the other half's lanes in another order)
+                        const uint32_t to = tile + half * kHalfBytes + r * 128 + ((((at & 7) + turn) ^ r) & 7) * 16;
+                        uint4 v = f[0];
+#pragma unroll
+                        for (int e = 1; e < kOut; ++e)
+                            if (turn == e) v = f[e];
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                    }
+                }
+            };
+            auto publish = [&](uint32_t bar) {   // this warp's rows are in shared memory, for the tensor cores to read
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar);
+            };
+            uint4 kw[kTurns], vw[kTurns];
+            int row = row_of(0);
+            uint32_t kp = parameter(kvq.ks, row), vp = parameter(kvq.vs, row);
+            if (n > 0) {
+                load(kw, kvq.k, row);
+                load(vw, kvq.v, row);
+            }
+            row = row_of(1);
+            for (int j = 0; j < n; ++j) {
+                const int s = j % kStages, i = j - kStages;   // (which tiles are free when: as for the copies above)
+                // A head whose scale is NaN reads as NaN.  A value like that makes its token's key one: the rows that see the token
+                // are NaN by their scores, and no weight of zero meets the value.
+                const bool nan = (vp & 0x7FFFu) >= 0x7F80u;
+                const uint32_t k_par = nan ? kp | 0x7FC0u : kp, v_par = nan ? 0u : vp;
+                const uint32_t kp1 = parameter(kvq.ks, row), vp1 = parameter(kvq.vs, row);
+                if (i >= 0) ok = mbar_wait(k_free + 8 * s, (i / kStages) & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                store(kw, k_par, sk + s * kTileBytes);
+                publish(k_full + 8 * s);
+                if (j + 1 < n) load(kw, kvq.k, row);
+                if (i >= 0) ok = mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                store(vw, v_par, sv + s * kTileBytes);
+                publish(v_full + 8 * s);
+                if (j + 1 < n) load(vw, kvq.v, row);
+                kp = kp1;
+                vp = vp1;
+                row = row_of(j + 2);
+            }
+        }
     } else {
         // ---------------- softmax of row tile i: one row per thread ----------------
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        const int i = (warp - 4) >> 2, r = tid & 127, token = r / G;
+        if constexpr (kBits == 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        const int i = (warp - kGroups) >> 2, r = tid & 127, token = r / G;
         const int my_tokens = i ? tokens[1] : tokens[0];
         const bool live = token < my_tokens;   // (the other rows hold anything; they take no part in the votes below)
         const int mine = i ? n1 : n0;
@@ -592,7 +722,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const __grid_con
             float odd[2];
             f2_split(f2_add(strange[0], strange[1]), odd[0], odd[1]);
             const int shown = mine > 0 && live ? min(see, mine * kTok) : 0;   // tokens that the row sees, from the part's first
-            unsigned again = __ballot_sync(0xffffffffu, shown > 0 && odd[0] + odd[1] != 0.f && sum < INFINITY && sum != 0.f);
+            // (Codes are finite: with a quantised cache there are none.)
+            unsigned again = kBits != 16 ? 0u : __ballot_sync(0xffffffffu, shown > 0 && odd[0] + odd[1] != 0.f && sum < INFINITY && sum != 0.f);
             while (again) {
                 const int rr = __ffs(again) - 1;
                 again &= again - 1;
@@ -740,22 +871,30 @@ bool encode_queries(CUtensorMap* map, const AttnParams& p) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kDim>
-qil_status go(const AttnParams& p, cudaStream_t st) {
+template <int kDim, int kBits>
+qil_status go(const AttnParams& p, const QuantCache& kvq, cudaStream_t st) {
     CUtensorMap mq, mk, mv;
-    if (!encode_queries(&mq, p) || !encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)) return QIL_ERR_CUDA;
+    if (!encode_queries(&mq, p)) return QIL_ERR_CUDA;
+    if (kBits != 16) mk = mv = mq;   // (the codes are read without one)
+    else if (!encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)) return QIL_ERR_CUDA;
     constexpr int kSmem = ManyShape<kDim>::kSmem;
     static_assert(kSmem <= 232448, "shared memory per block");
     static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(attn_many_kernel<kDim>, kSmem, allowed)) return QIL_ERR_CUDA;
+    if (!allow_smem(attn_many_kernel<kDim, kBits>, kSmem, allowed)) return QIL_ERR_CUDA;
     // (heads first, so that the long tiles of all heads start before the short ones of any)
     const dim3 grid((unsigned)((long long)p.c.num_kv_heads * (p.c.total_q / (2 * p.tile_tokens) + p.c.num_seqs)), 1u, (unsigned)p.splits);
-    return launch_early(attn_many_kernel<kDim>, grid, kThreads, kSmem, st, mq, mk, mv, p);
+    return launch_early(attn_many_kernel<kDim, kBits>, grid, kThreadsOf<kBits>, kSmem, st, mq, mk, mv, p, kvq);
 }
 
 }  // namespace
 
-qil_status launch_attn_many(const AttnParams& p, cudaStream_t st) { return p.c.head_dim == 128 ? go<128>(p, st) : go<64>(p, st); }
+qil_status launch_attn_many(const AttnParams& p, cudaStream_t st) {
+    return p.c.head_dim == 128 ? go<128, 16>(p, QuantCache{}, st) : go<64, 16>(p, QuantCache{}, st);
+}
+qil_status launch_attn_many_q(const AttnQuantParams& p, cudaStream_t st) {
+    if (p.a.c.head_dim == 128) return p.kv.bits == 8 ? go<128, 8>(p.a, p.kv, st) : go<128, 4>(p.a, p.kv, st);
+    return p.kv.bits == 8 ? go<64, 8>(p.a, p.kv, st) : go<64, 4>(p.a, p.kv, st);
+}
 
 qil_status launch_attn_many_join(const AttnParams& p, cudaStream_t st) {
     const long long items = (long long)p.c.total_q * p.c.num_heads;

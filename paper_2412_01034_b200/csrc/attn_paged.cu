@@ -5,7 +5,8 @@
 //   o = sum_j softmax_j(scale q . k_j) v_j;  a token that sees nothing (p < 0) gets zeros
 // The lengths are on the device; the host knows their bounds.  Requests of at most 16 query rows per key head go to
 // attn_few.cu, the others to attn_many.cu; a launch is left out where the bounds show that it would find nothing.
-#include "attn_paged.cuh"
+// The same over a quantised cache (attn_few_q.cu; attn_many.cu with warps that decode the cache).
+#include "attn_paged_q.cuh"
 
 namespace qil {
 
@@ -21,7 +22,7 @@ struct AttnPlan {
     size_t few_floats, many_floats;
 };
 
-AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, int max_kv) {
+AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int bits, int max_q, int max_kv) {
     AttnPlan pl = {};
     const int G = H / Hk;
     const long long sms = num_sms();
@@ -37,7 +38,9 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
         // are a cluster and join their results on the chip; one token over 500, 32 heads: 5.3 us (7.8 with blocks of 384),
         // over 1500: 7.6, over 4000: 10.9 (14.4 with parts in the workspace).  Eight blocks that would take more than 1024
         // tokens each give way to more, of 384 at least (a part's way through the workspace costs as much as 300 tokens).
-        const long long items = (long long)num_seqs * Hk, room = 2 * sms, per_row = room / items;
+        // Blocks over a quantised cache are four to an SM (three with more than 8 rows).
+        const long long rows = (long long)max_q * G < kFewRows ? (long long)max_q * G : kFewRows;
+        const long long items = (long long)num_seqs * Hk, room = (bits == 16 ? 2 : rows <= 8 ? 4 : 3) * sms, per_row = room / items;
         const auto round64 = [](long long n) { return (n + 63) / 64 * 64; };
         long long chunk = round64((max_kv * items + room - 1) / room);
         chunk = chunk < 384 ? 384 : chunk > 2048 ? 2048 : chunk;
@@ -52,8 +55,7 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int max_q, i
         if (items > kCounters) chunk = max_kv;   // (rows enough to fill the GPU many times over: one block each)
         pl.chunk = (int)chunk;
         pl.slots = (int)((max_kv + chunk - 1) / chunk);
-        const long long rows = (long long)max_q * G;
-        pl.few_rows = (int)(rows < kFewRows ? rows : kFewRows);
+        pl.few_rows = (int)rows;
         if (pl.slots > 1 && !pl.together) pl.few_floats = ((size_t)items * pl.slots * pl.few_rows * (D + 2) + 3) & ~(size_t)3;   // (16-byte stores behind them)
     }
     if (pl.many) {
@@ -75,18 +77,13 @@ static_assert(kHeader + kCounters * sizeof(int) == QIL_ATTN_PAGED_ZEROED_BYTES, 
 
 }  // namespace
 
-size_t attn_paged_workspace(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int max_q_len, int max_kv_len) {
-    const AttnPlan pl = plan_attn(total_q, num_seqs, num_heads, num_kv_heads, head_dim, max_q_len, max_kv_len);
-    return kHeader + kCounters * sizeof(int) + (pl.few_floats + pl.many_floats) * sizeof(float);
-}
+namespace {
 
-qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const PagedCache& c, int max_q_len,
-                             int max_kv_len, float scale, void* ws, cudaStream_t st) {
-    const AttnPlan pl = plan_attn(c.total_q, c.num_seqs, c.num_heads, c.num_kv_heads, c.head_dim, max_q_len, max_kv_len);
-    AttnParams p;
+size_t workspace_of(const AttnPlan& pl) { return kHeader + kCounters * sizeof(int) + (pl.few_floats + pl.many_floats) * sizeof(float); }
+
+AttnParams params_of(const AttnPlan& pl, const void* q, void* out, const PagedCache& c, float scale, void* ws) {
+    AttnParams p = {};
     p.q = reinterpret_cast<const __nv_bfloat16*>(q);
-    p.k = reinterpret_cast<const __nv_bfloat16*>(k_cache);
-    p.v = reinterpret_cast<const __nv_bfloat16*>(v_cache);
     p.out = reinterpret_cast<__nv_bfloat16*>(out);
     p.c = c;
     p.G = c.num_heads / c.num_kv_heads;
@@ -104,10 +101,39 @@ qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_c
     p.few_parts = reinterpret_cast<float*>(base + kHeader + kCounters * sizeof(int));
     p.many_parts = p.few_parts + pl.few_floats;   // (the two kernels may run at the same time)
     p.both = pl.few && pl.many;
+    return p;
+}
+
+}  // namespace
+
+size_t attn_paged_workspace(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int max_q_len, int max_kv_len) {
+    return workspace_of(plan_attn(total_q, num_seqs, num_heads, num_kv_heads, head_dim, 16, max_q_len, max_kv_len));
+}
+size_t attn_paged_q_workspace(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int bits, int max_q_len, int max_kv_len) {
+    return workspace_of(plan_attn(total_q, num_seqs, num_heads, num_kv_heads, head_dim, bits, max_q_len, max_kv_len));
+}
+
+qil_status launch_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* out, const PagedCache& c, int max_q_len,
+                             int max_kv_len, float scale, void* ws, cudaStream_t st) {
+    const AttnPlan pl = plan_attn(c.total_q, c.num_seqs, c.num_heads, c.num_kv_heads, c.head_dim, 16, max_q_len, max_kv_len);
+    AttnParams p = params_of(pl, q, out, c, scale, ws);
+    p.k = reinterpret_cast<const __nv_bfloat16*>(k_cache);
+    p.v = reinterpret_cast<const __nv_bfloat16*>(v_cache);
     qil_status s = QIL_OK;
     if (pl.many) s = launch_attn_many(p, st);
     if (s == QIL_OK && pl.few) s = launch_attn_few(p, st);
     if (s == QIL_OK && pl.many && pl.splits > 1) s = launch_attn_many_join(p, st);
+    return s;
+}
+
+qil_status launch_attn_paged_q(const void* q, const QuantCache& kvq, void* out, const PagedCache& c, int max_q_len, int max_kv_len, float scale,
+                               void* ws, cudaStream_t st) {
+    const AttnPlan pl = plan_attn(c.total_q, c.num_seqs, c.num_heads, c.num_kv_heads, c.head_dim, kvq.bits, max_q_len, max_kv_len);
+    const AttnQuantParams p = {params_of(pl, q, out, c, scale, ws), kvq};
+    qil_status s = QIL_OK;
+    if (pl.many) s = launch_attn_many_q(p, st);
+    if (s == QIL_OK && pl.few) s = launch_attn_few_q(p, st);
+    if (s == QIL_OK && pl.many && pl.splits > 1) s = launch_attn_many_join(p.a, st);
     return s;
 }
 

@@ -236,6 +236,88 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// the quantised cache and the requests: k, v, k_scale, v_scale, cu, kv_len, block_table; the codes' type says how many bits
+struct PagedQ {
+    int64_t pages, kv_heads, page, dim, seqs, width;
+    int bits;
+    void *k, *v, *ks, *vs;
+    int *cu, *len, *table;
+    explicit PagedQ(PyObject* const* a) {
+        const Tensor &kc = tensor(a[0], "k", 4), &bt = tensor(a[6], "block_table", 2);
+        const c10::ScalarType type = kc.scalar_type();
+        if (type != c10::kChar && type != c10::kInt)
+            throw std::invalid_argument("qil: k is torch." + type_name(type) + ", expected int8 (8 bits) or int32 (4 bits)");
+        bits = type == c10::kChar ? 8 : 4;
+        pages = kc.size(0), kv_heads = kc.size(1), page = kc.size(2), dim = kc.size(3) * (bits == 8 ? 1 : 8);
+        seqs = bt.size(0), width = bt.size(1);
+        const int64_t of[4] = {pages, kv_heads, page, 2};
+        const Sizes scales(of, bits == 8 ? 3 : 4);
+        k = arg(kc, "k", type, kc.sizes());
+        v = arg(tensor(a[1], "v"), "v", type, kc.sizes());
+        ks = arg(tensor(a[2], "k_scale"), "k_scale", c10::kBFloat16, scales);
+        vs = arg(tensor(a[3], "v_scale"), "v_scale", c10::kBFloat16, scales);
+        cu = static_cast<int*>(arg(tensor(a[4], "cu_q"), "cu_q", c10::kInt, {seqs + 1}));
+        len = static_cast<int*>(arg(tensor(a[5], "kv_len"), "kv_len", c10::kInt, {seqs}));
+        table = static_cast<int*>(arg(bt, "block_table", c10::kInt, {seqs, width}));
+    }
+};
+
+// rope_append_q(qkv, cos_sin, k, v, k_scale, v_scale, cu_q, kv_len, block_table, num_heads, out)
+PyObject* rope_append_q(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, {"qkv", "cos_sin", "k", "v", "k_scale", "v_scale", "cu_q", "kv_len", "block_table", "num_heads", "out"}, [&]() -> PyObject* {
+        const Tensor &qkv = tensor(a[0], "qkv", 2), &cs = tensor(a[1], "cos_sin", 2);
+        const PagedQ c(a + 2);
+        const int64_t heads = whole(a[9]), T = qkv.size(0);
+        void* pq = arg(qkv, "qkv", c10::kBFloat16, {T, (heads + 2 * c.kv_heads) * c.dim});
+        void* pcs = arg(cs, "cos_sin", c10::kFloat, {cs.size(0), c.dim});
+        const Tensor out = a[10] == Py_None ? fresh(qkv, {T, heads, c.dim}, c10::kBFloat16) : tensor(a[10], "out");
+        void* po = arg(out, "out", c10::kBFloat16, {T, heads, c.dim});
+        const qil_status s = qil_rope_append_q(pq, static_cast<float*>(pcs), po, c.k, c.v, c.ks, c.vs, c.bits, c.cu, c.len, c.table, size32(T),
+                                               size32(c.seqs), size32(heads), size32(c.kv_heads), size32(c.dim), size32(c.page),
+                                               size32(c.pages), size32(c.width), size32(cs.size(0)), stream_of(qkv));
+        return s != QIL_OK ? PyLong_FromLong(s) : wrap(out);
+    });
+}
+
+// kv_read_q(k, v, k_scale, v_scale, cu_q, kv_len, block_table, total_rows, k_out, v_out)
+PyObject* kv_read_q(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, {"k", "v", "k_scale", "v_scale", "cu_q", "kv_len", "block_table", "total_rows", "k_out", "v_out"}, [&]() -> PyObject* {
+        const PagedQ c(a);
+        const int64_t T = whole(a[7]);
+        if (T <= 0) return PyLong_FromLong(QIL_ERR_SHAPE);
+        const Tensor& kc = tensor(a[0], "k");
+        const Tensor k = a[8] == Py_None ? fresh(kc, {T, c.kv_heads, c.dim}, c10::kBFloat16) : tensor(a[8], "k_out");
+        const Tensor v = a[9] == Py_None ? fresh(kc, {T, c.kv_heads, c.dim}, c10::kBFloat16) : tensor(a[9], "v_out");
+        void* pk = arg(k, "k_out", c10::kBFloat16, {T, c.kv_heads, c.dim});
+        void* pv = arg(v, "v_out", c10::kBFloat16, {T, c.kv_heads, c.dim});
+        const qil_status s = qil_kv_read_q(c.k, c.v, c.ks, c.vs, c.bits, pk, pv, c.cu, c.len, c.table, size32(T), size32(c.seqs),
+                                           size32(c.kv_heads), size32(c.dim), size32(c.page), size32(c.pages), size32(c.width), stream_of(kc));
+        return s != QIL_OK ? PyLong_FromLong(s) : Py_BuildValue("(NN)", wrap(k), wrap(v));
+    });
+}
+
+// attn_paged_q(q, k, v, k_scale, v_scale, cu_q, kv_len, block_table, max_q_len, max_kv_len, scale, out, workspace)
+PyObject* attn_paged_q(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, {"q", "k", "v", "k_scale", "v_scale", "cu_q", "kv_len", "block_table", "max_q_len", "max_kv_len", "scale", "out",
+                          "workspace"}, [&]() -> PyObject* {
+        const Tensor& q = tensor(a[0], "q", 3);
+        const PagedQ c(a + 1);
+        const int64_t T = q.size(0), heads = q.size(1);
+        void* pq = arg(q, "q", c10::kBFloat16, {T, heads, c.dim});
+        const int max_q = size32(whole(a[8])), max_kv = size32(whole(a[9]));
+        const double scale = a[10] == Py_None ? 1.0 / std::sqrt((double)c.dim) : real(a[10]);
+        const Tensor out = a[11] == Py_None ? fresh(q, {T, heads, c.dim}, c10::kBFloat16) : tensor(a[11], "out");
+        void* po = arg(out, "out", c10::kBFloat16, {T, heads, c.dim});
+        const size_t bytes = a[12] != Py_None ? 0 : qil_attn_paged_q_workspace_size(size32(T), size32(c.seqs), size32(heads), size32(c.kv_heads),
+                                                                                    size32(c.dim), c.bits, max_q, max_kv);
+        const Tensor ws = workspace_of(a[12], bytes, QIL_ATTN_PAGED_ZEROED_BYTES, q);
+        const qil_status s = qil_attn_paged_q(pq, c.k, c.v, c.ks, c.vs, c.bits, po, c.cu, c.len, c.table, size32(T), size32(c.seqs),
+                                              size32(heads), size32(c.kv_heads), size32(c.dim), size32(c.page), size32(c.pages),
+                                              size32(c.width), max_q, max_kv, (float)scale, ws.data_ptr(), ws.nbytes(), stream_of(q));
+        return s != QIL_OK ? PyLong_FromLong(s) : wrap(out);
+    });
+}
+
 // lora_batch_add(x, a, b, y, cu_q, adapter, scales, out, workspace)
 PyObject* lora_batch_add(PyObject*, PyObject* const* p, Py_ssize_t n) {
     return guarded(p, n, {"x", "a", "b", "y", "cu_q", "adapter", "scales", "out", "workspace"}, [&]() -> PyObject* {
@@ -263,6 +345,7 @@ PyObject* lora_batch_add(PyObject*, PyObject* const* p, Py_ssize_t n) {
 
 #define QIL_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {QIL_METHOD(rmsnorm), QIL_METHOD(rope_append), QIL_METHOD(attn_paged), QIL_METHOD(lora_batch_add),
+                         QIL_METHOD(rope_append_q), QIL_METHOD(kv_read_q), QIL_METHOD(attn_paged_q),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qil_torch", "Marshalling of the qil layer operators.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
