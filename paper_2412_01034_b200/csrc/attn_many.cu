@@ -46,13 +46,15 @@ constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 constexpr float kMostSum = 16384.f;   // 64 weights of 2^kRaise
 constexpr float kRaise = 8.f;   // log2 by which a score may exceed the reference maximum
 
-template <int kDim>
+template <int kDim, int kBits>
 struct ManyShape {
     static constexpr int kHalves = kDim / 64;                 // 64 columns (128 bytes) per swizzled half
     static constexpr int kTileBytes = kTok * kDim * 2;        // Q_i, K and V tiles: 128 rows each
     static constexpr int kHalfBytes = kTok * 128;
     static constexpr int kStages = kDim == 128 ? 2 : 4;
-    static constexpr int kSmem = 2 * kTileBytes + 2 * kStages * kTileBytes + 1024 + 256;
+    static constexpr int kRowBytes = kDim * kBits / 8;        // of codes; a quantised cache: one tile of those of keys and one of values
+    static constexpr int kBars = 2 * kTileBytes + 2 * kStages * kTileBytes + (kBits == 16 ? 0 : 2 * kTok * kRowBytes);
+    static constexpr int kSmem = kBars + 1024 + 256;
     static constexpr uint32_t kO = 256;                       // tensor memory: S_0, S_1 at 0, 128; O_0, O_1 behind them
     static_assert(kO + 2 * kDim <= 512, "tensor memory");
 };
@@ -226,7 +228,7 @@ constexpr int kThreadsOf = kBits == 16 ? 384 : 512;
 template <int kDim, int kBits>
 __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                          const __grid_constant__ CUtensorMap map_v, const AttnParams p, const QuantCache kvq) {
-    using Shape = ManyShape<kDim>;
+    using Shape = ManyShape<kDim, kBits>;
     constexpr int kGroups = kBits == 16 ? 4 : 8;   // the first warp of the softmax groups
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
@@ -236,9 +238,10 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
     const int G = p.G, H = p.c.num_heads, kvh = blockIdx.x % p.c.num_kv_heads;
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sq = smem_u32(smem), sk = sq + 2 * kTileBytes, sv = sk + kStages * kTileBytes;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kTileBytes + 2 * kStages * kTileBytes);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Shape::kBars);
     const uint32_t q_full = smem_u32(bars), s_full = q_full + 16, p_full = q_full + 32, o_done = q_full + 64, v_raw = q_full + 80,
-                   drain = q_full + 88, k_full = q_full + 96, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages;
+                   drain = q_full + 88, k_full = q_full + 96, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages, raw_full = k_free + 8 * kStages + 8,
+                   raw_free = raw_full + 16;   // (between k_free and raw_full: where tensor memory is)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 3 * kStages);
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -250,6 +253,10 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
         }
         mbar_init(v_raw, 1);                    // the copy of a V tile whose last tokens are still to be cleared
         mbar_init(drain, 1);
+        for (int i = 0; i < 2 && kBits != 16; ++i) {
+            mbar_init(raw_full + 8 * i, 1);     // the copy of a tile of codes
+            mbar_init(raw_free + 8 * i, 4);     // the decoding warps
+        }
         for (int s = 0; s < kStages; ++s) {
             mbar_init(k_full + 8 * s, kBits == 16 ? 1 : 4);   // a copy, or the decoding warps
             mbar_init(v_full + 8 * s, kBits == 16 ? 1 : 4);
@@ -292,30 +299,20 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
     if (warp < 4) {
         if constexpr (kBits == 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (kBits != 16 && warp == 0) {
-            // ---------------- queries (the decoding warps take care of the cache) ----------------
-            if (lane < 2 && (lane ? n1 : n0) > 0) {
-                mbar_expect_tx(q_full + 8 * lane, (uint32_t)(p.tile_tokens * G * kDim * 2));
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h)
-                    tma_load_3d(sq + lane * kTileBytes + h * kHalfBytes, &map_q, h * 64, kvh * G, q_lo + token0 + lane * p.tile_tokens,
-                                q_full + 8 * lane);
-                (void)mbar_wait(q_full + 8 * lane, 0);   // (not in flight when the block retires)
-            }
-        } else if (warp == 0) {
+        if (warp == 0) {
             // ---------------- copies: lane = (page of the tile, half of the head's columns) ----------------
             const int page_rows = p.c.page_size, per_tile = kTok / page_rows;
             const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
-            const int my_page = lane / kHalves, my_half = lane % kHalves;
+            const int my_page = kBits == 16 ? lane / kHalves : lane, my_half = kBits == 16 ? lane % kHalves : 0;
             const uint32_t my_dst = (uint32_t)(my_half * kHalfBytes + my_page * page_rows * 128);
-            auto copy = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int tok0, int row) {
+            [[maybe_unused]] auto copy = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int tok0, int row) {
                 const int pages = min(per_tile, (end - tok0 + page_rows - 1) / page_rows);   // pages that hold cached tokens
                 if (lane == 0) mbar_expect_tx(bar, (uint32_t)(pages * page_rows * kDim * 2));
                 __syncwarp();
                 if (lane < pages * kHalves) tma_load_2d(dst + my_dst, map, my_half * 64, row, bar);
             };
             auto first_row = [&](int tok0) {   // the cache row where this lane's page begins (a page that does not exist: no row, zeros)
-                if (lane >= per_tile * kHalves || tok0 + my_page * page_rows >= end) return -1;
+                if (my_page >= per_tile || tok0 + my_page * page_rows >= end) return -1;
                 const int page = __ldg(table + tok0 / page_rows + my_page);
                 return page < 0 || page >= p.c.num_pages ? -page_rows : (page * p.c.num_kv_heads + kvh) * page_rows;
             };
@@ -327,31 +324,59 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                     tma_load_3d(sq + lane * kTileBytes + h * kHalfBytes, &map_q, h * 64, kvh * G, q_lo + token0 + lane * p.tile_tokens,
                                 q_full + 8 * lane);
             }
-            int k_sent = 0, v_sent = 0;
-            for (int j = 0; j < n; ++j) {
-                const int s = j % kStages, tok0 = (j0 + j) * kTok;
-                const int next = j + 1 < n ? first_row(tok0 + kTok) : 0;
-                // The lead's S(i) complete: K(i) is free, and V(i - 1), whose last product was issued before that S.  (The
-                // barrier of a stage cannot get a second phase ahead of this warp: that would take a K tile not copied yet.)
-                const int i = j - kStages;
-                if (i >= 0) ok = mbar_wait(k_free + 8 * s, (i / kStages) & 1);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                copy(&map_k, sk + s * kTileBytes, k_full + 8 * s, tok0, row);
-                k_sent = j + 1;
-                if (i >= 0) ok = mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                copy(&map_v, sv + s * kTileBytes, j == tail ? v_raw : v_full + 8 * s, tok0, row);
-                v_sent = j + 1;
-                row = next;
+            if constexpr (kBits != 16) {
+                // codes, one tile of keys and one of values at a time: they leave as soon as they are decoded
+                const uint32_t raw = sv + kStages * kTileBytes;
+                int sent = 0;
+                for (int j = 0; j < n; ++j) {
+                    const int tok0 = (j0 + j) * kTok, pages = min(per_tile, (end - tok0 + page_rows - 1) / page_rows);
+                    const int next = j + 1 < n ? first_row(tok0 + kTok) : 0;
+#pragma unroll
+                    for (int side = 0; side < 2; ++side) {
+                        if (j > 0) ok = mbar_wait(raw_free + 8 * side, (j - 1) & 1);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        if (lane == 0) mbar_expect_tx(raw_full + 8 * side, (uint32_t)(pages * page_rows * Shape::kRowBytes));
+                        __syncwarp();
+                        if (lane < pages)
+                            tma_load_2d(raw + side * (kTok * Shape::kRowBytes) + lane * page_rows * Shape::kRowBytes, side ? &map_v : &map_k, 0, row,
+                                        raw_full + 8 * side);
+                        ++sent;
+                    }
+                    if (!ok) break;
+                    row = next;
+                }
+                for (int i = 0; i < 2; ++i)
+                    if ((i ? n1 : n0) > 0) (void)mbar_wait(q_full + 8 * i, 0);
+                if (sent > 0) (void)mbar_wait(raw_full, ((sent - 1) / 2) & 1);
+                if (sent > 1) (void)mbar_wait(raw_full + 8, (sent / 2 - 1) & 1);
+            } else {
+                int k_sent = 0, v_sent = 0;
+                for (int j = 0; j < n; ++j) {
+                    const int s = j % kStages, tok0 = (j0 + j) * kTok;
+                    const int next = j + 1 < n ? first_row(tok0 + kTok) : 0;
+                    // The lead's S(i) complete: K(i) is free, and V(i - 1), whose last product was issued before that S.  (The
+                    // barrier of a stage cannot get a second phase ahead of this warp: that would take a K tile not copied yet.)
+                    const int i = j - kStages;
+                    if (i >= 0) ok = mbar_wait(k_free + 8 * s, (i / kStages) & 1);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    copy(&map_k, sk + s * kTileBytes, k_full + 8 * s, tok0, row);
+                    k_sent = j + 1;
+                    if (i >= 0) ok = mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    copy(&map_v, sv + s * kTileBytes, j == tail ? v_raw : v_full + 8 * s, tok0, row);
+                    v_sent = j + 1;
+                    row = next;
+                }
+                // no copy may still be in flight when the block retires (after a time-out elsewhere either)
+                for (int i = 0; i < 2; ++i)
+                    if ((i ? n1 : n0) > 0) (void)mbar_wait(q_full + 8 * i, 0);
+                for (int j = max(0, k_sent - kStages); j < k_sent; ++j) (void)mbar_wait(k_full + 8 * (j % kStages), (j / kStages) & 1);
+                for (int j = max(0, v_sent - kStages); j < v_sent; ++j)
+                    (void)(j == tail ? mbar_wait(v_raw, 0) : mbar_wait(v_full + 8 * (j % kStages), (j / kStages) & 1));
             }
-            // no copy may still be in flight when the block retires (after a time-out elsewhere either)
-            for (int i = 0; i < 2; ++i)
-                if ((i ? n1 : n0) > 0) (void)mbar_wait(q_full + 8 * i, 0);
-            for (int j = max(0, k_sent - kStages); j < k_sent; ++j) (void)mbar_wait(k_full + 8 * (j % kStages), (j / kStages) & 1);
-            for (int j = max(0, v_sent - kStages); j < v_sent; ++j)
-                (void)(j == tail ? mbar_wait(v_raw, 0) : mbar_wait(v_full + 8 * (j % kStages), (j / kStages) & 1));
         } else if (warp == 1) {
             // ---------------- products ----------------
             if (lane == 0 && n > 0) {
@@ -434,104 +459,86 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             }
         }
     } else if (warp < kGroups) {
-        // ---------------- codes to bf16 operand tiles: 32 tokens a warp ----------------
-        // A 16-byte piece of codes a lane and turn; its values go to shared memory in the operands' swizzle, the order of a
-        // lane's pieces chosen so that eight lanes meet all banks.  The codes of the next tile are on the way meanwhile.
+        // ---------------- codes to bf16 operand tiles: a token a thread ----------------
+        // The codes arrive by bulk tensor copies in a swizzle of their own row length and go out in the operands', so that eight
+        // threads that read or write the same piece of eight tokens meet all banks.
         if constexpr (kBits != 16) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-            constexpr int kRowBytes = kDim * kBits / 8, kAcross = kRowBytes / 16, kDown = 32 / kAcross, kTurns = 32 / kDown;
-            constexpr int kOut = kBits == 8 ? 2 : 4;   // 16-byte pieces of values of a piece of codes
-            const int across = lane % kAcross, down = lane / kAcross, first = 32 * (warp - 4);
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+            const int r = tid & 127;
             const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
-            // the row of the cache where this lane's token of tile j lies, or -1
-            auto row_of = [&](int j) {
-                const int tok = (j0 + j) * kTok + first + lane;
+            auto row_of = [&](int j) {   // the row of the cache where this thread's token of tile j lies, or -1
+                const int tok = (j0 + j) * kTok + r;
                 if (j >= n || tok >= end) return -1;
                 const int page = __ldg(table + (tok >> p.page_shift));
                 return page < 0 || page >= p.c.num_pages ? -1 : (page * p.c.num_kv_heads + kvh) * p.c.page_size + (tok & (p.c.page_size - 1));
             };
-            auto load = [&](uint4 (&w)[kTurns], const void* codes, int row) {
-#pragma unroll
-                for (int x = 0; x < kTurns; ++x) {
-                    const int from = __shfl_sync(0xffffffffu, row, x * kDown + down);
-                    w[x] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(codes) + (size_t)max(from, 0) * kRowBytes) + across);
-                }
-            };
             auto parameter = [&](const __nv_bfloat16* scales, int row) -> uint32_t {   // scale, zero point above it
-                if (row < 0) return 0u;   // (zeros)
+                if (row < 0) return 0u;   // (zeros, whatever lies in the place of the codes)
                 return kBits == 8 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(scales) + row) : __ldg(reinterpret_cast<const uint32_t*>(scales) + row);
             };
-            auto store = [&](const uint4 (&w)[kTurns], uint32_t par, uint32_t tile) {
+            auto decode = [&](const unsigned char* raw, uint32_t par, unsigned char* tile) {
+                const uint32_t scale2 = __byte_perm(par, par, 0x1010);
+                uint32_t zero2 = __byte_perm(par, par, 0x3232);
+                if (kBits == 4) asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(zero2) : "r"(0x43004300u));
+                constexpr int kOut = kBits == 8 ? 2 : 4;   // 16-byte pieces of values of a piece of codes
 #pragma unroll
-                for (int x = 0; x < kTurns; ++x) {
-                    const uint32_t mine = __shfl_sync(0xffffffffu, par, x * kDown + down);
-                    const uint32_t scale2 = __byte_perm(mine, mine, 0x1010);
+                for (int x = 0; x < Shape::kRowBytes / 16; ++x) {
+                    const int turn = Shape::kRowBytes == 128 ? r & 7 : Shape::kRowBytes == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+                    const uint4 w = *reinterpret_cast<const uint4*>(raw + r * Shape::kRowBytes + ((x ^ turn) * 16));
                     uint4 f[kOut];
                     if (kBits == 8) {
-                        f[0] = values_of_bytes(w[x].x, w[x].y, scale2);
-                        f[1] = values_of_bytes(w[x].z, w[x].w, scale2);
+                        f[0] = values_of_bytes(w.x, w.y, scale2);
+                        f[1] = values_of_bytes(w.z, w.w, scale2);
                     } else {
-                        uint32_t zero2 = __byte_perm(mine, mine, 0x3232);
-                        asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(zero2) : "r"(0x43004300u));
-                        f[0] = values_of_nibbles(w[x].x, zero2, scale2);
-                        f[1] = values_of_nibbles(w[x].y, zero2, scale2);
-                        f[kOut - 2] = values_of_nibbles(w[x].z, zero2, scale2);
-                        f[kOut - 1] = values_of_nibbles(w[x].w, zero2, scale2);
+                        f[0] = values_of_nibbles(w.x, zero2, scale2);
+                        f[1] = values_of_nibbles(w.y, zero2, scale2);
+                        f[kOut - 2] = values_of_nibbles(w.z, zero2, scale2);
+                        f[kOut - 1] = values_of_nibbles(w.w, zero2, scale2);
                     }
-                    const int r = first + x * kDown + down, at = across * kOut, half = at / 8;
 #pragma unroll
-                    for (int k = 0; k < kOut; ++k) {
-                        const int turn = kDim == 64 || half == 0 ? k : k ^ (kOut / 2);   // (the other half's lanes in another order)
-                        const uint32_t to = tile + half * kHalfBytes + r * 128 + ((((at & 7) + turn) ^ r) & 7) * 16;
-                        uint4 v = f[0];
-#pragma unroll
-                        for (int e = 1; e < kOut; ++e)
-                            if (turn == e) v = f[e];
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                    for (int e = 0; e < kOut; ++e) {
+                        const int at = x * kOut + e;
+                        *reinterpret_cast<uint4*>(tile + (at >> 3) * kHalfBytes + r * 128 + (((at ^ r) & 7) * 16)) = f[e];
                     }
                 }
             };
-            auto publish = [&](uint32_t bar) {   // this warp's rows are in shared memory, for the tensor cores to read
+            auto publish = [&](uint32_t full, uint32_t raw_free) {   // this warp's tokens are in shared memory, for the tensor cores to read
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar);
+                if (lane == 0) {
+                    mbar_arrive(full);
+                    mbar_arrive(raw_free);
+                }
             };
-            uint4 kw[kTurns], vw[kTurns];
-            int row = row_of(0);
+            unsigned char *k_tiles = smem + 2 * kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes, *raw_k = v_tiles + kStages * kTileBytes,
+                          *raw_v = raw_k + kTok * Shape::kRowBytes;
+            int row = row_of(0), next = row_of(1);
             uint32_t kp = parameter(kvq.ks, row), vp = parameter(kvq.vs, row);
-            if (n > 0) {
-                load(kw, kvq.k, row);
-                load(vw, kvq.v, row);
-            }
-            row = row_of(1);
             for (int j = 0; j < n; ++j) {
-                const int s = j % kStages, i = j - kStages;   // (which tiles are free when: as for the copies above)
+                const int s = j % kStages, i = j - kStages;   // (which tiles are free when: as for the copies of a bf16 cache)
                 // A head whose scale is NaN reads as NaN.  A value like that makes its token's key one: the rows that see the token
                 // are NaN by their scores, and no weight of zero meets the value.
                 const bool nan = (vp & 0x7FFFu) >= 0x7F80u;
                 const uint32_t k_par = nan ? kp | 0x7FC0u : kp, v_par = nan ? 0u : vp;
-                const uint32_t kp1 = parameter(kvq.ks, row), vp1 = parameter(kvq.vs, row);
-                if (i >= 0) ok = mbar_wait(k_free + 8 * s, (i / kStages) & 1);
+                kp = parameter(kvq.ks, next);   // (of the next tile)
+                vp = parameter(kvq.vs, next);
+                next = row_of(j + 2);
+                ok = mbar_wait(raw_full, j & 1) && (i < 0 || mbar_wait(k_free + 8 * s, (i / kStages) & 1));
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                store(kw, k_par, sk + s * kTileBytes);
-                publish(k_full + 8 * s);
-                if (j + 1 < n) load(kw, kvq.k, row);
-                if (i >= 0) ok = mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1);
+                decode(raw_k, k_par, k_tiles + s * kTileBytes);
+                publish(k_full + 8 * s, raw_free);
+                ok = mbar_wait(raw_full + 8, j & 1) && (i < 0 || mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1));
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                store(vw, v_par, sv + s * kTileBytes);
-                publish(v_full + 8 * s);
-                if (j + 1 < n) load(vw, kvq.v, row);
-                kp = kp1;
-                vp = vp1;
-                row = row_of(j + 2);
+                decode(raw_v, v_par, v_tiles + s * kTileBytes);
+                publish(v_full + 8 * s, raw_free + 8);
             }
         }
     } else {
         // ---------------- softmax of row tile i: one row per thread ----------------
         if constexpr (kBits == 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int i = (warp - kGroups) >> 2, r = tid & 127, token = r / G;
         const int my_tokens = i ? tokens[1] : tokens[0];
         const bool live = token < my_tokens;   // (the other rows hold anything; they take no part in the votes below)
@@ -859,6 +866,18 @@ bool encode_cache(CUtensorMap* map, const void* cache, const PagedCache& c) {
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same of codes: rows of 128, 64 or 32 bytes, a copy takes a page in the swizzle of that length.
+bool encode_codes(CUtensorMap* map, const void* codes, const PagedCache& c, int bits) {
+    const EncodeFn enc = encode_fn();
+    if (!enc) return false;
+    const cuuint64_t bytes = (cuuint64_t)c.head_dim * bits / 8;
+    const cuuint64_t dims[2] = {bytes, (cuuint64_t)c.num_pages * c.num_kv_heads * c.page_size}, strides[1] = {bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)bytes, (cuuint32_t)c.page_size}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The queries as [total_q][H][D]; a copy takes 64 columns of the G heads of a group for tile_tokens tokens.
 bool encode_queries(CUtensorMap* map, const AttnParams& p) {
     const EncodeFn enc = encode_fn();
@@ -875,9 +894,10 @@ template <int kDim, int kBits>
 qil_status go(const AttnParams& p, const QuantCache& kvq, cudaStream_t st) {
     CUtensorMap mq, mk, mv;
     if (!encode_queries(&mq, p)) return QIL_ERR_CUDA;
-    if (kBits != 16) mk = mv = mq;   // (the codes are read without one)
-    else if (!encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)) return QIL_ERR_CUDA;
-    constexpr int kSmem = ManyShape<kDim>::kSmem;
+    if (kBits == 16 ? !encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)
+                    : !encode_codes(&mk, kvq.k, p.c, kBits) || !encode_codes(&mv, kvq.v, p.c, kBits))
+        return QIL_ERR_CUDA;
+    constexpr int kSmem = ManyShape<kDim, kBits>::kSmem;
     static_assert(kSmem <= 232448, "shared memory per block");
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(attn_many_kernel<kDim, kBits>, kSmem, allowed)) return QIL_ERR_CUDA;
