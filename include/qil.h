@@ -538,6 +538,29 @@ qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const
                               size_t workspace_bytes, qil_stream_t stream);
 
 /* ------------------------------------------------------------------------
+ * qil_sample: one token per row of logits (the policy answers in action tokens, Sec. 2.2), from given uniform numbers.
+ *   logits [B][V] of `type` (QIL_F32, QIL_BF16, QIL_F16), rows `ld` >= 0 elements apart (aligned to their elements only, so
+ *   that a row may be a slice of a wider one; 0: all rows are the same)
+ *   u [B] fp32 in [0, 1)   temperature [B] fp32   top_k [B] int32, top_p [B] fp32, min_p [B] fp32, each optional (null: off)
+ *   out [B] int32
+ * Of row x (a NaN counts as -inf), with m = max x and w_i = exp((x_i - m) / temperature) in 64 bits, rounded to multiples of 2^-42:
+ *   the candidates stand in the order of x, descending, equal ones by index, lowest first;
+ *   top_k: the first k stay (k <= 0 or k >= V: all);  top_p < 1: of those, the ones before which less than top_p times their total
+ *   weight stands;  min_p > 0: of those, the ones with w_i >= min_p;  the first candidate always stays;
+ *   out = the first index, in the order of the vocabulary, at which the running sum of the weights that stay exceeds u times
+ *   their total (of the last one's, where u >= 1).
+ * temperature <= 0 or NaN, top_p <= 0, and min_p > 1 or NaN leave the first candidate alone: the largest logit with the lowest
+ * index.  top_p NaN is off.  Infinite logits share the weight among themselves; a row without a logit above -inf gives -1.
+ * The sums are of whole numbers: a row's token depends on that row and its settings only.
+ * V <= QIL_SAMPLE_MAX_VOCAB (UNSUPPORTED above).
+ * Errors: NULL, SHAPE (sizes, ld < 0), ALIGN (u, temperature, top_k, top_p, min_p, out: 4 bytes; logits: their type), UNSUPPORTED,
+ *   CUDA.
+ * ---------------------------------------------------------------------- */
+#define QIL_SAMPLE_MAX_VOCAB 262144
+qil_status qil_sample(const void* logits, qil_dtype type, long long ld, const float* u, const float* temperature,
+                      const int* top_k, const float* top_p, const float* min_p, int* out, int B, int V, qil_stream_t stream);
+
+/* ------------------------------------------------------------------------
  * Helpers
  * ---------------------------------------------------------------------- */
 const char* qil_status_string(qil_status s);

@@ -28,6 +28,7 @@ SIGNATURES = {
     "qil_kv_read_q": (_i, [_vp] * 4 + [_i] + [_vp] * 5 + [_i] * 7 + [_vp]),
     "qil_attn_paged_q_workspace_size": (_sz, [_i] * 8),
     "qil_attn_paged_q": (_i, [_vp] * 5 + [_i] + [_vp] * 4 + [_i] * 10 + [C.c_float, _vp, _sz, _vp]),
+    "qil_sample": (_i, [_vp, _i, C.c_longlong] + [_vp] * 6 + [_i, _i, _vp]),
     "qil_lora_batch_workspace_size": (_sz, [_i, _i, _i]),
     "qil_lora_batch_add": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, C.c_longlong, C.c_longlong,
                                 C.c_longlong, _vp, _sz, _vp]),

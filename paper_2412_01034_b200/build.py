@@ -15,7 +15,7 @@ BINDING_SOURCE = "torch_binding.cpp"
 SOURCES = ["api.cu", "quantize.cu", "w4a16_general.cu", "w4a16_skinny.cu", "w4a4.cu", "ref_gemv.cu",
            "w4a16_static_ws.cu", "w4a16_tc.cu", "w4a16_prefill.cu", "w8a16.cu", "probe_mma.cu", "igemm_list.cu", "lora_side.cu",
            "rmsnorm.cu", "rope_cache.cu", "attn_paged.cu", "attn_few.cu", "attn_many.cu", "lora_batch.cu", "kv_quant.cu",
-           "attn_few_q.cu"]
+           "attn_few_q.cu", "sample.cu"]
 
 
 def _nvcc() -> str:

@@ -5,6 +5,7 @@
 
 #include "kv_quant.cuh"
 #include "layer_common.cuh"
+#include "sample.cuh"
 
 namespace qil {
 
@@ -408,6 +409,17 @@ qil_status qil_lora_batch_add(const void* x, const void* a, const void* b, const
     if (!workspace || workspace_bytes < lora_batch_workspace(M, num_seqs, rank)) return QIL_ERR_WORKSPACE;
     return launch_lora_batch_add(x, a, b, y, out, cu_q, adapter, scales, M, N, K, rank, num_seqs, num_adapters, ldx, ldy, ldo, workspace,
                                  S(stream));
+}
+
+qil_status qil_sample(const void* logits, qil_dtype type, long long ld, const float* u, const float* temperature, const int* top_k,
+                      const float* top_p, const float* min_p, int* out, int B, int V, qil_stream_t stream) {
+    if (!logits || !u || !temperature || !out) return QIL_ERR_NULL;
+    if (B <= 0 || V <= 0 || ld < 0 || B > (1 << 27)) return QIL_ERR_SHAPE;   // (eight blocks a row)
+    if (!dtype_ok(type) || V > QIL_SAMPLE_MAX_VOCAB) return QIL_ERR_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(logits) & (type == QIL_F32 ? 3u : 1u)) != 0 || !aligned4(u) || !aligned4(temperature) || !aligned4(top_k) ||
+        !aligned4(top_p) || !aligned4(min_p) || !aligned4(out))
+        return QIL_ERR_ALIGN;
+    return launch_sample(logits, type, ld, u, temperature, top_k, top_p, min_p, out, B, V, S(stream));
 }
 
 qil_status qil_linear_w4a16_batch(const qil_linear_desc* descs, int count, void* workspace, size_t workspace_bytes,

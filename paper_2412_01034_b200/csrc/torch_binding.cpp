@@ -318,6 +318,30 @@ PyObject* attn_paged_q(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// sample(logits, u, temperature, top_k, top_p, min_p, out)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, {"logits", "u", "temperature", "top_k", "top_p", "min_p", "out"}, [&]() -> PyObject* {
+        const Tensor& x = tensor(a[0], "logits", 2);
+        const int64_t B = x.size(0), V = x.size(1);
+        const c10::ScalarType type = x.scalar_type();
+        if (type != c10::kFloat && type != c10::kBFloat16 && type != c10::kHalf)
+            throw std::invalid_argument("qil: logits is torch." + type_name(type) + ", expected float32, bfloat16 or float16");
+        if (!x.is_cuda() || (V > 1 && x.stride(1) != 1)) throw std::invalid_argument("qil: the rows of logits have to be contiguous, on a CUDA device");
+        const long long ld = B > 1 ? x.stride(0) : V;   // (the stride of a single row says nothing)
+        const auto optional = [&](PyObject* o, const char* name, c10::ScalarType t) { return o == Py_None ? nullptr : arg(tensor(o, name), name, t, {B}); };
+        float* u = static_cast<float*>(arg(tensor(a[1], "u"), "u", c10::kFloat, {B}));
+        float* t = static_cast<float*>(arg(tensor(a[2], "temperature"), "temperature", c10::kFloat, {B}));
+        int* k = static_cast<int*>(optional(a[3], "top_k", c10::kInt));
+        float* p = static_cast<float*>(optional(a[4], "top_p", c10::kFloat));
+        float* m = static_cast<float*>(optional(a[5], "min_p", c10::kFloat));
+        const Tensor out = a[6] == Py_None ? fresh(x, {B}, c10::kInt) : tensor(a[6], "out");
+        int* po = static_cast<int*>(arg(out, "out", c10::kInt, {B}));
+        const qil_status s = qil_sample(x.data_ptr(), type == c10::kFloat ? QIL_F32 : type == c10::kBFloat16 ? QIL_BF16 : QIL_F16, ld, u, t, k, p, m,
+                                        po, size32(B), size32(V), stream_of(x));
+        return s != QIL_OK ? PyLong_FromLong(s) : wrap(out);
+    });
+}
+
 // lora_batch_add(x, a, b, y, cu_q, adapter, scales, out, workspace)
 PyObject* lora_batch_add(PyObject*, PyObject* const* p, Py_ssize_t n) {
     return guarded(p, n, {"x", "a", "b", "y", "cu_q", "adapter", "scales", "out", "workspace"}, [&]() -> PyObject* {
@@ -346,6 +370,7 @@ PyObject* lora_batch_add(PyObject*, PyObject* const* p, Py_ssize_t n) {
 #define QIL_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {QIL_METHOD(rmsnorm), QIL_METHOD(rope_append), QIL_METHOD(attn_paged), QIL_METHOD(lora_batch_add),
                          QIL_METHOD(rope_append_q), QIL_METHOD(kv_read_q), QIL_METHOD(attn_paged_q),
+                         QIL_METHOD(sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qil_torch", "Marshalling of the qil layer operators.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
