@@ -54,7 +54,7 @@ struct ManyShape {
     static constexpr int kStages = kDim == 128 ? 2 : 4;
     static constexpr int kRowBytes = kDim * kBits / 8;        // of codes; a quantised cache: one tile of those of keys and one of values
     static constexpr int kBars = 2 * kTileBytes + 2 * kStages * kTileBytes + (kBits == 16 ? 0 : 2 * kTok * kRowBytes);
-    static constexpr int kSmem = kBars + 1024 + 256;
+    static constexpr int kSmem = kBars + 1024 + (kBits == 16 ? 256 : 512);
     static constexpr uint32_t kO = 256;                       // tensor memory: S_0, S_1 at 0, 128; O_0, O_1 behind them
     static_assert(kO + 2 * kDim <= 512, "tensor memory");
 };
@@ -203,22 +203,52 @@ __device__ __forceinline__ bool find_pair(const PagedCache& c, int G, int tokens
     return false;
 }
 
-// Codes as bf16 values of the cache, one rounding each: eight of them (16 bytes of the result).
-__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
+// Codes as fp16 values, one rounding each: eight of them (16 bytes of the result).  1024 + n is 0x6400 | n for n < 1024.
+__device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b) {
     uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+template <uint32_t mask>
+__device__ __forceinline__ uint32_t plus1024(uint32_t x) {   // (x & mask) | 0x64006400
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(x), "n"(mask), "n"(0x64006400u));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
 __device__ __forceinline__ uint4 values_of_bytes(uint32_t a, uint32_t b, uint32_t scale2) {
-    const auto pair = [&](uint32_t w, uint32_t pick) { return bf2_mul(bytes02(__byte_perm(w, 0u, pick)), scale2); };
+    const auto pair = [&](uint32_t w, uint32_t pick) {   // 1024 + 128 + code, less 1152
+        return h2_mul(h2_sub(__byte_perm(w ^ 0x80808080u, 0x64646464u, pick), 0x64806480u), scale2);
+    };
     return make_uint4(pair(a, 0x4140), pair(a, 0x4342), pair(b, 0x4140), pair(b, 0x4342));
 }
-__device__ __forceinline__ uint4 values_of_nibbles(uint32_t w, uint32_t zero2, uint32_t scale2) {   // zero2: 128 + zero point, twice
+// zero2: 1024 + zero point, twice; zero16: -(64 + zero point), twice
+__device__ __forceinline__ uint4 values_of_nibbles(uint32_t w, uint32_t zero2, uint32_t zero16, uint32_t scale2) {
     uint32_t x[4];   // elements (e, e + 4)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = bf2_mul(bf2_sub(plus128<0x000F000Fu>(w >> (4 * e)), zero2), scale2);
+    for (int e = 0; e < 4; e += 2) {
+        x[e] = h2_mul(h2_sub(plus1024<0x000F000Fu>(w >> (4 * e)), zero2), scale2);
+        x[e + 1] = h2_mul(h2_fma(plus1024<0x00F000F0u>(w >> (4 * e)), 0x2C002C00u, zero16), scale2);   // (1024 + 16 code) / 16
+    }
     return make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
 }
+// the weights of two tokens in the operands' type
+template <int kBits>
+__device__ __forceinline__ uint32_t pack_weights(float lo, float hi) { return kBits == 16 ? pack2(lo, hi) : pack_half2(lo, hi); }
 
 // Threads: warp 0 copies, warp 1 issues the products, warp 2 clears (warp 3 idles); with a quantised cache four more warps
 // decode it into the operands' tiles; then the two softmax groups.
@@ -241,7 +271,8 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Shape::kBars);
     const uint32_t q_full = smem_u32(bars), s_full = q_full + 16, p_full = q_full + 32, o_done = q_full + 64, v_raw = q_full + 80,
                    drain = q_full + 88, k_full = q_full + 96, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages, raw_full = k_free + 8 * kStages + 8,
-                   raw_free = raw_full + 16;   // (between k_free and raw_full: where tensor memory is)
+                   raw_free = raw_full + 16, q_ready = raw_free + 16, e_full = q_ready + 16;   // (before raw_full: where tensor memory is)
+    int* exponents = reinterpret_cast<int*>(bars + 48);   // (a quantised cache; behind the barriers)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 3 * kStages);
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -256,6 +287,8 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
         for (int i = 0; i < 2 && kBits != 16; ++i) {
             mbar_init(raw_full + 8 * i, 1);     // the copy of a tile of codes
             mbar_init(raw_free + 8 * i, 4);     // the decoding warps
+            mbar_init(q_ready + 8 * i, 4);      // the group's warps: Q_i in fp16
+            mbar_init(e_full, 4);               // the decoding warps: exponents of keys and values
         }
         for (int s = 0; s < kStages; ++s) {
             mbar_init(k_full + 8 * s, kBits == 16 ? 1 : 4);   // a copy, or the decoding warps
@@ -380,8 +413,8 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
         } else if (warp == 1) {
             // ---------------- products ----------------
             if (lane == 0 && n > 0) {
-                // bf16 operands, fp32 accumulators; S: N = 128 tokens, both operands K-major; O: N = kDim, V is N-major
-                constexpr uint32_t kBase = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24);
+                // bf16 (fp16) operands, fp32 accumulators; S: N = 128 tokens, both operands K-major; O: N = kDim, V is N-major
+                constexpr uint32_t kBase = (1u << 4) | (kBits == 16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(kRows >> 4) << 24);
                 constexpr uint32_t kDescS = kBase | ((uint32_t)(kTok >> 3) << 17);
                 constexpr uint32_t kDescO = kBase | (1u << 16) | ((uint32_t)(kDim >> 3) << 17);
                 // 128-byte swizzle, version 1, 8 rows are 1024 bytes; V: the 64-column halves are kHalfBytes apart
@@ -401,7 +434,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                 ok = mbar_wait(k_full, 0);
                 for (int i = 0; i < 2 && ok; ++i) {
                     if ((i ? n1 : n0) == 0) continue;
-                    ok = mbar_wait(q_full + 8 * i, 0);
+                    ok = mbar_wait((kBits == 16 ? q_full : q_ready) + 8 * i, 0);
                     tc_fence_after();
                     if (ok) scores(i, 0);
                 }
@@ -476,10 +509,10 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                 if (row < 0) return 0u;   // (zeros, whatever lies in the place of the codes)
                 return kBits == 8 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(scales) + row) : __ldg(reinterpret_cast<const uint32_t*>(scales) + row);
             };
-            auto decode = [&](const unsigned char* raw, uint32_t par, unsigned char* tile) {
-                const uint32_t scale2 = __byte_perm(par, par, 0x1010);
-                uint32_t zero2 = __byte_perm(par, par, 0x3232);
-                if (kBits == 4) asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(zero2) : "r"(0x43004300u));
+            auto decode = [&](const unsigned char* raw, uint32_t par, int exponent, unsigned char* tile) {
+                const float scale = ldexpf(__uint_as_float(par << 16), -exponent), zero = __uint_as_float(par & 0xFFFF0000u);
+                const uint32_t scale2 = pack_half2(scale, scale);
+                const uint32_t zero2 = pack_half2(1024.f + zero, 1024.f + zero), zero16 = pack_half2(-64.f - zero, -64.f - zero);   // (4 bits)
                 constexpr int kOut = kBits == 8 ? 2 : 4;   // 16-byte pieces of values of a piece of codes
 #pragma unroll
                 for (int x = 0; x < Shape::kRowBytes / 16; ++x) {
@@ -490,10 +523,10 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                         f[0] = values_of_bytes(w.x, w.y, scale2);
                         f[1] = values_of_bytes(w.z, w.w, scale2);
                     } else {
-                        f[0] = values_of_nibbles(w.x, zero2, scale2);
-                        f[1] = values_of_nibbles(w.y, zero2, scale2);
-                        f[kOut - 2] = values_of_nibbles(w.z, zero2, scale2);
-                        f[kOut - 1] = values_of_nibbles(w.w, zero2, scale2);
+                        f[0] = values_of_nibbles(w.x, zero2, zero16, scale2);
+                        f[1] = values_of_nibbles(w.y, zero2, zero16, scale2);
+                        f[kOut - 2] = values_of_nibbles(w.z, zero2, zero16, scale2);
+                        f[kOut - 1] = values_of_nibbles(w.w, zero2, zero16, scale2);
                     }
 #pragma unroll
                     for (int e = 0; e < kOut; ++e) {
@@ -512,6 +545,40 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             };
             unsigned char *k_tiles = smem + 2 * kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes, *raw_k = v_tiles + kStages * kTileBytes,
                           *raw_v = raw_k + kTok * Shape::kRowBytes;
+            // The largest scales of the block's tokens put the values into fp16's range.
+            uint32_t most_k = 0u, most_v = 0u;
+#pragma unroll 1
+            for (int j = 0; j < n; j += 16) {
+                int at[16];
+#pragma unroll
+                for (int x = 0; x < 16; ++x) at[x] = row_of(j + x);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const uint32_t a = parameter(kvq.ks, at[x]) & 0x7FFFu, b = parameter(kvq.vs, at[x]) & 0x7FFFu;
+                    most_k = max(most_k, a < 0x7F80u ? a : 0u);   // (the others are no numbers)
+                    most_v = max(most_v, b < 0x7F80u ? b : 0u);
+                }
+            }
+            most_k = __reduce_max_sync(0xffffffffu, most_k);
+            most_v = __reduce_max_sync(0xffffffffu, most_v);
+            if (lane == 0) {
+                exponents[2 * (warp - 3)] = (int)most_k;   // (behind the results' places)
+                exponents[2 * (warp - 3) + 1] = (int)most_v;
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+            for (int x = 1; x <= 4; ++x) {
+                most_k = max(most_k, (uint32_t)exponents[2 * x]);
+                most_v = max(most_v, (uint32_t)exponents[2 * x + 1]);
+            }
+            const auto exponent_of = [](uint32_t bits) { return bits ? (int)(bits >> 7) - 127 - 8 : 0; };   // scales below 2^9: 127 of them stay below 65504
+            const int k_exponent = exponent_of(most_k), v_exponent = exponent_of(most_v);
+            if (warp == 4 && lane == 0) {
+                exponents[0] = k_exponent;
+                exponents[1] = v_exponent;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(e_full);
             int row = row_of(0), next = row_of(1);
             uint32_t kp = parameter(kvq.ks, row), vp = parameter(kvq.vs, row);
             for (int j = 0; j < n; ++j) {
@@ -526,12 +593,12 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                 ok = mbar_wait(raw_full, j & 1) && (i < 0 || mbar_wait(k_free + 8 * s, (i / kStages) & 1));
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                decode(raw_k, k_par, k_tiles + s * kTileBytes);
+                decode(raw_k, k_par, k_exponent, k_tiles + s * kTileBytes);
                 publish(k_full + 8 * s, raw_free);
                 ok = mbar_wait(raw_full + 8, j & 1) && (i < 0 || mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1));
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                decode(raw_v, v_par, v_tiles + s * kTileBytes);
+                decode(raw_v, v_par, v_exponent, v_tiles + s * kTileBytes);
                 publish(v_full + 8 * s, raw_free + 8);
             }
         }
@@ -544,7 +611,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
         const bool live = token < my_tokens;   // (the other rows hold anything; they take no part in the votes below)
         const int mine = i ? n1 : n0;
         const int see = live ? visible(token0 + i * p.tile_tokens + token) - j0 * kTok : 0x40000000;   // (rows that are no token's never mask)
-        const float scale = p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2);
+        float scale = p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2), value_scale = 1.f;   // of scores and of results
         const uint32_t lane_base = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const uint32_t s_at = lane_base + 128 * i, o_at = lane_base + Shape::kO + (uint32_t)(i * kDim);
         auto publish = [&](int half) {   // this warp's rows of half of P are in tensor memory
@@ -553,6 +620,40 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             __syncwarp();
             if (lane == 0) mbar_arrive(p_full + 16 * i + 8 * half);
         };
+        if constexpr (kBits != 16) {
+            // This thread's query in fp16, divided by the power of two of its largest element (8 bits fit 11; what is 2^-24 of the
+            // largest or less is lost).
+            if (mine > 0) {
+                ok = mbar_wait(q_full + 8 * i, 0);
+                ok = __all_sync(0xffffffffu, ok);
+            }
+            if (mine > 0 && ok) {
+                unsigned char* tile = smem + i * kTileBytes + r * 128;
+                uint32_t most = 0u;
+#pragma unroll
+                for (int x = 0; x < kDim / 8; ++x) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(tile + (x >> 3) * kHalfBytes + ((x ^ r) & 7) * 16);
+                    most = __vmaxu2(most, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+                }
+                most = max(most & 0xFFFFu, most >> 16);
+                const int q_exponent = most >= 0x7F80u || most < 0x80u ? 0 : (int)(most >> 7) - 127;
+                const float down = ldexpf(1.f, -q_exponent);
+#pragma unroll
+                for (int x = 0; x < kDim / 8; ++x) {
+                    uint4* at = reinterpret_cast<uint4*>(tile + (x >> 3) * kHalfBytes + ((x ^ r) & 7) * 16);
+                    float f[8];
+                    unpack8(*at, f);
+                    *at = make_uint4(pack_half2(f[0] * down, f[1] * down), pack_half2(f[2] * down, f[3] * down), pack_half2(f[4] * down, f[5] * down),
+                                     pack_half2(f[6] * down, f[7] * down));
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_ready + 8 * i);
+                ok = mbar_wait(e_full, 0);
+                if (p.scale_log2 != 0.f) scale = ldexpf(scale, exponents[0] + q_exponent);
+                value_scale = ldexpf(1.f, exponents[1]);
+            }
+        }
         float ref = -INFINITY, sum = 0.f;
         for (int j = 0; j < mine && ok; ++j) {
             ok = mbar_wait(s_full + 8 * i, j & 1);
@@ -590,7 +691,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                         b = fast_exp2(b);
                         if (find) top[e & 1] = max3(top[e & 1], __uint_as_float(s[64 + 2 * e]), __uint_as_float(s[64 + 2 * e + 1]));
                         acc[e & 1] = f2_add(acc[e & 1], f2(a, b));
-                        w[e] = pack2(a, b);
+                        w[e] = pack_weights<kBits>(a, b);
                     }
                     tmem_st32(s_at + c / 2, w);
                 };
@@ -648,7 +749,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                         a = fast_exp2(a);
                         b = fast_exp2(b);
                         acc[e & 1] = f2_add(acc[e & 1], f2(a, b));
-                        w[e] = pack2(a, b);
+                        w[e] = pack_weights<kBits>(a, b);
                     }
                     tmem_st32(s_at + c / 2, w);
                     publish(c / 64);
@@ -667,7 +768,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             // group's query tile (8 KB a time, pieces permuted by the row; the tile has been read, the last S is long there)
             // and writes 16 bytes a lane, whole rows at once.
             const bool whole = p.splits == 1;
-            const float inv = 1.f / sum;
+            const float inv = value_scale / sum;
             const size_t items = (size_t)p.c.total_q * H;
             const int item = live ? (q_lo + token0 + i * p.tile_tokens + token) * H + kvh * G + (r - token * G) : 0;   // this thread's (token, head)
             unsigned char* turn = smem + i * kTileBytes + (warp & 3) * (32 * kDim * 2);
@@ -692,8 +793,10 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                     for (int e = 0; e < 16; e += 2)
                         strange[(e >> 1) & 1] = f2_fma(f2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), 0ull, strange[(e >> 1) & 1]);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
+                    for (int e = 0; e < 16; ++e) {
                         if (mine == 0 || sum == 0.f) o[e] = 0u;
+                        if (kBits != 16 && !whole) o[e] = __float_as_uint(__uint_as_float(o[e]) * value_scale);
+                    }
                     if (whole) {
 #pragma unroll
                         for (int e = 0; e < 16; e += 8) {

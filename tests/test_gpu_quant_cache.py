@@ -210,8 +210,9 @@ def check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens, scale=None
             continue
         lo = cu[b]
         k, v = (np_layer.gather_cache(side[0], tab[b], kv) for side in sides)
-        if n * G > 16:   # (values rounded to bf16, as the read-back gives them)
-            k, v = (np_quant_cache.bf16(x.astype(np.float32)).astype(np.float64) for x in (k, v))
+        if n * G > 16 and kv > 0:   # (values and weights have fp16's 11 bits; the largest value is near the end of its range)
+            k, v = (np.ldexp(np.ldexp(x, -e).astype(np.float16).astype(np.float64), e)
+                    for x, e in ((x, int(np.floor(np.log2(np.abs(x).max()))) - 14) for x in (k, v)))
         want, spread, absdot = np_layer.attn(qd[lo:lo + n], k, v, kv - n, scale)
         if bits == 4 and n * G <= 16 and kv > 0:
             # a score is a difference of sums over 128 + code and 128 + zero point: 143 |q| at the most, times the scale
@@ -219,9 +220,12 @@ def check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens, scale=None
             ks = np.stack([s[tab[b, j // cache.k.shape[2]], :, j % cache.k.shape[2]] for j in range(kv)]).max(axis=0)   # [Hk]
             absdot = 143.0 * np.abs(qd[lo:lo + n]).sum(axis=2) * np.repeat(ks, G)[None, :] * abs(scale)
         # as for the bf16 cache: fp32 sums of D products, once in the numerator and once in the sum; a weight times its value's
-        # scale rounded to bf16; exp2 and the sums in fp32
-        weight = BF16_HALF_ULP + 2 * (D + 8) * 2.0 ** -24 * absdot[:, :, None] + 2.0 ** -14
-        assert_within(gd[lo:lo + n], want, BF16_HALF_ULP * np.abs(want) + weight * spread + 1e-30)
+        # scale rounded to bf16 (a weight alone to fp16); exp2 and the sums in fp32
+        weight = (BF16_HALF_ULP if n * G <= 16 else 2.0 ** -11) + 2 * (D + 8) * 2.0 ** -24 * absdot[:, :, None] + 2.0 ** -14
+        tol = BF16_HALF_ULP * np.abs(want) + weight * spread + 1e-30
+        if n * G > 16 and kv > 0:   # a weight below 2^-14 of the reference is off by 2^-25 of it, whatever its size
+            tol += 2.0 ** -25 * np.repeat(np.abs(v).sum(axis=0), G, axis=0)[None]
+        assert_within(gd[lo:lo + n], want, tol)
     return got
 
 
