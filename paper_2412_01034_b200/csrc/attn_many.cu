@@ -499,15 +499,18 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
             const int r = tid & 127;
             const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
-            auto row_of = [&](int j) {   // the row of the cache where this thread's token of tile j lies, or -1
-                const int tok = (j0 + j) * kTok + r;
-                if (j >= n || tok >= end) return -1;
-                const int page = __ldg(table + (tok >> p.page_shift));
-                return page < 0 || page >= p.c.num_pages ? -1 : (page * p.c.num_kv_heads + kvh) * p.c.page_size + (tok & (p.c.page_size - 1));
+            // the row of the cache where this thread's token of tile j lies, or -1 (loads without conditions do not wait for one another)
+            const int last_tok = max(0, min(end, (j0 + n) * kTok) - 1);
+            auto row_of = [&](int j) {
+                const int tok = (j0 + j) * kTok + r, held = min(tok, last_tok), page = __ldg(table + (held >> p.page_shift));
+                const bool there = tok == held && page >= 0 && page < p.c.num_pages;
+                return there ? (page * p.c.num_kv_heads + kvh) * p.c.page_size + (held & (p.c.page_size - 1)) : -1;
             };
             auto parameter = [&](const __nv_bfloat16* scales, int row) -> uint32_t {   // scale, zero point above it
-                if (row < 0) return 0u;   // (zeros, whatever lies in the place of the codes)
-                return kBits == 8 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(scales) + row) : __ldg(reinterpret_cast<const uint32_t*>(scales) + row);
+                const int at = max(row, 0);
+                const uint32_t par = kBits == 8 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(scales) + at)
+                                                : __ldg(reinterpret_cast<const uint32_t*>(scales) + at);
+                return row < 0 ? 0u : par;   // (zeros, whatever lies in the place of the codes)
             };
             auto decode = [&](const unsigned char* raw, uint32_t par, int exponent, unsigned char* tile) {
                 const float scale = ldexpf(__uint_as_float(par << 16), -exponent), zero = __uint_as_float(par & 0xFFFF0000u);
