@@ -4,13 +4,14 @@
 // As in attn_few.cu a block takes `chunk` cached tokens of one request and key head, its four warps take tiles of 16 tokens in
 // turn, each with its own ring in shared memory, and blocks of a request are joined in a cluster or through the workspace.
 // What differs is what a tile costs apart from its bytes, a half or a quarter of those of bf16:
-//   S^T = K Q^T and O^T += V^T P^T: the cache is the 16-row operand of mma.sync 16 x 8 x 16 and the query rows are the 8
-//   columns, so that up to 8 rows take half the products and accumulators of a tile of 16 rows.
-//   Codes become bf16 in registers by a few logic operations, exactly: whole numbers of at most 8 bits.  The operands' columns
-//   may be in any order as long as both sides agree, so a lane's codes are 16 bytes or less in one piece, and the words come
-//   apart in the order that needs the fewest operations (nibbles 0 and 4 of a word are one mask away from a pair).
-//   A key's scale multiplies its scores, a value's scale its weight.  Zero points: S = s (q . (128 + c) - (128 + z) sum q) for
-//   keys; for values, whose sums cancel, 128 + z is taken off every code.
+//   S^T = K Q^T and O^T += V^T P^T: the cache is the 16-row operand of mma.sync and the query rows are the 8 columns, so that up
+//   to 8 rows take half the products and accumulators of a tile of 16 rows.
+//   The integer pipe (masks, shifts, byte selects) is what a tile of codes would be bound by, so keys meet the queries as they
+//   are, in whole numbers: a query row is t (256 h + l) with h and l of 8 bits (off by 2^-16 of the row's largest element at
+//   most), its scores are exact int32 sums, 256 (k . h) + k . l less the zero point times the row's sum.
+//   Values become bf16 in registers by a few logic operations, exactly.  The operands' columns may be in any order as long as both sides agree, so a lane's codes are 16 bytes or
+//   less in one piece, and the words come apart in the order that needs the fewest operations.
+//   A key's scale multiplies its scores, a value's scale its weight.
 //   The running reference of a row is only raised by scores more than 2^8 above it, which a vote finds; maxima are reduced
 //   over the lanes in those tiles alone, sums once at the end.
 // A weight times its value's scale is rounded to bf16 for the product (2^-9 of each at most, of either sign).
@@ -29,7 +30,9 @@ struct FewQ {
     static constexpr int kRowBytes = kDim * kBits / 8;               // 128, 64, 64, 32
     static constexpr int kTileBytes = kTile * kRowBytes;
     static constexpr int kParBytes = kTile * (kBits == 8 ? 2 : 4);   // of one side
-    static constexpr int kStageBytes = 2 * kTileBytes + 2 * kParBytes;
+    static constexpr int kSub = kRowBytes <= 64 ? 2 : 1;             // tiles of one turn of the loop
+    static constexpr int kSubBytes = 2 * kTileBytes + 2 * kParBytes;
+    static constexpr int kStageBytes = kSub * kSubBytes;
     static constexpr int kStages = 13056 / kStageBytes;              // 51 KB a block, four blocks an SM
     static constexpr int kWarpBytes = kStages * kStageBytes;
     static constexpr int kSteps = kDim / 16;
@@ -45,6 +48,12 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
     return (row >> 2) * 128 + (((row & 3) * 2 + piece) ^ ((row >> 1) & 2)) * 16;
 }
 
+// D[16 x 8] += A[16 x 32] B[32 x 8], signed bytes, int32 accumulators
+__device__ __forceinline__ void mma16832(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t d;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
@@ -91,6 +100,7 @@ __device__ __forceinline__ float over_tokens(float v, F f) {
 template <int kDim, int kBits, int kCols, bool kTogether>
 __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_kernel(const AttnQuantParams pq) {
     using Shape = FewQ<kDim, kBits>;
+    constexpr int kSub = Shape::kSub, kTurn = kSub * kTile;   // tokens of a turn
     constexpr int kStages = Shape::kStages, kRowBytes = Shape::kRowBytes, kTileBytes = Shape::kTileBytes, kSteps = Shape::kSteps;
     constexpr int kRows = 8 * kCols, kKeyWords = kRowBytes >= 64 ? 4 : 2, kKeyLoads = kRowBytes == 128 ? 2 : 1, kValWords = kRowBytes / 32;
     const AttnParams& p = pq.a;
@@ -109,7 +119,9 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
     const int begin = split * p.chunk;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
     const int kv = __ldg(p.c.kv_len + seq);
-    int page = __ldg(table + min((begin + warp * kTile) >> p.page_shift, p.c.max_pages - 1));
+    int page[kSub];
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) page[u] = __ldg(table + min((begin + warp * kTurn + u * kTile) >> p.page_shift, p.c.max_pages - 1));
     int row0, row1;
     request_rows(p.c.cu_q, seq, p.c.total_q, row0, row1);
     const int q_len = row1 - row0;
@@ -121,41 +133,49 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
     const bool idle = split >= parts;
     if (idle && !kTogether) return;
     const int stop = idle ? begin : split + 1 == parts ? end : min(begin + p.chunk, end);
-    const int tiles = (stop - begin + kTile - 1) / kTile;
+    const int turns = (stop - begin + kTurn - 1) / kTurn;
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * Shape::kWarpBytes;
-    auto page_of = [&](int i) -> int { return __ldg(table + (min(begin + i * kTile, stop - 1) >> p.page_shift)); };
-    auto fetch = [&](int i, int stage, int page) {
-        const int tok = begin + i * kTile;
-        const uint32_t bytes = page >= 0 && page < p.c.num_pages ? 16u : 0u;   // (a page that does not exist: zeros)
-        const size_t at = bytes ? ((size_t)page * p.c.num_kv_heads + kvh) * p.c.page_size + (tok & (p.c.page_size - 1)) : 0;   // a row of the cache
-        const uint32_t dst = ring + stage * Shape::kStageBytes;
-        const char *k = static_cast<const char*>(pq.kv.k) + at * kRowBytes, *v = static_cast<const char*>(pq.kv.v) + at * kRowBytes;
+    auto pages_of = [&](int i, int (&to)[kSub]) {   // of the tiles of turn i (of the last token where there are none)
 #pragma unroll
-        for (int j = 0; j < kRowBytes / 32; ++j) {
-            const int piece = j * 32 + lane;
-            const uint32_t to = dst + place<kRowBytes>(piece / (kRowBytes / 16), piece % (kRowBytes / 16));
-            cp_async16(to, k + piece * 16, bytes);
-            cp_async16(to + kTileBytes, v + piece * 16, bytes);
-        }
-        constexpr int kPieces = Shape::kParBytes / 16;
-        if (lane < 2 * kPieces) {
-            const char* par = reinterpret_cast<const char*>(lane < kPieces ? pq.kv.ks : pq.kv.vs) + at * (Shape::kParBytes / kTile);
-            cp_async16(dst + 2 * kTileBytes + lane * 16, par + (lane % kPieces) * 16, bytes);
+        for (int u = 0; u < kSub; ++u) to[u] = __ldg(table + (min(begin + i * kTurn + u * kTile, stop - 1) >> p.page_shift));
+    };
+    auto fetch = [&](int i, int stage, const int (&page)[kSub]) {
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+            const int tok = begin + i * kTurn + u * kTile;
+            const uint32_t bytes = page[u] >= 0 && page[u] < p.c.num_pages ? 16u : 0u;   // (a page that does not exist: zeros)
+            const size_t at = bytes ? ((size_t)page[u] * p.c.num_kv_heads + kvh) * p.c.page_size + (tok & (p.c.page_size - 1)) : 0;   // a row of the cache
+            const uint32_t dst = ring + stage * Shape::kStageBytes + u * Shape::kSubBytes;
+            const char *k = static_cast<const char*>(pq.kv.k) + at * kRowBytes, *v = static_cast<const char*>(pq.kv.v) + at * kRowBytes;
+#pragma unroll
+            for (int j = 0; j < kRowBytes / 32; ++j) {
+                const int piece = j * 32 + lane;
+                const uint32_t to = dst + place<kRowBytes>(piece / (kRowBytes / 16), piece % (kRowBytes / 16));
+                cp_async16(to, k + piece * 16, bytes);
+                cp_async16(to + kTileBytes, v + piece * 16, bytes);
+            }
+            constexpr int kPieces = Shape::kParBytes / 16;
+            if (lane < 2 * kPieces) {
+                const char* par = reinterpret_cast<const char*>(lane < kPieces ? pq.kv.ks : pq.kv.vs) + at * (Shape::kParBytes / kTile);
+                cp_async16(dst + 2 * kTileBytes + lane * 16, par + (lane % kPieces) * 16, bytes);
+            }
         }
     };
-
-    int ahead = warp;               // the next tile to fetch
+    int ahead = warp;               // the next turn to fetch
+    auto fetch_ahead = [&](int stage) {
+        if (ahead < turns) {
+            int next[kSub];
+            pages_of(ahead + kWarps, next);   // (asked for one turn ahead of its use)
+            fetch(ahead, stage, page);
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) {
-        if (ahead < tiles) {
-            const int next = page_of(ahead + kWarps);
-            fetch(ahead, s, page);
-            page = next;
+            for (int u = 0; u < kSub; ++u) page[u] = next[u];
         }
         ahead += kWarps;
         asm volatile("cp.async.commit_group;" ::: "memory");
-    }
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) fetch_ahead(s);
 
     // visible tokens of this lane's query rows 8 n + 2 c, 8 n + 2 c + 1
     int see[kCols][2];
@@ -169,33 +189,59 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
     const int all_see = min(first_pos + 1, end);   // every row sees what the first new token sees
 
     // The query rows as the B operand: lane (g, c) holds row 8 n + g in the order in which the codes of lane c come apart.
-    uint32_t qb[kCols][kSteps][2];
-    float total[kCols][2];   // 4 bits: sums of the elements of rows 8 n + 2 c, 8 n + 2 c + 1
+    constexpr int kKSteps = kDim / 32;
+    uint32_t qh[kCols][kKSteps][2], ql[kCols][kKSteps][2];
+    float unit[kCols][2];   // t of rows 8 n + 2 c, 8 n + 2 c + 1, times the scale of the scores
+    int total[kCols][2];    // 4 bits: sums of their whole numbers
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
         const int r = min(8 * n + g, rows - 1), tok = r / G;
         const __nv_bfloat16* row = p.q + ((size_t)(row0 + tok) * H + kvh * G + (r - tok * G)) * kDim;
-        float sum = 0.f;
+        uint4 x[kKSteps];   // elements of this lane, eight to a step
+        float most = 0.f;
+        bool strange = false;
 #pragma unroll
-        for (int s = 0; s < kSteps; s += 2) {   // eight elements
-            const int d = kBits == 4 ? c * (kDim / 4) + 8 * (s / 2) : (s >> 2) * 64 + 16 * c + 4 * (s & 3);
-            const uint4 x = __ldg(reinterpret_cast<const uint4*>(row + d));
-            if (kBits == 4) {   // elements (0, 4), (1, 5); (2, 6), (3, 7)
-                qb[n][s][0] = __byte_perm(x.x, x.z, 0x5410);
-                qb[n][s][1] = __byte_perm(x.x, x.z, 0x7632);
-                qb[n][s + 1][0] = __byte_perm(x.y, x.w, 0x5410);
-                qb[n][s + 1][1] = __byte_perm(x.y, x.w, 0x7632);
-                float f[8];
-                unpack8(x, f);
+        for (int k = 0; k < kKSteps; ++k)
+            x[k] = __ldg(reinterpret_cast<const uint4*>(row + (kBits == 4 ? c * (kDim / 4) + 8 * k : (k >> 1) * 64 + 16 * c + 8 * (k & 1))));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += f[e];
-            } else {            // elements (0, 2), (1, 3) of each word of codes
-                qb[n][s][0] = __byte_perm(x.x, x.y, 0x5410);
-                qb[n][s][1] = __byte_perm(x.x, x.y, 0x7632);
-                qb[n][s + 1][0] = __byte_perm(x.z, x.w, 0x5410);
-                qb[n][s + 1][1] = __byte_perm(x.z, x.w, 0x7632);
+        for (int k = 0; k < kKSteps; ++k) {
+            float f[8];
+            unpack8(x[k], f);
+            strange |= any_not_finite(x[k]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[e]));
+        }
+        if (strange) most = INFINITY;
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        // (a row of numbers near fp32's smallest counts as zeros; one with an element that is none has no scores)
+        const bool whole = most > 1e-30f && most < INFINITY;
+        const float up = whole ? 32512.f / most : 0.f;
+        float t = whole ? most / 32512.f : most < INFINITY ? 0.f : INFINITY - INFINITY;
+        int sum = 0;
+#pragma unroll
+        for (int k = 0; k < kKSteps; ++k) {
+            float f[8];
+            unpack8(x[k], f);
+            uint32_t h[2] = {0u, 0u}, l[2] = {0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int v = __float2int_rn(f[e] * up), low = (int)(signed char)v, high = (v - low) >> 8;
+                sum += v;
+                // 4 bits: elements 0, 2, 4, 6 of a word of codes, then the others; 8 bits: those of one word, then of the next
+                const int word = kBits == 4 ? e & 1 : e >> 2, at = kBits == 4 ? e >> 1 : e & 3;
+                h[word] |= (uint32_t)(high & 0xFF) << (8 * at);
+                l[word] |= (uint32_t)(low & 0xFF) << (8 * at);
+            }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                qh[n][k][w] = h[w];
+                ql[n][k][w] = l[w];
             }
         }
+        t *= p.scale_log2;
+        unit[n][0] = __shfl_sync(0xffffffffu, t, 8 * c);
+        unit[n][1] = __shfl_sync(0xffffffffu, t, 8 * c + 4);
         if (kBits == 4) {
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -204,11 +250,11 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
         }
     }
 
-    float m[kCols][2], l[kCols][2], o[kCols][kSteps][4];
+    float m[kCols][2], ref[kCols][2], l[kCols][2], o[kCols][kSteps][4];   // (ref: m, or zero before anything is seen)
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) m[n][j] = -INFINITY, l[n][j] = 0.f;
+        for (int j = 0; j < 2; ++j) m[n][j] = -INFINITY, ref[n][j] = l[n][j] = 0.f;
 #pragma unroll
         for (int t = 0; t < kSteps; ++t)
 #pragma unroll
@@ -216,92 +262,106 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
     }
 
     int stage = 0, into = kStages - 1;
-    for (int i = warp; i < tiles; i += kWarps) {
-        __syncwarp();               // every lane has read the tile that the next fetch overwrites
-        if (ahead < tiles) {
-            const int next = page_of(ahead + kWarps);   // (asked for one tile ahead of its use)
-            fetch(ahead, into, page);
-            page = next;
-        }
-        ahead += kWarps;
-        asm volatile("cp.async.commit_group;" ::: "memory");
+    for (int i = warp; i < turns; i += kWarps) {
+        __syncwarp();               // every lane has read what the next fetch overwrites
+        fetch_ahead(into);
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
         __syncwarp();
-        const uint32_t kt = ring + stage * Shape::kStageBytes, vt = kt + kTileBytes, kp = kt + 2 * kTileBytes, vp = kp + Shape::kParBytes;
+        const uint32_t turn = ring + stage * Shape::kStageBytes;
 
-        // ---- scores of tokens g and g + 8 for rows 2 c, 2 c + 1
-        float s[kCols][4];
+        // ---- scores of tokens g and g + 8 of each tile for rows 2 c, 2 c + 1
+        float s[kSub][kCols][4], v_scale[kSub][2];
 #pragma unroll
-        for (int n = 0; n < kCols; ++n)
+        for (int u = 0; u < kSub; ++u) {
+            const uint32_t kt = turn + u * Shape::kSubBytes, kp = kt + 2 * kTileBytes, vp = kp + Shape::kParBytes;
+            uint32_t ka[kKSteps][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+            for (int h = 0; h < kKeyLoads; ++h) {
+                uint32_t w[2][kKeyWords];
+                load_words<kRowBytes>(kt, g, h * 64 + c * (4 * kKeyWords), w[0]);
+                load_words<kRowBytes>(kt, g + 8, h * 64 + c * (4 * kKeyWords), w[1]);
 #pragma unroll
-        for (int h = 0; h < kKeyLoads; ++h) {
-            uint32_t w[2][kKeyWords];
-            load_words<kRowBytes>(kt, g, h * 64 + c * (4 * kKeyWords), w[0]);
-            load_words<kRowBytes>(kt, g + 8, h * 64 + c * (4 * kKeyWords), w[1]);
+                for (int x = 0; x < kKeyWords; ++x) {
+                    if constexpr (kBits == 8) {
+                        ka[(kKeyWords * h + x) >> 1][2 * (x & 1)] = w[0][x];
+                        ka[(kKeyWords * h + x) >> 1][2 * (x & 1) + 1] = w[1][x];
+                    } else {
 #pragma unroll
-            for (int x = 0; x < kKeyWords; ++x) {
-                if constexpr (kBits == 8) {
-                    const uint32_t a[4] = {bytes02(w[0][x]), bytes02(w[1][x]), bytes02(w[0][x] >> 8), bytes02(w[1][x] >> 8)};
-#pragma unroll
-                    for (int n = 0; n < kCols; ++n) mma16816(s[n], a, qb[n][kKeyWords * h + x][0], qb[n][kKeyWords * h + x][1]);
-                } else {
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const uint32_t a[4] = {plus128<0x000F000Fu>(w[0][x] >> (8 * y)), plus128<0x000F000Fu>(w[1][x] >> (8 * y)),
-                                               plus128<0x000F000Fu>(w[0][x] >> (8 * y + 4)), plus128<0x000F000Fu>(w[1][x] >> (8 * y + 4))};
-#pragma unroll
-                        for (int n = 0; n < kCols; ++n) mma16816(s[n], a, qb[n][2 * x + y][0], qb[n][2 * x + y][1]);
+                        for (int y = 0; y < 2; ++y) {
+                            ka[x][y] = w[y][x] & 0x0F0F0F0Fu;
+                            ka[x][2 + y] = (w[y][x] >> 4) & 0x0F0F0F0Fu;
+                        }
                     }
                 }
             }
-        }
-        float v_scale[2];
+            int acc[kCols][2][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int at = g + 8 * h;
-            if constexpr (kBits == 8) {
-                const float k_scale = __uint_as_float(lds16(kp + 2 * at) << 16) * p.scale_log2;
-                v_scale[h] = __uint_as_float(lds16(vp + 2 * at) << 16);
+            for (int n = 0; n < kCols; ++n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[n][0][e] = acc[n][1][e] = 0;
+#pragma unroll
+                for (int k = 0; k < kKSteps; ++k) {
+                    mma16832(acc[n][0], ka[k], qh[n][k][0], qh[n][k][1]);
+                    mma16832(acc[n][1], ka[k], ql[n][k][0], ql[n][k][1]);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = g + 8 * h;
+                float k_scale;
+                int zero = 0;
+                if constexpr (kBits == 8) {
+                    k_scale = __uint_as_float(lds16(kp + 2 * at) << 16);
+                    v_scale[u][h] = __uint_as_float(lds16(vp + 2 * at) << 16);
+                } else {
+                    const uint32_t k_par = lds32(kp + 4 * at);
+                    k_scale = __uint_as_float(k_par << 16);
+                    zero = __float2int_rn(__uint_as_float(k_par & 0xFFFF0000u));
+                    v_scale[u][h] = __uint_as_float(lds32(vp + 4 * at) << 16);
+                }
 #pragma unroll
                 for (int n = 0; n < kCols; ++n)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) s[n][2 * h + j] *= k_scale;
-            } else {
-                const uint32_t k_par = lds32(kp + 4 * at);
-                const float k_scale = __uint_as_float(k_par << 16) * p.scale_log2, zero = -128.f - __uint_as_float(k_par & 0xFFFF0000u);
-                v_scale[h] = __uint_as_float(lds32(vp + 4 * at) << 16);
-#pragma unroll
-                for (int n = 0; n < kCols; ++n)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) s[n][2 * h + j] = fmaf(zero, total[n][j], s[n][2 * h + j]) * k_scale;
+                    for (int j = 0; j < 2; ++j) {
+                        const int whole = acc[n][0][2 * h + j] * 256 + acc[n][1][2 * h + j];
+                        s[u][n][2 * h + j] = (float)(kBits == 8 ? whole : whole - zero * total[n][j]) * (k_scale * unit[n][j]);
+                    }
             }
         }
 
         // ---- weights
-        const int tok = begin + i * kTile;
-        const bool masked = tok + kTile > all_see;
+        const int tok = begin + i * kTurn;
+        const bool masked = tok + kTurn > all_see;
+        const auto hidden = [&](int u, int n, int e) { return tok + kTile * u + g + 8 * (e >> 1) >= see[n][e & 1]; };
         if (masked) {
 #pragma unroll
-            for (int n = 0; n < kCols; ++n)
+            for (int u = 0; u < kSub; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (tok + g + 8 * (e >> 1) >= see[n][e & 1]) s[n][e] = -INFINITY;
+                for (int n = 0; n < kCols; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (hidden(u, n, e)) s[u][n][e] = -INFINITY;
         }
+        float top[kCols][2];
         bool raise = false;
 #pragma unroll
         for (int n = 0; n < kCols; ++n)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) raise |= fmaxf(s[n][j], s[n][2 + j]) > m[n][j] + 8.f;
+            for (int j = 0; j < 2; ++j) {
+                top[n][j] = fmaxf(s[0][n][j], s[0][n][2 + j]);
+#pragma unroll
+                for (int u = 1; u < kSub; ++u) top[n][j] = fmaxf(top[n][j], fmaxf(s[u][n][j], s[u][n][2 + j]));
+                raise |= top[n][j] > m[n][j] + 8.f;
+            }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
             for (int n = 0; n < kCols; ++n)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float now = fmaxf(m[n][j], over_tokens(fmaxf(s[n][j], s[n][2 + j]), [](float a, float b) { return fmaxf(a, b); }));
+                    const float now = fmaxf(m[n][j], over_tokens(top[n][j], [](float a, float b) { return fmaxf(a, b); }));
                     const float keep = now == m[n][j] ? 1.f : fast_exp2(m[n][j] - now);
                     m[n][j] = now;
+                    ref[n][j] = now == -INFINITY ? 0.f : now;
                     l[n][j] *= keep;
 #pragma unroll
                     for (int t = 0; t < kSteps; ++t) {
@@ -310,64 +370,70 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
                     }
                 }
         }
-        uint32_t pb[kCols][2];
+        uint32_t pb[kSub][kCols][2];
 #pragma unroll
-        for (int n = 0; n < kCols; ++n) {
-            float w[4];
+        for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float ref = m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1];
-                const float x = fast_exp2(s[n][e] - ref);
-                l[n][e & 1] += x;
-                w[e] = x * v_scale[e >> 1];
+            for (int n = 0; n < kCols; ++n) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = fast_exp2(s[u][n][e] - ref[n][e & 1]);
+                    l[n][e & 1] += x;
+                    w[e] = x * v_scale[u][e >> 1];
+                }
+                if (masked) {   // (a scale behind the last token may be anything)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (hidden(u, n, e)) w[e] = 0.f;
+                }
+                pb[u][n][0] = transpose8(pack2(w[0], w[1]));
+                pb[u][n][1] = transpose8(pack2(w[2], w[3]));
             }
-            if (masked) {   // (a scale behind the last token may be anything)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (tok + g + 8 * (e >> 1) >= see[n][e & 1]) w[e] = 0.f;
-            }
-            pb[n][0] = transpose8(pack2(w[0], w[1]));
-            pb[n][1] = transpose8(pack2(w[2], w[3]));
-        }
 
-        // ---- weighted values: lane g holds elements g D / 8 ... of the tile's tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-        uint32_t w[4][kValWords];
+        // ---- weighted values: lane g holds elements g D / 8 ... of a tile's tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
 #pragma unroll
-        for (int x = 0; x < 4; ++x) load_words<kRowBytes>(vt, 2 * c + (x & 1) + 8 * (x >> 1), g * (4 * kValWords), w[x]);
-        if constexpr (kBits == 8) {
+        for (int u = 0; u < kSub; ++u) {
+            const uint32_t vt = turn + u * Shape::kSubBytes + kTileBytes, vp = vt + kTileBytes + Shape::kParBytes;
+            uint32_t w[4][kValWords];
 #pragma unroll
-            for (int x = 0; x < kValWords; ++x)
+            for (int x = 0; x < 4; ++x) load_words<kRowBytes>(vt, 2 * c + (x & 1) + 8 * (x >> 1), g * (4 * kValWords), w[x]);
+            if constexpr (kBits == 8) {
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {   // elements 4 x + 2 y, 4 x + 2 y + 1: bytes 0 and 1 of a word of both tokens
-                    const uint32_t lo = __byte_perm(w[0][x], w[1][x], y ? 0x7632 : 0x5410), hi = __byte_perm(w[2][x], w[3][x], y ? 0x7632 : 0x5410);
-                    const uint32_t a[4] = {bytes02(lo), bytes02(lo >> 8), bytes02(hi), bytes02(hi >> 8)};
+                for (int x = 0; x < kValWords; ++x)
 #pragma unroll
-                    for (int n = 0; n < kCols; ++n) mma16816(o[n][2 * x + y], a, pb[n][0], pb[n][1]);
-                }
-        } else {
-            uint32_t zero[2];   // 128 + zero points of tokens 2 c, 2 c + 1 and 2 c + 8, 2 c + 9
+                    for (int y = 0; y < 2; ++y) {   // elements 4 x + 2 y, 4 x + 2 y + 1: bytes 0 and 1 of a word of both tokens
+                        const uint32_t lo = __byte_perm(w[0][x], w[1][x], y ? 0x7632 : 0x5410), hi = __byte_perm(w[2][x], w[3][x], y ? 0x7632 : 0x5410);
+                        const uint32_t a[4] = {bytes02(lo), bytes02(lo >> 8), bytes02(hi), bytes02(hi >> 8)};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint2 par = lds64(vp + 4 * (2 * c + 8 * h));
-                uint32_t z = __byte_perm(par.x, par.y, 0x7632);
-                // (behind the last token it may be anything, and the weight of zero must not meet a NaN)
-                asm("min.bf16x2 %0, %0, %1;" : "+r"(z) : "r"(0x41704170u));
-                asm("max.bf16x2 %0, %0, %1;" : "+r"(z) : "r"(0u));
-                asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(zero[h]) : "r"(z), "r"(0x43004300u));
-            }
-#pragma unroll
-            for (int x = 0; x < kValWords; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {   // half a word of both tokens: elements 8 x + 4 y ...
-                    const uint32_t lo = __byte_perm(w[0][x], w[1][x], y ? 0x7632 : 0x5410), hi = __byte_perm(w[2][x], w[3][x], y ? 0x7632 : 0x5410);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t a[4] = {bf2_sub(plus128<0x000F000Fu>(lo >> (8 * e)), zero[0]), bf2_sub(plus128<0x000F000Fu>(lo >> (8 * e + 4)), zero[0]),
-                                               bf2_sub(plus128<0x000F000Fu>(hi >> (8 * e)), zero[1]), bf2_sub(plus128<0x000F000Fu>(hi >> (8 * e + 4)), zero[1])};
-#pragma unroll
-                        for (int n = 0; n < kCols; ++n) mma16816(o[n][4 * x + 2 * y + e], a, pb[n][0], pb[n][1]);
+                        for (int n = 0; n < kCols; ++n) mma16816(o[n][2 * x + y], a, pb[u][n][0], pb[u][n][1]);
                     }
+            } else {
+                uint32_t zero[2];   // 128 + zero points of tokens 2 c, 2 c + 1 and 2 c + 8, 2 c + 9
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint2 par = lds64(vp + 4 * (2 * c + 8 * h));
+                    uint32_t z = __byte_perm(par.x, par.y, 0x7632);
+                    if (masked) {   // (behind the last token it may be anything, and the weight of zero must not meet a NaN)
+                        asm("min.bf16x2 %0, %0, %1;" : "+r"(z) : "r"(0x41704170u));
+                        asm("max.bf16x2 %0, %0, %1;" : "+r"(z) : "r"(0u));
+                    }
+                    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(zero[h]) : "r"(z), "r"(0x43004300u));
                 }
+#pragma unroll
+                for (int x = 0; x < kValWords; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {   // half a word of both tokens: elements 8 x + 4 y ...
+                        const uint32_t lo = __byte_perm(w[0][x], w[1][x], y ? 0x7632 : 0x5410), hi = __byte_perm(w[2][x], w[3][x], y ? 0x7632 : 0x5410);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t a[4] = {bf2_sub(plus128<0x000F000Fu>(lo >> (8 * e)), zero[0]), bf2_sub(plus128<0x000F000Fu>(lo >> (8 * e + 4)), zero[0]),
+                                                   bf2_sub(plus128<0x000F000Fu>(hi >> (8 * e)), zero[1]), bf2_sub(plus128<0x000F000Fu>(hi >> (8 * e + 4)), zero[1])};
+#pragma unroll
+                            for (int n = 0; n < kCols; ++n) mma16816(o[n][4 * x + 2 * y + e], a, pb[u][n][0], pb[u][n][1]);
+                        }
+                    }
+            }
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
         into = into + 1 == kStages ? 0 : into + 1;
