@@ -2,8 +2,9 @@
 of requests that are at different places: prompts, chunks of prompts and single tokens together.
 
 The linears are the library's (4-bit weight-only; the fused query / key / value projection optionally W8A8), and what lies
-between them runs on its layer operators: residual norm, rotary embedding with append to the paged cache, attention over
-the cache, low-rank adapters per request.  Weights are quantised on the device once; ``forward`` only enqueues kernels.
+between them runs on its layer operators: residual norm, rotary embedding with append to the paged cache (bf16, or quantised
+to 8 or 4 bits as it is written), attention over the cache, low-rank adapters per request.  ``TokenHead`` ends a step: norm,
+head and the next token of every request.  Weights are quantised on the device once; ``forward`` only enqueues kernels.
 """
 from __future__ import annotations
 
@@ -65,11 +66,15 @@ def linear_workspace_size(max_tokens, linears, gate_up, linears8=()):
 class DecoderLayer:
     """weights: fp32 CUDA tensors norm1, norm2 [hidden], qkv [(H + 2 Hk) D][hidden], o [hidden][H D], gate, up [ffn][hidden],
     down [hidden][ffn].  adapters: None or (a [n][r][hidden], b [n][(H + 2 Hk) D][r], scales [n]) beside the qkv projection.
+    kv_bits: 16 (bf16 cache: k_cache, v_cache), 8 or 4 (quantised cache: cache).
     The caches and workspaces are the layer's own: its calls belong on one stream, or have to be ordered by the caller.
     Steps may be captured in CUDA graphs."""
 
     def __init__(self, weights, heads, kv_heads, head_dim, num_pages, page_size, max_pos, max_tokens, qkv_bits=4, adapters=None,
-                 eps=1e-5, theta=10000.0):
+                 eps=1e-5, theta=10000.0, kv_bits=16):
+        if kv_bits not in (16, 8, 4):
+            raise ValueError(f"kv_bits is {kv_bits}, expected 16, 8 or 4")
+        self.kv_bits = kv_bits
         self.heads, self.kv_heads, self.head_dim, self.eps, self.qkv_bits = heads, kv_heads, head_dim, eps, qkv_bits
         self.norm1, self.norm2 = (weights[n].to(torch.bfloat16) for n in ("norm1", "norm2"))
         if qkv_bits == 8:
@@ -81,7 +86,10 @@ class DecoderLayer:
         self.gate_up = Linear4(api.interleave_rows(weights["gate"], weights["up"]))
         self.adapters = adapters
         self.cos_sin = api.rope_table(max_pos, head_dim, theta)
-        self.k_cache, self.v_cache = api.new_kv_cache(num_pages, kv_heads, page_size, head_dim)
+        if kv_bits == 16:
+            self.k_cache, self.v_cache = api.new_kv_cache(num_pages, kv_heads, page_size, head_dim)
+        else:
+            self.cache = api.new_kv_cache_q(num_pages, kv_heads, page_size, head_dim, kv_bits)
         # one workspace for all linears of the layer (they run one after another)
         self.workspace = api.new_workspace(linear_workspace_size(
             max_tokens, [(lin.N, lin.K) for lin in (self.o, self.down) + (() if qkv_bits == 8 else (self.qkv,))],
@@ -97,7 +105,9 @@ class DecoderLayer:
     def _attn_workspace(self, tokens, requests, max_q, max_kv):
         """The attention's workspace for such a batch: the newest one if it is large enough, or a larger one.  The older ones
         stay (each is at least twice the one before), because a captured graph may hold them."""
-        need = api.attn_paged_workspace_size(tokens, requests, self.heads, self.kv_heads, self.head_dim, max_q, max_kv)
+        sizes = (tokens, requests, self.heads, self.kv_heads, self.head_dim)
+        need = (api.attn_paged_workspace_size(*sizes, max_q, max_kv) if self.kv_bits == 16 else
+                api.attn_paged_q_workspace_size(*sizes, self.kv_bits, max_q, max_kv))
         held = self._attn_workspaces[-1].numel() if self._attn_workspaces else 0
         if held < need:
             if torch.cuda.is_current_stream_capturing():
@@ -132,15 +142,56 @@ class DecoderLayer:
                                workspace=self.lora_workspace if x.shape[0] <= self.max_tokens else None)
         return qkv, residual
 
+    def _attention(self, qkv, batch):
+        """The rotation, the append to the cache and the attention over it."""
+        where = (batch.cu_q, batch.kv_len, batch.block_table)
+        workspace = self._attn_workspace(qkv.shape[0], batch.kv_len.shape[0], batch.max_q, batch.max_kv)
+        if self.kv_bits == 16:
+            q = api.rope_append(qkv, self.cos_sin, self.k_cache, self.v_cache, *where, self.heads)
+            return api.attn_paged(q, self.k_cache, self.v_cache, *where, batch.max_q, batch.max_kv, workspace=workspace)
+        q = api.rope_append_q(qkv, self.cos_sin, self.cache, *where, self.heads)
+        return api.attn_paged_q(q, self.cache, *where, batch.max_q, batch.max_kv, workspace=workspace)
+
+    def read_cache(self, kv_lens, tables):
+        """What the quantised cache holds of requests with these lengths and pages (a request that moves to another worker):
+        (k, v), bf16 [sum of the lengths][kv_heads][head_dim], one request after another."""
+        if self.kv_bits == 16:
+            raise ValueError("a bf16 cache is read as it is: k_cache, v_cache")
+        whole = Requests.of(kv_lens, kv_lens, tables, [-1] * len(kv_lens))
+        return api.kv_read_q(self.cache, whole.cu_q, whole.kv_len, whole.block_table, sum(kv_lens))
+
     def forward(self, h, residual, batch: Requests):
         """h [T][hidden]: the layer's input (residual None) or the part of it that is still to be added to residual.
         Returns the same pair for the next layer."""
         qkv, residual = self._qkv(h, residual, batch)
-        q = api.rope_append(qkv, self.cos_sin, self.k_cache, self.v_cache, batch.cu_q, batch.kv_len, batch.block_table, self.heads)
-        a = api.attn_paged(q, self.k_cache, self.v_cache, batch.cu_q, batch.kv_len, batch.block_table, batch.max_q, batch.max_kv,
-                           workspace=self._attn_workspace(q.shape[0], batch.kv_len.shape[0], batch.max_q, batch.max_kv))
+        a = self._attention(qkv, batch)
         o = self.o(a.view(a.shape[0], -1), self.workspace)
         x, residual = api.rmsnorm(o, self.norm2, self.eps, residual=residual)
         g = api.linear_w4a16_swiglu(x, self.gate_up.packed, self.gate_up.scales, self.gate_up.zeros, self.gate_up.N, GROUP,
                                     workspace=self.workspace)
         return self.down(g, self.workspace), residual
+
+
+class TokenHead:
+    """The end of a step: the norm of each request's last row, a 4-bit head, and the next token.  norm [hidden], w [V][hidden], fp32
+    CUDA tensors.  tokens: (first, past the last) of the vocabulary to choose from (a policy's action tokens), None for all."""
+
+    def __init__(self, norm, w, max_requests, tokens=None, eps=1e-5):
+        self.norm, self.eps, self.head = norm.to(torch.bfloat16), eps, Linear4(w)
+        self.tokens = (0, w.shape[0]) if tokens is None else tokens
+        if not 0 <= self.tokens[0] < self.tokens[1] <= w.shape[0]:
+            raise ValueError(f"tokens is {tokens}, expected a range within {w.shape[0]}")
+        self.workspace = api.new_workspace(max([256] + [api.linear_w4a16_workspace_size(M, *w.shape, GROUP) for M in range(1, max_requests + 1)]))
+
+    def logits(self, h, residual, batch: Requests):
+        """bf16 [requests][V] of every request's last row (h and residual as the last layer returns them).  The row of a request
+        without new tokens says nothing."""
+        last = (batch.cu_q[1:] - 1).clamp_(min=0)
+        x, _ = api.rmsnorm(h.index_select(0, last), self.norm, self.eps, residual=residual.index_select(0, last))
+        return self.head(x, self.workspace)
+
+    def forward(self, h, residual, batch: Requests, u, temperature, top_k=None, top_p=None, min_p=None):
+        """The next tokens, int32 [requests], from uniform numbers u [requests] and the requests' settings (see api.sample)."""
+        first, end = self.tokens
+        chosen = api.sample(self.logits(h, residual, batch)[:, first:end], u, temperature, top_k, top_p, min_p)
+        return chosen + first if first else chosen
