@@ -18,27 +18,36 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// 8 codes of 8 values as bytes or nibbles.  Rounding to the nearest, ties to even, as rint does.
-template <int kBits>
-__device__ __forceinline__ int code_of(float v, float s, int z) {
-    const int q = __float2int_rn(__fdiv_rn(v, s)) + z;
-    return kBits == 8 ? min(max(q, -128), 127) : min(max(q, 0), 15);
+// rint(v / s) + 1.5 2^23.  The quotient by Markstein's theorem (IBM J. Res. Dev. 34, 1990): with the correctly rounded reciprocal
+// one residual step gives the correctly rounded quotient, as long as the residual is not subnormal.
+constexpr float kMagic = 12582912.f;
+__device__ __forceinline__ float rounded(float v, float s, float inv) {
+    const float q = v * inv;
+    return fmaf(fmaf(-q, s, v), inv, q) + kMagic;
 }
-__device__ __forceinline__ uint32_t nibbles8(const int (&q)[8]) {
-    uint32_t w = 0;
+__device__ __forceinline__ uint2 bytes8(const float (&t)[8]) {
+    uint32_t w[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w |= (uint32_t)q[e] << (4 * e);
-    return w;
-}
-__device__ __forceinline__ uint2 bytes8(const int (&q)[8]) {
-    uint32_t w[2] = {0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(q[e] & 0xFF) << (8 * (e & 3));
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo = __byte_perm(__float_as_uint(t[4 * h]), __float_as_uint(t[4 * h + 1]), 0x0040);
+        const uint32_t hi = __byte_perm(__float_as_uint(t[4 * h + 2]), __float_as_uint(t[4 * h + 3]), 0x0040);
+        w[h] = __byte_perm(lo, hi, 0x5410);
+    }
     return make_uint2(w[0], w[1]);
+}
+// (t - kMagic + z, at most 15, for each of eight: whole numbers below 2^16 are exact on the way)
+__device__ __forceinline__ uint32_t nibbles8(const float (&t)[8], float z) {
+    float q[8], w[2];
+    const float less = z - kMagic;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = fminf(t[e] + less, 15.f);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[h] = fmaf(fmaf(fmaf(q[4 * h + 3], 16.f, q[4 * h + 2]), 16.f, q[4 * h + 1]), 16.f, q[4 * h]) + kMagic;
+    return __byte_perm(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x5410);
 }
 
 template <int kDim, int kBits>
-__global__ void __launch_bounds__(kThreads) rope_append_q_kernel(const __nv_bfloat16* __restrict__ qkv, const float* __restrict__ cos_sin,
+__global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_bfloat16* __restrict__ qkv, const float* __restrict__ cos_sin,
                                                                  __nv_bfloat16* __restrict__ q_out, QuantCache kvq, PagedCache c, int max_pos,
                                                                  int pieces) {
     constexpr int kHalf = kDim / 2, kPer = kHalf / 8;   // threads of a head: 8 pairs or 16 values each
@@ -93,36 +102,48 @@ __global__ void __launch_bounds__(kThreads) rope_append_q_kernel(const __nv_bflo
             v[e] = b[e];
         }
     }
-    // the head's range over its threads (the largest |v| as bits: a NaN is above infinity)
-    uint32_t most = 0u;
-    float low = 0.f, high = 0.f;
+    // the head's range over its threads
+    float low = 0.f, high = 0.f, nan = 0.f;   // (8 bits: high alone, of |v|; nan: zero, or a NaN where a value is not finite)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        most = max(most, max(__float_as_uint(u[e]) & 0x7FFFFFFFu, __float_as_uint(v[e]) & 0x7FFFFFFFu));
-        low = fminf(low, fminf(u[e], v[e]));
-        high = fmaxf(high, fmaxf(u[e], v[e]));
+        nan = fmaf(u[e], 0.f, fmaf(v[e], 0.f, nan));
+        if (kBits == 8) {
+            high = fmaxf(high, fmaxf(fabsf(u[e]), fabsf(v[e])));
+        } else {
+            low = fminf(low, fminf(u[e], v[e]));
+            high = fmaxf(high, fmaxf(u[e], v[e]));
+        }
     }
+    high += nan;   // (stays a NaN in the maxima below by its bits: above infinity's)
+    uint32_t most = __float_as_uint(fabsf(high));
     const unsigned mine = ((1u << kPer) - 1u) << (threadIdx.x & 31 & ~(kPer - 1));
 #pragma unroll
     for (int x = 1; x < kPer; x <<= 1) {
         most = max(most, __shfl_xor_sync(mine, most, x));
-        if (kBits == 4) {
-            low = fminf(low, __shfl_xor_sync(mine, low, x));
-            high = fmaxf(high, __shfl_xor_sync(mine, high, x));
-        }
+        if (kBits == 4) low = fminf(low, __shfl_xor_sync(mine, low, x));
     }
-    const float exact = kBits == 8 ? __fdiv_rn(__uint_as_float(most), 127.f) : __fdiv_rn(__fsub_rn(high, low), 15.f);
-    __nv_bfloat16 scale = __float2bfloat16_rn(exact);
-    float s = __bfloat162float(scale);
-    const bool strange = most >= 0x7F800000u || !(s < INFINITY), none = s < 1.17549435e-38f;
+    high = __uint_as_float(most);
+    const float exact = kBits == 8 ? __fdiv_rn(high, 127.f) : __fdiv_rn(__fsub_rn(high, low), 15.f);
+    float s = __bfloat162float(__float2bfloat16_rn(exact));
+    const bool strange = !(high < INFINITY) || !(s < INFINITY), none = s < 1.17549435e-38f;
     if (strange || none) s = 1.f;
     const bool codes = !strange && !none;
-    const int z = kBits == 4 && codes ? min(max(__float2int_rn(__fdiv_rn(-low, s)), 0), 15) : 0;
-    int qu[8], qv[8];
+    // (v / s is below 127.5, or 15.1: the scale is rounded by 2^-9 at most; only rint(v / s) + z can be one too large)
+    const float inv = codes ? __frcp_rn(s) : 0.f;
+    float z = 0.f;
+    if (kBits == 4 && codes) z = rintf(__fdiv_rn(-low, s));
+    float qu[8], qv[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        qu[e] = codes ? code_of<kBits>(u[e], s, z) : 0;
-        qv[e] = codes ? code_of<kBits>(v[e], s, z) : 0;
+    for (int e = 0; e < 8; ++e) {   // (no codes: 0 times whatever it is may be a NaN)
+        qu[e] = rounded(codes ? u[e] : 0.f, s, inv);
+        qv[e] = rounded(codes ? v[e] : 0.f, s, inv);
+    }
+    if (codes && s < 7.9e-31f) {   // (2^-100)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            qu[e] = rintf(__fdiv_rn(u[e], s)) + kMagic;
+            qv[e] = rintf(__fdiv_rn(v[e], s)) + kMagic;
+        }
     }
     if (kBits == 8) {
         unsigned char* dst = static_cast<unsigned char*>(turn ? kvq.k : kvq.v) + row * kDim;
@@ -136,17 +157,17 @@ __global__ void __launch_bounds__(kThreads) rope_append_q_kernel(const __nv_bflo
     } else {
         uint32_t* dst = static_cast<uint32_t*>(turn ? kvq.k : kvq.v) + row * (kDim / 8);
         if (turn) {
-            dst[o / 8] = nibbles8(qu);
-            dst[(o + kHalf) / 8] = nibbles8(qv);
+            dst[o / 8] = nibbles8(qu, z);
+            dst[(o + kHalf) / 8] = nibbles8(qv, z);
         } else {
-            *reinterpret_cast<uint2*>(dst + 2 * o / 8) = make_uint2(nibbles8(qu), nibbles8(qv));
+            *reinterpret_cast<uint2*>(dst + 2 * o / 8) = make_uint2(nibbles8(qu, z), nibbles8(qv, z));
         }
     }
     if (o == 0) {
         const uint32_t held_scale = strange ? 0x7FC0u : __float_as_uint(s) >> 16;   // (s is a bf16 value)
         __nv_bfloat16* to = turn ? kvq.ks : kvq.vs;
         if (kBits == 8) reinterpret_cast<uint16_t*>(to)[row] = (uint16_t)held_scale;
-        else reinterpret_cast<uint32_t*>(to)[row] = held_scale | (__float_as_uint((float)z) & 0xFFFF0000u);
+        else reinterpret_cast<uint32_t*>(to)[row] = held_scale | (__float_as_uint(z) & 0xFFFF0000u);
     }
 }
 
