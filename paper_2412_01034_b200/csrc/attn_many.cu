@@ -52,8 +52,12 @@ struct ManyShape {
     static constexpr int kTileBytes = kTok * kDim * 2;        // Q_i, K and V tiles: 128 rows each
     static constexpr int kHalfBytes = kTok * 128;
     static constexpr int kStages = kDim == 128 ? 2 : 4;
-    static constexpr int kRowBytes = kDim * kBits / 8;        // of codes; a quantised cache: one tile of those of keys and one of values
-    static constexpr int kBars = 2 * kTileBytes + 2 * kStages * kTileBytes + (kBits == 16 ? 0 : 2 * kTok * kRowBytes);
+    static constexpr int kRowBytes = kBits == 16 ? 0 : kDim * kBits / 8;   // of codes
+    // Rows of 128 bytes of codes come through shared memory, a tile of keys and one of values at a time; shorter ones straight into
+    // the registers of the warps that decode them (4096 tokens over 8192, 32 heads of 128: 8 bits 490 us staged, 730 direct, where
+    // two tiles would take 64 registers a thread; 4 bits 542 staged, 515 direct).
+    static constexpr bool kStaged = kRowBytes == 128;
+    static constexpr int kBars = 2 * kTileBytes + 2 * kStages * kTileBytes + (kStaged ? 2 * kTok * kRowBytes : 0);
     static constexpr int kSmem = kBars + 1024 + (kBits == 16 ? 256 : 512);
     static constexpr uint32_t kO = 256;                       // tensor memory: S_0, S_1 at 0, 128; O_0, O_1 behind them
     static_assert(kO + 2 * kDim <= 512, "tensor memory");
@@ -260,6 +264,10 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                                                                          const __grid_constant__ CUtensorMap map_v, const AttnParams p, const QuantCache kvq) {
     using Shape = ManyShape<kDim, kBits>;
     constexpr int kGroups = kBits == 16 ? 4 : 8;   // the first warp of the softmax groups
+    // registers of a thread of the four warps at the front, of those that decode, of the softmax groups (512 with four groups)
+    constexpr int kFrontRegs = kBits == 16 ? 80 : Shape::kStaged ? 40 : 48, kDecodeRegs = Shape::kStaged ? 104 : 112,
+                  kSoftmaxRegs = kBits == 16 ? 208 : Shape::kStaged ? 184 : 176;
+    static_assert(kBits == 16 || kFrontRegs + kDecodeRegs + 2 * kSoftmaxRegs <= 512, "no more than the block was launched with");
     constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kHalfBytes = Shape::kHalfBytes, kHalves = Shape::kHalves;
     extern __shared__ unsigned char smem_raw[];
     wait_for_earlier_kernels();
@@ -270,8 +278,8 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
     const uint32_t sq = smem_u32(smem), sk = sq + 2 * kTileBytes, sv = sk + kStages * kTileBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Shape::kBars);
     const uint32_t q_full = smem_u32(bars), s_full = q_full + 16, p_full = q_full + 32, o_done = q_full + 64, v_raw = q_full + 80,
-                   drain = q_full + 88, k_full = q_full + 96, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages, raw_full = k_free + 8 * kStages + 8,
-                   raw_free = raw_full + 16, q_ready = raw_free + 16, e_full = q_ready + 16;   // (before raw_full: where tensor memory is)
+                   drain = q_full + 88, k_full = q_full + 96, v_full = k_full + 8 * kStages, k_free = v_full + 8 * kStages, q_ready = k_free + 8 * kStages + 8, e_full = q_ready + 16, raw_full = e_full + 8,
+                   raw_free = raw_full + 16;   // (before q_ready: where tensor memory is)
     int* exponents = reinterpret_cast<int*>(bars + 48);   // (a quantised cache; behind the barriers)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 3 * kStages);
     if (tid == 0) {
@@ -285,9 +293,9 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
         mbar_init(v_raw, 1);                    // the copy of a V tile whose last tokens are still to be cleared
         mbar_init(drain, 1);
         for (int i = 0; i < 2 && kBits != 16; ++i) {
+            mbar_init(q_ready + 8 * i, 4);      // the group's warps: Q_i in fp16
             mbar_init(raw_full + 8 * i, 1);     // the copy of a tile of codes
             mbar_init(raw_free + 8 * i, 4);     // the decoding warps
-            mbar_init(q_ready + 8 * i, 4);      // the group's warps: Q_i in fp16
             mbar_init(e_full, 4);               // the decoding warps: exponents of keys and values
         }
         for (int s = 0; s < kStages; ++s) {
@@ -330,8 +338,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
     }
 
     if (warp < 4) {
-        if constexpr (kBits == 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFrontRegs));
         if (warp == 0) {
             // ---------------- copies: lane = (page of the tile, half of the head's columns) ----------------
             const int page_rows = p.c.page_size, per_tile = kTok / page_rows;
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                 const int page = __ldg(table + tok0 / page_rows + my_page);
                 return page < 0 || page >= p.c.num_pages ? -page_rows : (page * p.c.num_kv_heads + kvh) * page_rows;
             };
-            int row = n > 0 ? first_row(j0 * kTok) : 0;
+            [[maybe_unused]] int row = (kBits == 16 || Shape::kStaged) && n > 0 ? first_row(j0 * kTok) : 0;
             if (lane < 2 && (lane ? n1 : n0) > 0) {   // Q_lane: the heads of the group by tile_tokens tokens, rows in that order
                 mbar_expect_tx(q_full + 8 * lane, (uint32_t)(p.tile_tokens * G * kDim * 2));
 #pragma unroll
@@ -357,7 +364,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                     tma_load_3d(sq + lane * kTileBytes + h * kHalfBytes, &map_q, h * 64, kvh * G, q_lo + token0 + lane * p.tile_tokens,
                                 q_full + 8 * lane);
             }
-            if constexpr (kBits != 16) {
+            if constexpr (Shape::kStaged) {
                 // codes, one tile of keys and one of values at a time: they leave as soon as they are decoded
                 const uint32_t raw = sv + kStages * kTileBytes;
                 int sent = 0;
@@ -383,6 +390,9 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                     if ((i ? n1 : n0) > 0) (void)mbar_wait(q_full + 8 * i, 0);
                 if (sent > 0) (void)mbar_wait(raw_full, ((sent - 1) / 2) & 1);
                 if (sent > 1) (void)mbar_wait(raw_full + 8, (sent / 2 - 1) & 1);
+            } else if constexpr (kBits != 16) {   // (the decoding warps fetch the codes)
+                for (int i = 0; i < 2; ++i)
+                    if ((i ? n1 : n0) > 0) (void)mbar_wait(q_full + 8 * i, 0);
             } else {
                 int k_sent = 0, v_sent = 0;
                 for (int j = 0; j < n; ++j) {
@@ -492,17 +502,16 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             }
         }
     } else if (warp < kGroups) {
-        // ---------------- codes to bf16 operand tiles: a token a thread ----------------
-        // The codes arrive by bulk tensor copies in a swizzle of their own row length and go out in the operands', so that eight
-        // threads that read or write the same piece of eight tokens meet all banks.
+        // ---------------- codes to fp16 operand tiles ----------------
+        // The values of a token's codes are written in the operands' swizzle; the codes of the next tile are on the way meanwhile.
         if constexpr (kBits != 16) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-            const int r = tid & 127;
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
+            constexpr int kRowBytes = Shape::kRowBytes;
             const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
-            // the row of the cache where this thread's token of tile j lies, or -1 (loads without conditions do not wait for one another)
+            // the row of the cache where a token lies, or -1 (loads without conditions do not wait for one another)
             const int last_tok = max(0, min(end, (j0 + n) * kTok) - 1);
-            auto row_of = [&](int j) {
-                const int tok = (j0 + j) * kTok + r, held = min(tok, last_tok), page = __ldg(table + (held >> p.page_shift));
+            auto row_at = [&](int tok) {
+                const int held = min(tok, last_tok), page = __ldg(table + (held >> p.page_shift));
                 const bool there = tok == held && page >= 0 && page < p.c.num_pages;
                 return there ? (page * p.c.num_kv_heads + kvh) * p.c.page_size + (held & (p.c.page_size - 1)) : -1;
             };
@@ -512,54 +521,51 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                                                 : __ldg(reinterpret_cast<const uint32_t*>(scales) + at);
                 return row < 0 ? 0u : par;   // (zeros, whatever lies in the place of the codes)
             };
-            auto decode = [&](const unsigned char* raw, uint32_t par, int exponent, unsigned char* tile) {
-                const float scale = ldexpf(__uint_as_float(par << 16), -exponent), zero = __uint_as_float(par & 0xFFFF0000u);
-                const uint32_t scale2 = pack_half2(scale, scale);
-                const uint32_t zero2 = pack_half2(1024.f + zero, 1024.f + zero), zero16 = pack_half2(-64.f - zero, -64.f - zero);   // (4 bits)
-                constexpr int kOut = kBits == 8 ? 2 : 4;   // 16-byte pieces of values of a piece of codes
-#pragma unroll
-                for (int x = 0; x < Shape::kRowBytes / 16; ++x) {
-                    const int turn = Shape::kRowBytes == 128 ? r & 7 : Shape::kRowBytes == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
-                    const uint4 w = *reinterpret_cast<const uint4*>(raw + r * Shape::kRowBytes + ((x ^ turn) * 16));
-                    uint4 f[kOut];
-                    if (kBits == 8) {
-                        f[0] = values_of_bytes(w.x, w.y, scale2);
-                        f[1] = values_of_bytes(w.z, w.w, scale2);
-                    } else {
-                        f[0] = values_of_nibbles(w.x, zero2, zero16, scale2);
-                        f[1] = values_of_nibbles(w.y, zero2, zero16, scale2);
-                        f[kOut - 2] = values_of_nibbles(w.z, zero2, zero16, scale2);
-                        f[kOut - 1] = values_of_nibbles(w.w, zero2, zero16, scale2);
-                    }
-#pragma unroll
-                    for (int e = 0; e < kOut; ++e) {
-                        const int at = x * kOut + e;
-                        *reinterpret_cast<uint4*>(tile + (at >> 3) * kHalfBytes + r * 128 + (((at ^ r) & 7) * 16)) = f[e];
-                    }
-                }
-            };
-            auto publish = [&](uint32_t full, uint32_t raw_free) {   // this warp's tokens are in shared memory, for the tensor cores to read
+            auto publish = [&](uint32_t full) {   // this warp's tokens are in shared memory, for the tensor cores to read
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(full);
-                    mbar_arrive(raw_free);
-                }
+                if (lane == 0) mbar_arrive(full);
             };
-            unsigned char *k_tiles = smem + 2 * kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes, *raw_k = v_tiles + kStages * kTileBytes,
-                          *raw_v = raw_k + kTok * Shape::kRowBytes;
-            // The largest scales of the block's tokens put the values into fp16's range.
+            unsigned char *k_tiles = smem + 2 * kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes;
+            auto row_of = [&](int j) { return row_at((j0 + j) * kTok + (tid & 127)); };   // this thread's token of tile j
+            int row = row_of(0), next = row_of(1);
+            uint32_t kp = parameter(kvq.ks, row), vp = parameter(kvq.vs, row);
+            // The largest scales of the block's tokens put the values into fp16's range: 16 bytes of them at a time.
             uint32_t most_k = 0u, most_v = 0u;
+            constexpr int kUnit = kBits == 8 ? 8 : 4;   // tokens
+            const int tok0 = j0 * kTok, units = n > 0 ? (last_tok - tok0) / kUnit + 1 : 0;
 #pragma unroll 1
-            for (int j = 0; j < n; j += 16) {
-                int at[16];
+            for (int base = tid & 127; base < units; base += 4 * 128) {
+                int at[4], tok[4];
+                uint4 a[4], b[4];
 #pragma unroll
-                for (int x = 0; x < 16; ++x) at[x] = row_of(j + x);
+                for (int x = 0; x < 4; ++x) {
+                    tok[x] = tok0 + (base + 128 * x) * kUnit;
+                    at[x] = row_at(min(tok[x], last_tok - (last_tok - tok0) % kUnit));
+                }
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const uint32_t a = parameter(kvq.ks, at[x]) & 0x7FFFu, b = parameter(kvq.vs, at[x]) & 0x7FFFu;
-                    most_k = max(most_k, a < 0x7F80u ? a : 0u);   // (the others are no numbers)
-                    most_v = max(most_v, b < 0x7F80u ? b : 0u);
+                for (int x = 0; x < 4; ++x) {
+                    a[x] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(kvq.ks) + (size_t)max(at[x], 0) * (16 / kUnit)));
+                    b[x] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(kvq.vs) + (size_t)max(at[x], 0) * (16 / kUnit)));
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t wa[4] = {a[x].x, a[x].y, a[x].z, a[x].w}, wb[4] = {b[x].x, b[x].y, b[x].z, b[x].w};
+                    const auto take = [&](uint32_t& most, uint32_t bits, bool there) {   // (scales that are no numbers do not count)
+                        bits &= 0x7FFFu;
+                        most = max(most, there && bits < 0x7F80u ? bits : 0u);
+                    };
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool there = at[x] >= 0 && tok[x] + e * (kUnit / 4) <= last_tok;
+                        take(most_k, wa[e], there);
+                        take(most_v, wb[e], there);
+                        if (kBits == 8) {
+                            const bool second = at[x] >= 0 && tok[x] + 2 * e + 1 <= last_tok;
+                            take(most_k, wa[e] >> 16, second);
+                            take(most_v, wb[e] >> 16, second);
+                        }
+                    }
                 }
             }
             most_k = __reduce_max_sync(0xffffffffu, most_k);
@@ -582,33 +588,131 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(e_full);
-            int row = row_of(0), next = row_of(1);
-            uint32_t kp = parameter(kvq.ks, row), vp = parameter(kvq.vs, row);
-            for (int j = 0; j < n; ++j) {
-                const int s = j % kStages, i = j - kStages;   // (which tiles are free when: as for the copies of a bf16 cache)
-                // A head whose scale is NaN reads as NaN.  A value like that makes its token's key one: the rows that see the token
-                // are NaN by their scores, and no weight of zero meets the value.
+            // The parameters of this thread's token of the next tile that it decodes, and on to the one after.  A head whose scale is
+            // NaN reads as NaN.  A value like that makes its token's key one: the rows that see the token are NaN by their scores, and
+            // no weight of zero meets the value.
+            auto parameters = [&](int j, uint32_t& k_par, uint32_t& v_par) {
                 const bool nan = (vp & 0x7FFFu) >= 0x7F80u;
-                const uint32_t k_par = nan ? kp | 0x7FC0u : kp, v_par = nan ? 0u : vp;
-                kp = parameter(kvq.ks, next);   // (of the next tile)
+                k_par = nan ? kp | 0x7FC0u : kp;
+                v_par = nan ? 0u : vp;
+                kp = parameter(kvq.ks, next);
                 vp = parameter(kvq.vs, next);
+                row = next;
                 next = row_of(j + 2);
-                ok = mbar_wait(raw_full, j & 1) && (i < 0 || mbar_wait(k_free + 8 * s, (i / kStages) & 1));
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                decode(raw_k, k_par, k_exponent, k_tiles + s * kTileBytes);
-                publish(k_full + 8 * s, raw_free);
-                ok = mbar_wait(raw_full + 8, j & 1) && (i < 0 || mbar_wait(k_free + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1));
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                decode(raw_v, v_par, v_exponent, v_tiles + s * kTileBytes);
-                publish(v_full + 8 * s, raw_free + 8);
+            };
+            // (which tiles are free when: as for the copies of a bf16 cache)
+            auto k_there = [&](int j) { return j < kStages || mbar_wait(k_free + 8 * (j % kStages), (j / kStages - 1) & 1); };
+            auto v_there = [&](int j) { return j < kStages || mbar_wait(k_free + 8 * ((j + 1) % kStages), ((j + 1 - kStages) / kStages) & 1); };
+            if constexpr (Shape::kStaged) {
+                // a token a thread; eight threads that read or write the same piece of eight tokens meet all banks
+                const int r = tid & 127;
+                unsigned char *raw_k = v_tiles + kStages * kTileBytes, *raw_v = raw_k + kTok * kRowBytes;
+                auto decode = [&](const unsigned char* raw, uint32_t par, int exponent, unsigned char* tile) {
+                    const float scale = ldexpf(__uint_as_float(par << 16), -exponent);
+                    const uint32_t scale2 = pack_half2(scale, scale);
+#pragma unroll
+                    for (int x = 0; x < kRowBytes / 16; ++x) {
+                        const uint4 w = *reinterpret_cast<const uint4*>(raw + r * kRowBytes + ((x ^ r) & 7) * 16);
+                        const uint4 f[2] = {values_of_bytes(w.x, w.y, scale2), values_of_bytes(w.z, w.w, scale2)};
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int at = 2 * x + e;
+                            *reinterpret_cast<uint4*>(tile + (at >> 3) * kHalfBytes + r * 128 + ((at ^ r) & 7) * 16) = f[e];
+                        }
+                    }
+                };
+                for (int j = 0; j < n; ++j) {
+                    const int s = j % kStages;
+                    uint32_t k_par, v_par;
+                    parameters(j, k_par, v_par);
+                    ok = mbar_wait(raw_full, j & 1) && k_there(j);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    decode(raw_k, k_par, k_exponent, k_tiles + s * kTileBytes);
+                    publish(k_full + 8 * s);
+                    if (lane == 0) mbar_arrive(raw_free);
+                    ok = mbar_wait(raw_full + 8, j & 1) && v_there(j);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    decode(raw_v, v_par, v_exponent, v_tiles + s * kTileBytes);
+                    publish(v_full + 8 * s);
+                    if (lane == 0) mbar_arrive(raw_free + 8);
+                }
+            } else {
+                // 32 bytes of codes a lane and turn; lanes of the second half of a row take their two pieces in the other order, so that
+                // eight lanes meet all banks
+                constexpr int kAcross = kRowBytes / 32, kDown = 32 / kAcross, kTurns = 32 / kDown;
+                constexpr int kOut = kBits == 8 ? 2 : 4;   // 16-byte pieces of values of 16 bytes of codes
+                const int across = lane % kAcross, down = lane / kAcross, first = 32 * (warp - 4);
+                const int other = kDim == 128 ? across : 0;   // which of its two pieces comes first
+                auto load = [&](uint4 (&w)[kTurns][2], const void* codes, int row) {
+    #pragma unroll
+                    for (int x = 0; x < kTurns; ++x) {
+                        const int from = max(__shfl_sync(0xffffffffu, row, x * kDown + down), 0);
+                        const uint4* at = reinterpret_cast<const uint4*>(static_cast<const char*>(codes) + (size_t)from * kRowBytes) + 2 * across;
+                        w[x][0] = __ldg(at + other);
+                        w[x][1] = __ldg(at + (other ^ 1));
+                    }
+                };
+                auto decode = [&](const uint4 (&w)[kTurns][2], uint32_t par, int exponent, unsigned char* tile) {
+                    // (of this lane's token; the lanes that decode it fetch them)
+                    const float scale = ldexpf(__uint_as_float(par << 16), -exponent), zero = __uint_as_float(par & 0xFFFF0000u);
+                    const uint32_t mine = pack_half2(scale, zero);
+    #pragma unroll
+                    for (int x = 0; x < kTurns; ++x) {
+                        const uint32_t both = __shfl_sync(0xffffffffu, mine, x * kDown + down), scale2 = __byte_perm(both, both, 0x1010);
+                        uint32_t zero2 = 0u, zero16 = 0u;   // 1024 + zero point, -(64 + zero point)
+                        if (kBits == 4) {
+                            const uint32_t z = __byte_perm(both, both, 0x3232);
+                            zero2 = h2_fma(z, 0x3C003C00u, 0x64006400u);
+                            zero16 = h2_fma(z, 0xBC00BC00u, 0xD400D400u);
+                        }
+                        const int r = first + x * kDown + down;
+    #pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const uint4 c = w[x][y];
+                            uint4 f[kOut];
+                            if (kBits == 8) {
+                                f[0] = values_of_bytes(c.x, c.y, scale2);
+                                f[1] = values_of_bytes(c.z, c.w, scale2);
+                            } else {
+                                f[0] = values_of_nibbles(c.x, zero2, zero16, scale2);
+                                f[1] = values_of_nibbles(c.y, zero2, zero16, scale2);
+                                f[kOut - 2] = values_of_nibbles(c.z, zero2, zero16, scale2);
+                                f[kOut - 1] = values_of_nibbles(c.w, zero2, zero16, scale2);
+                            }
+                            const int at = (2 * across + (y ^ other)) * kOut;   // the first piece of the row's values
+                            unsigned char* to = tile + (at >> 3) * kHalfBytes + r * 128;
+    #pragma unroll
+                            for (int e = 0; e < kOut; ++e) *reinterpret_cast<uint4*>(to + (((at + e) ^ r) & 7) * 16) = f[e];
+                        }
+                    }
+                };
+                uint4 kw[kTurns][2], vw[kTurns][2];
+                if (n > 0) {
+                    load(kw, kvq.k, row);
+                    load(vw, kvq.v, row);
+                }
+                for (int j = 0; j < n; ++j) {
+                    const int s = j % kStages;
+                    uint32_t k_par, v_par;
+                    parameters(j, k_par, v_par);
+                    ok = __all_sync(0xffffffffu, k_there(j));
+                    if (!ok) break;
+                    decode(kw, k_par, k_exponent, k_tiles + s * kTileBytes);
+                    publish(k_full + 8 * s);
+                    if (j + 1 < n) load(kw, kvq.k, row);
+                    ok = __all_sync(0xffffffffu, v_there(j));
+                    if (!ok) break;
+                    decode(vw, v_par, v_exponent, v_tiles + s * kTileBytes);
+                    publish(v_full + 8 * s);
+                    if (j + 1 < n) load(vw, kvq.v, row);
+                }
             }
         }
     } else {
         // ---------------- softmax of row tile i: one row per thread ----------------
-        if constexpr (kBits == 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int i = (warp - kGroups) >> 2, r = tid & 127, token = r / G;
         const int my_tokens = i ? tokens[1] : tokens[0];
         const bool live = token < my_tokens;   // (the other rows hold anything; they take no part in the votes below)
@@ -972,16 +1076,15 @@ bool encode_cache(CUtensorMap* map, const void* cache, const PagedCache& c) {
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same of codes: rows of 128, 64 or 32 bytes, a copy takes a page in the swizzle of that length.
-bool encode_codes(CUtensorMap* map, const void* codes, const PagedCache& c, int bits) {
+// The same of codes in rows of 128 bytes; a copy takes a page.
+bool encode_codes(CUtensorMap* map, const void* codes, const PagedCache& c) {
     const EncodeFn enc = encode_fn();
     if (!enc) return false;
-    const cuuint64_t bytes = (cuuint64_t)c.head_dim * bits / 8;
+    const cuuint64_t bytes = 128;
     const cuuint64_t dims[2] = {bytes, (cuuint64_t)c.num_pages * c.num_kv_heads * c.page_size}, strides[1] = {bytes};
     const cuuint32_t box[2] = {(cuuint32_t)bytes, (cuuint32_t)c.page_size}, estr[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The queries as [total_q][H][D]; a copy takes 64 columns of the G heads of a group for tile_tokens tokens.
@@ -1000,9 +1103,9 @@ template <int kDim, int kBits>
 qil_status go(const AttnParams& p, const QuantCache& kvq, cudaStream_t st) {
     CUtensorMap mq, mk, mv;
     if (!encode_queries(&mq, p)) return QIL_ERR_CUDA;
-    if (kBits == 16 ? !encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c)
-                    : !encode_codes(&mk, kvq.k, p.c, kBits) || !encode_codes(&mv, kvq.v, p.c, kBits))
-        return QIL_ERR_CUDA;
+    mk = mv = mq;   // (codes that come without a copy)
+    if (kBits == 16 && (!encode_cache(&mk, p.k, p.c) || !encode_cache(&mv, p.v, p.c))) return QIL_ERR_CUDA;
+    if (ManyShape<kDim, kBits>::kStaged && (!encode_codes(&mk, kvq.k, p.c) || !encode_codes(&mv, kvq.v, p.c))) return QIL_ERR_CUDA;
     constexpr int kSmem = ManyShape<kDim, kBits>::kSmem;
     static_assert(kSmem <= 232448, "shared memory per block");
     static std::atomic<unsigned long long> allowed{0};

@@ -18,12 +18,13 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// rint(v / s) + 1.5 2^23.  The quotient by Markstein's theorem (IBM J. Res. Dev. 34, 1990): with the correctly rounded reciprocal
-// one residual step gives the correctly rounded quotient, as long as the residual is not subnormal.
+// rint(v / s) + 1.5 2^23 by the reciprocal of s, where that decides: v times it is off by 2^-24 of 128 (8e-6) at most, so that the
+// division itself has to be taken only within 2e-5 of a half (`far` collects the distances from whole numbers).
 constexpr float kMagic = 12582912.f;
-__device__ __forceinline__ float rounded(float v, float s, float inv) {
-    const float q = v * inv;
-    return fmaf(fmaf(-q, s, v), inv, q) + kMagic;
+__device__ __forceinline__ float rounded(float v, float inv, float& far) {
+    const float t = fmaf(v, inv, kMagic);
+    far = fmaxf(far, fabsf(fmaf(v, inv, kMagic - t)));
+    return t;
 }
 __device__ __forceinline__ uint2 bytes8(const float (&t)[8]) {
     uint32_t w[2];
@@ -132,13 +133,13 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_b
     const float inv = codes ? __frcp_rn(s) : 0.f;
     float z = 0.f;
     if (kBits == 4 && codes) z = rintf(__fdiv_rn(-low, s));
-    float qu[8], qv[8];
+    float qu[8], qv[8], far = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {   // (no codes: 0 times whatever it is may be a NaN)
-        qu[e] = rounded(codes ? u[e] : 0.f, s, inv);
-        qv[e] = rounded(codes ? v[e] : 0.f, s, inv);
+        qu[e] = rounded(codes ? u[e] : 0.f, inv, far);
+        qv[e] = rounded(codes ? v[e] : 0.f, inv, far);
     }
-    if (codes && s < 7.9e-31f) {   // (2^-100)
+    if (far > 0.49998f) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             qu[e] = rintf(__fdiv_rn(u[e], s)) + kMagic;

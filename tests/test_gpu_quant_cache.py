@@ -118,6 +118,32 @@ def test_append_of_heads_of_every_kind(api, D, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+def test_append_of_values_half_way_between_codes(api, bits):
+    """Keys whose quotient by the scale is a half, or a few units in the last place beside one: the fp32 division decides.  (Cosines
+    that are the keys themselves and sines of zero give any fp32 key.)"""
+    rows, Hk, D, page = 400, 1, 128, 16
+    rng = np.random.default_rng(7)
+    top = 127 if bits == 8 else 15
+    table = np.zeros((rows, D), dtype=np.float32)
+    for t in range(rows):
+        s = np.float32(np_quant_cache.bf16(np.float32([2.0 ** rng.uniform(-20, 20)]))[0])
+        k = rng.integers(0, top, D // 2)
+        v = ((k + 0.5) * np.float64(s)).astype(np.float32)
+        v = (v.view(np.int32) + rng.integers(-3, 4, D // 2).astype(np.int32)).view(np.float32)
+        v[0] = np.float32(top) * s   # (the scale is s)
+        table[t, : D // 2] = v
+    cs = torch.from_numpy(table).cuda()
+    qkv = torch.ones(rows, 3 * D, dtype=torch.bfloat16, device="cuda")
+    cache = api.new_kv_cache_q(rows // page, Hk, page, D, bits)
+    pages = ints([list(range(rows // page))])
+    api.rope_append_q(qkv, cs, cache, ints([0, rows]), ints([rows]), pages, 1)
+    keys = np.concatenate([table[:, : D // 2], table[:, : D // 2]], axis=1)[:, None]
+    got = parts_of(cache)[0]
+    for held, made in zip(got, np_quant_cache.quantise(keys, bits)):
+        np.testing.assert_array_equal(held.transpose(0, 2, 1, *range(3, held.ndim)).reshape(made.shape), made)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 def test_append_skips_what_has_no_place(api, bits):
     g = gen(1130)
     H, Hk, D, page, pages = 2, 1, 64, 16, 4
