@@ -358,13 +358,17 @@ __device__ static __forceinline__ Hit find_step(Row& r, float hi, float lo, doub
 template <bool kBlocks>
 __device__ static __forceinline__ void gather(Row& r, float hi, float lo, int from, int to) {
     const Steps steps((double)lo, (double)hi);
-    for (int i = threadIdx.x; i < r.n; i += kThreads) {
-        const float v = r.x(i);
-        if (!r.kept(v, i) || v < lo || v > hi) continue;
-        const int b = steps.of(v);
-        if (b < from || b > to) continue;
-        const unsigned at = take_shared(r.mem + kListed);
-        if (at < kCap) sts64(r.mem + kList + 8 * at, (u64)~ordered(v) << 32 | (unsigned)(r.first + i));
+    for (int base = threadIdx.x; base < r.n; base += 4 * kThreads) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = r.x(min(base + e * kThreads, r.n - 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = base + e * kThreads, b = steps.of(v[e]);
+            if (i >= r.n || !r.kept(v[e], i) || v[e] < lo || v[e] > hi || b < from || b > to) continue;
+            const unsigned at = take_shared(r.mem + kListed);
+            if (at < kCap) sts64(r.mem + kList + 8 * at, (u64)~ordered(v[e]) << 32 | (unsigned)(r.first + i));
+        }
     }
     row_sync<kBlocks>();
     if (!kBlocks || r.mine != 0) return;
@@ -664,14 +668,16 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) sample_kernel(const 
     const T* src = logits + (size_t)b * ld + first;
     constexpr int kPer = 16 / (int)sizeof(T);
     const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T))), body = (n - head) / kPer;
-    u64 most = 0, low = 0;   // largest value with the lowest index; smallest finite one (inverted)
+    float best = -INFINITY, least_v = INFINITY;   // (a thread's indices ascend: the first of equal ones stays)
+    int best_at = 0;
     auto take = [&](float v, int i) {
-        v = v == v ? v + 0.f : -INFINITY;   // (one zero)
+        v = fmaxf(v, -INFINITY) + 0.f;   // (a NaN is -inf; one zero)
         sts32(mem + kLogits + 4 * i, __float_as_uint(v));
-        if (v > -INFINITY) {
-            most = Max()(most, (u64)ordered(v) << 32 | ~(unsigned)(first + i));
-            low = Max()(low, ~ordered(v));
+        if (v > best) {
+            best = v;
+            best_at = i;
         }
+        least_v = fminf(least_v, v > -INFINITY ? v : INFINITY);
     };
     for (int i = threadIdx.x; i < head; i += kThreads) take(widen(src[i]), i);
 #pragma unroll 4
@@ -682,6 +688,8 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) sample_kernel(const 
         for (int e = 0; e < kPer; ++e) take(widen(f[e]), head + j * kPer + e);
     }
     for (int i = head + body * kPer + (int)threadIdx.x; i < n; i += kThreads) take(widen(src[i]), i);
+    // largest value with the lowest index; smallest above -inf (inverted); zero: none
+    u64 most = best > -INFINITY ? (u64)ordered(best) << 32 | ~(unsigned)(first + best_at) : 0ull, low = best > -INFINITY ? ~ordered(least_v) : 0ull;
     using S = Sampler<kThreads>;
     typename S::Row r{mem, n, first, blocks, mine, 0, 0, 0.0, 1.4426950408889634 / t, -INFINITY, -INFINITY, -1, least * kOne};
     S::template largest<kBlocks>(r, most, low);
