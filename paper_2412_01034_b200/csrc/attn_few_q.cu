@@ -198,8 +198,7 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
         const int r = min(8 * n + g, rows - 1), tok = r / G;
         const __nv_bfloat16* row = p.q + ((size_t)(row0 + tok) * H + kvh * G + (r - tok * G)) * kDim;
         uint4 x[kKSteps];   // elements of this lane, eight to a step
-        float most = 0.f;
-        bool strange = false;
+        float most = 0.f, nan = 0.f;   // (nan: zero, or a NaN where an element is not finite)
 #pragma unroll
         for (int k = 0; k < kKSteps; ++k)
             x[k] = __ldg(reinterpret_cast<const uint4*>(row + (kBits == 4 ? c * (kDim / 4) + 8 * k : (k >> 1) * 64 + 16 * c + 8 * (k & 1))));
@@ -207,38 +206,46 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
         for (int k = 0; k < kKSteps; ++k) {
             float f[8];
             unpack8(x[k], f);
-            strange |= any_not_finite(x[k]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[e]));
+            for (int e = 0; e < 8; ++e) {
+                most = fmaxf(most, fabsf(f[e]));
+                nan = fmaf(f[e], 0.f, nan);
+            }
         }
-        if (strange) most = INFINITY;
+        most = nan == 0.f ? most : INFINITY;
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         // (a row of numbers near fp32's smallest counts as zeros; one with an element that is none has no scores)
         const bool whole = most > 1e-30f && most < INFINITY;
-        const float up = whole ? 32512.f / most : 0.f;
-        float t = whole ? most / 32512.f : most < INFINITY ? 0.f : INFINITY - INFINITY;
-        int sum = 0;
+        const float up = whole ? __fdividef(32512.f, most) : 0.f;
+        float t = whole ? most * (1.f / 32512.f) : most < INFINITY ? 0.f : INFINITY - INFINITY;
+        if (!whole) {   // (0 times an element that is no number)
+#pragma unroll
+            for (int k = 0; k < kKSteps; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        // v = rint(f up) as the low bits of 1.5 2^23 + v: its lowest byte is l, and the next one of v + 128 is h
+        uint32_t bits = 0u;
 #pragma unroll
         for (int k = 0; k < kKSteps; ++k) {
             float f[8];
+            uint32_t lo[8], hi[8];
             unpack8(x[k], f);
-            uint32_t h[2] = {0u, 0u}, l[2] = {0u, 0u};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int v = __float2int_rn(f[e] * up), low = (int)(signed char)v, high = (v - low) >> 8;
-                sum += v;
-                // 4 bits: elements 0, 2, 4, 6 of a word of codes, then the others; 8 bits: those of one word, then of the next
-                const int word = kBits == 4 ? e & 1 : e >> 2, at = kBits == 4 ? e >> 1 : e & 3;
-                h[word] |= (uint32_t)(high & 0xFF) << (8 * at);
-                l[word] |= (uint32_t)(low & 0xFF) << (8 * at);
+                const float v = fmaf(f[e], up, 12582912.f);
+                lo[e] = __float_as_uint(v);
+                hi[e] = __float_as_uint(v + 128.f);
+                bits += lo[e];
             }
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-                qh[n][k][w] = h[w];
-                ql[n][k][w] = l[w];
+                // 4 bits: elements 0, 2, 4, 6 of a word of codes, then the others; 8 bits: those of one word, then of the next
+                const int a = kBits == 4 ? w : 4 * w, b = kBits == 4 ? 2 : 1;
+                ql[n][k][w] = __byte_perm(__byte_perm(lo[a], lo[a + b], 0x0040), __byte_perm(lo[a + 2 * b], lo[a + 3 * b], 0x0040), 0x5410);
+                qh[n][k][w] = __byte_perm(__byte_perm(hi[a], hi[a + b], 0x0051), __byte_perm(hi[a + 2 * b], hi[a + 3 * b], 0x0051), 0x5410);
             }
         }
+        int sum = (int)(bits - (uint32_t)(kKSteps * 8) * 0x4B400000u);
         t *= p.scale_log2;
         unit[n][0] = __shfl_sync(0xffffffffu, t, 8 * c);
         unit[n][1] = __shfl_sync(0xffffffffu, t, 8 * c + 4);
