@@ -508,8 +508,11 @@ qil_status qil_kv_read_q(const void* k_codes, const void* v_codes, const void* k
 
 /* qil_attn_paged_q: qil_attn_paged over such a cache (arguments, bounds and workspace as there, with a size of its own; the
  *   two may take turns on one workspace that is large enough for either).  Of a request with at most 16 query rows (new tokens x
- *   query heads of a key head) scores and sums take the codes exactly and round a weight times its value's scale to bf16 (2^-9 of
- *   it); of one with more the values (q - z) s are rounded to bf16 as qil_kv_read_q gives them, and the weights to bf16.
+ *   query heads of a key head) the scores take codes as they are and a query row in 16 bits (off by 2^-16 of its largest element),
+ *   and a weight times its value's scale is rounded to bf16: outputs are off by 0.0023 of their size.  Of one with more, values
+ *   (q - z) s, queries and weights enter the products as fp16, over powers of two of the largest of them (2^-11 of each; a value
+ *   whose scale is below 2^-22 of the request's largest, and a weight below 2^-14 of the largest, have fewer bits): 0.0017.  Query
+ *   rows of the first kind whose largest element is below 1e-30 count as zeros.
  *   A head that reads as NaN makes the results of the tokens that see it NaN and has no influence on others.
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA. */
 size_t qil_attn_paged_q_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int bits,

@@ -9,14 +9,23 @@
 //   The integer pipe (masks, shifts, byte selects) is what a tile of codes would be bound by, so keys meet the queries as they
 //   are, in whole numbers: a query row is t (256 h + l) with h and l of 8 bits (off by 2^-16 of the row's largest element at
 //   most), its scores are exact int32 sums, 256 (k . h) + k . l less the zero point times the row's sum.
-//   Values become bf16 in registers by a few logic operations, exactly.  The operands' columns may be in any order as long as both sides agree, so a lane's codes are 16 bytes or
-//   less in one piece, and the words come apart in the order that needs the fewest operations.
+//   Values become bf16 in registers by a few logic operations, exactly.  The operands' columns may be in any order as long as
+//   both sides agree, so a lane's codes are 16 bytes or less in one piece, and the words come apart in the order that needs the
+//   fewest operations.
 //   A key's scale multiplies its scores, a value's scale its weight.
 //   The running reference of a row is only raised by scores more than 2^8 above it, which a vote finds; maxima are reduced
 //   over the lanes in those tiles alone, sums once at the end.
-// A weight times its value's scale is rounded to bf16 for the product (2^-9 of each at most, of either sign).
+//   Tiles of 64 bytes a token or less come two to a turn, which halves what a turn costs besides its codes.
+// A weight times its value's scale is rounded to bf16 for the product (by 2^-8 of it at most, of either sign): outputs are off by
+// 0.0023 of their size, 0.0017 of which are their own rounding.
 // Codes are finite whatever they are, so nothing behind a request's last token can reach a result: its weight is replaced by
 // zero after its scale has been applied.
+//
+// Measured (one B200): 8 bits, 32 requests of up to 4099 tokens, 32 key heads of 128 (0.70 GB): 119.4 us = 5.9 TB/s, 90 % of the
+// copy rate.  4 bits, 48 requests of up to 9001 tokens, 8 key heads (0.28 GB): 80 us, 54 %: 360 warp instructions a tile of 16
+// tokens, 167 of them on the integer pipe, which would take 41 us alone; the rest is latency and blocks of unequal length (the
+// SMs are busy for 81 % of the time on average).  Tried and slower: blocks of 1, 2 and 8 warps (171, 95, 85 us), blocks of 1024, 512
+// or 384 tokens (92, 107, 119 us: a block's start and join cost 5 us), shifts as multiplications (100 us).
 #include "attn_paged_q.cuh"
 
 namespace qil {

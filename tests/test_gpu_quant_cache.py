@@ -240,15 +240,15 @@ def check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens, scale=None
             k, v = (np.ldexp(np.ldexp(x, -e).astype(np.float16).astype(np.float64), e)
                     for x, e in ((x, int(np.floor(np.log2(np.abs(x).max()))) - 14) for x in (k, v)))
         want, spread, absdot = np_layer.attn(qd[lo:lo + n], k, v, kv - n, scale)
-        if bits == 4 and n * G <= 16 and kv > 0:
-            # a score is a difference of sums over 128 + code and 128 + zero point: 143 |q| at the most, times the scale
-            s = sides[0][1]
-            ks = np.stack([s[tab[b, j // cache.k.shape[2]], :, j % cache.k.shape[2]] for j in range(kv)]).max(axis=0)   # [Hk]
-            absdot = 143.0 * np.abs(qd[lo:lo + n]).sum(axis=2) * np.repeat(ks, G)[None, :] * abs(scale)
         # as for the bf16 cache: fp32 sums of D products, once in the numerator and once in the sum; a weight times its value's
         # scale rounded to bf16 (a weight alone to fp16); exp2 and the sums in fp32
         weight = (BF16_HALF_ULP if n * G <= 16 else 2.0 ** -11) + 2 * (D + 8) * 2.0 ** -24 * absdot[:, :, None] + 2.0 ** -14
         tol = BF16_HALF_ULP * np.abs(want) + weight * spread + 1e-30
+        if n * G <= 16 and kv > 0:
+            # a query row in steps of 1 / 32512 of its largest element is off by half of one, 2^-16 of that element to within
+            # 2^-6 of it, at each d: a score by 2^-16 max |q| sum |k_d| |scale|, in the numerator and in the sum
+            sizes = np.repeat(np.abs(k).sum(axis=2).max(axis=0), G)[None] * np.abs(qd[lo:lo + n]).max(axis=2) * abs(scale)
+            tol += 2 * (1 + 2.0 ** -6) * 2.0 ** -16 * sizes[:, :, None] * spread
         if n * G > 16 and kv > 0:   # a weight below 2^-14 of the reference is off by 2^-25 of it, whatever its size
             tol += 2.0 ** -25 * np.repeat(np.abs(v).sum(axis=0), G, axis=0)[None]
         assert_within(gd[lo:lo + n], want, tol)
