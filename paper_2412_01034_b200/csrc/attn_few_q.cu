@@ -105,39 +105,23 @@ __device__ __forceinline__ float over_tokens(float v, F f) {
     return f(v, __shfl_xor_sync(0xffffffffu, v, 16));
 }
 
-// kCols: columns of 8 query rows.  kTogether: the blocks of a request and key head are one cluster.
+// A block of a request, from its rows and the pages of its warps' first tiles on.  kCols: columns of 8 query rows.  kTogether: the
+// blocks of a request and key head are one cluster.
 template <int kDim, int kBits, int kCols, bool kTogether>
-__global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_kernel(const AttnQuantParams pq) {
+__device__ __forceinline__ void attend(const AttnQuantParams& pq, unsigned char* smem, int (&page)[FewQ<kDim, kBits>::kSub], int kv, int row0, int q_len) {
     using Shape = FewQ<kDim, kBits>;
     constexpr int kSub = Shape::kSub, kTurn = kSub * kTile;   // tokens of a turn
     constexpr int kStages = Shape::kStages, kRowBytes = Shape::kRowBytes, kTileBytes = Shape::kTileBytes, kSteps = Shape::kSteps;
     constexpr int kRows = 8 * kCols, kKeyWords = kRowBytes >= 64 ? 4 : 2, kKeyLoads = kRowBytes == 128 ? 2 : 1, kValWords = kRowBytes / 32;
     const AttnParams& p = pq.a;
-    extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
     __shared__ float s_scale[2][kRows];
     __shared__ int s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z, G = p.G, H = p.c.num_heads;
-    // (beside the kernel for many rows, as in attn_few.cu)
-    if (!p.both) wait_for_earlier_kernels();
-    if (seq == p.c.num_seqs) {
-        if (split == 0 && kvh == 0) wait_for_earlier_kernels();
-        return;
-    }
     const int begin = split * p.chunk;
     const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
-    const int kv = __ldg(p.c.kv_len + seq);
-    int page[kSub];
-#pragma unroll
-    for (int u = 0; u < kSub; ++u) page[u] = __ldg(table + min((begin + warp * kTurn + u * kTile) >> p.page_shift, p.c.max_pages - 1));
-    int row0, row1;
-    request_rows(p.c.cu_q, seq, p.c.total_q, row0, row1);
-    const int q_len = row1 - row0;
-    if (q_len <= 0 || q_len * (long long)G > kFewRows) return;
     const int rows = q_len * G, end = cache_end(p.c, kv), first_pos = kv - q_len;
-    // a request with more rows than the bound says is left out
-    if (rows > kRows || (!kTogether && p.slots > 1 && rows > p.few_rows)) return;
     const int parts = max(1, min((end + p.chunk - 1) / p.chunk, p.slots));
     const bool idle = split >= parts;
     if (idle && !kTogether) return;
@@ -581,6 +565,37 @@ __global__ void __launch_bounds__(32 * kWarps, kCols == 1 ? 4 : 3) attn_few_q_ke
         }
         write(at, v, sum);
     }
+}
+
+// kMostCols: columns of the request with the most rows.  In a kernel of two columns a block takes one where its request has no
+// more than eight rows (single tokens beside prompts, grouped heads).
+template <int kDim, int kBits, int kMostCols, bool kTogether>
+__global__ void __launch_bounds__(32 * kWarps, kMostCols == 1 ? 4 : 3) attn_few_q_kernel(const AttnQuantParams pq) {
+    constexpr int kSub = FewQ<kDim, kBits>::kSub;
+    const AttnParams& p = pq.a;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int warp = threadIdx.x >> 5, split = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z;
+    // (beside the kernel for many rows, as in attn_few.cu)
+    if (!p.both) wait_for_earlier_kernels();
+    if (seq == p.c.num_seqs) {
+        if (split == 0 && kvh == 0) wait_for_earlier_kernels();
+        return;
+    }
+    const int begin = split * p.chunk;
+    const int* table = p.c.block_table + (size_t)seq * p.c.max_pages;
+    const int kv = __ldg(p.c.kv_len + seq);
+    int page[kSub];
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) page[u] = __ldg(table + min((begin + (warp * kSub + u) * kTile) >> p.page_shift, p.c.max_pages - 1));
+    int row0, row1;
+    request_rows(p.c.cu_q, seq, p.c.total_q, row0, row1);
+    const int q_len = row1 - row0;
+    if (q_len <= 0 || q_len * (long long)p.G > kFewRows) return;
+    // a request with more rows than the bound says is left out
+    const int rows = q_len * p.G;
+    if (rows > 8 * kMostCols || (!kTogether && p.slots > 1 && rows > p.few_rows)) return;
+    if (kMostCols == 1 || rows <= 8) attend<kDim, kBits, 1, kTogether>(pq, smem, page, kv, row0, q_len);
+    else attend<kDim, kBits, kMostCols, kTogether>(pq, smem, page, kv, row0, q_len);
 }
 
 template <int kDim, int kBits, int kCols, bool kTogether>
