@@ -44,7 +44,13 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int bits, in
         const auto round64 = [](long long n) { return (n + 63) / 64 * 64; };
         long long chunk = round64((max_kv * items + room - 1) / room);
         chunk = chunk < 384 ? 384 : chunk > 2048 ? 2048 : chunk;
-        if (per_row >= 2) {
+        // Beside the kernel for many rows they come up as SMs become free, some beside its blocks and most when those end: a
+        // cluster would wait for its last place, and short blocks fill what is left (512-token chunk and 15 single tokens over
+        // up to 6001, 8 key heads, 8 bits: 107 us with blocks of 1024, 110 with 512, 116 with 2048, 124 to 131 with clusters;
+        // 4 bits: 112, 115, 116, 121 to 128).
+        const bool apart = bits != 16 && pl.many;
+        if (apart && chunk > 1024) chunk = 1024;
+        if (per_row >= 2 && !apart) {
             const long long most = per_row < kMostTogether ? per_row : kMostTogether;
             const long long of = round64((max_kv + most - 1) / most), mine = of < 128 ? 128 : of;
             if (mine <= (per_row > kMostTogether ? 1024 : 2048)) {
