@@ -603,8 +603,8 @@ qil_status go(const AttnQuantParams& p, cudaStream_t st) {
     constexpr int kJoin = (kWarps + 1) * 8 * kCols * kDim * 4, kRing = kWarps * FewQ<kDim, kBits>::kWarpBytes, kSmem = kJoin > kRing ? kJoin : kRing;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(attn_few_q_kernel<kDim, kBits, kCols, kTogether>, kSmem, allowed)) return QIL_ERR_CUDA;
-    const int slots = p.a.slots;
-    const unsigned across = !kTogether ? (unsigned)slots : slots <= 2 ? 2u : slots <= 4 ? 4u : (unsigned)kMostTogether;
+    // (a cluster of as many blocks as have work, 2 to 8: one more would hold its place until the others are done)
+    const unsigned across = (unsigned)p.a.slots;
     const dim3 grid(across, (unsigned)p.a.c.num_kv_heads, (unsigned)(p.a.c.num_seqs + p.a.both));
     return launch_early_clusters(attn_few_q_kernel<kDim, kBits, kCols, kTogether>, kTogether ? across : 1u, grid, 32 * kWarps, kSmem, st, p);
 }
