@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_b
     const bool strange = !(high < INFINITY) || !(s < INFINITY), none = s < 1.17549435e-38f;
     if (strange || none) s = 1.f;
     const bool codes = !strange && !none;
-    // (v / s is below 127.5, or 15.1: the scale is rounded by 2^-9 at most; only rint(v / s) + z can be one too large)
+    // (v / s is below 127.5, or 15.1: the scale is rounded by 2^-8 of it at most; only rint(v / s) + z can be one too large)
     const float inv = codes ? __frcp_rn(s) : 0.f;
     float z = 0.f;
     if (kBits == 4 && codes) z = rintf(__fdiv_rn(-low, s));

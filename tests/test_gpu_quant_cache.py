@@ -273,6 +273,27 @@ def test_attention_wide_groups(api, H, Hk, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("B,kv,D", [(55, 257, 64), (37, 385, 128), (28, 513, 64), (22, 700, 64), (18, 769, 128), (15, 1000, 64), (150, 300, 64)])
+def test_attention_blocks_of_a_request(api, B, kv, D, bits):
+    """One to eight blocks to a request and key head, of which shorter requests have no work for some."""
+    q_lens, kv_lens = [1 + (b % 3 == 1) for b in range(B)], [kv] + [2 + (b * 131) % (kv - 1) for b in range(B - 1)]
+    args = quant_attention_inputs(api, gen(1215 + B), q_lens, kv_lens, 6, 3, D, 32, bits)
+    check_quant_attention(api, *args, q_lens, kv_lens)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("D", [128, 64])
+def test_attention_single_tokens_beside_a_prompt(api, D, bits):
+    """Requests of 4, 8, 12 and 16 rows in blocks of their own beside one of 80; the workspace twice."""
+    q_lens, kv_lens = [1, 20, 2, 1, 3, 0, 4, 1], [2300, 2500, 1025, 1024, 1500, 9, 2049, 1]
+    q, cache, table, tab = quant_attention_inputs(api, gen(1216 + D), q_lens, kv_lens, 8, 2, D, 64, bits)
+    ws = api.new_workspace(api.attn_paged_q_workspace_size(sum(q_lens), len(q_lens), 8, 2, D, bits, max(q_lens), max(kv_lens)))
+    first = check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens, workspace=ws)
+    second = check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens, workspace=ws)
+    assert torch.equal(first, second)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("q_std,scale", [(30.0, None), (1.0, 0.0), (1.0, -0.5), (0.01, 1.0)])
 @pytest.mark.parametrize("q_lens,kv_lens", [([1, 1], [700, 65]), ([200], [500])])
 def test_attention_scores_of_every_size(api, q_std, scale, q_lens, kv_lens, bits):
