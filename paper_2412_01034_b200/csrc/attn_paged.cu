@@ -41,13 +41,16 @@ AttnPlan plan_attn(int total_q, int num_seqs, int H, int Hk, int D, int bits, in
         // Blocks over a quantised cache are four to an SM (three with more than 8 rows).  Clusters find no room for the last of so
         // many: they are counted as one block an SM less (24 requests of up to 2000 tokens, 8 key heads, 4 bits: 20.9 -> 17.6 us,
         // 3 of up to 2000, 32 key heads, 8 bits: 20.1 -> 14.5).  Where less than two are left for a row of the cache, rows are
-        // not split up to 2048 tokens (8 requests of up to 1000, 32 key heads: 16.7 -> 14.8).
+        // not split up to 2048 tokens (8 requests of up to 1000, 32 key heads: 16.7 -> 14.8); longer ones are in blocks of 1280
+        // (40 requests of up to 6000, 8 key heads, 4 bits: 55.3 us with 1536, 53.9, 54.4 with 1024, 58.4 with 2048; of seven
+        // other batches six 0.3 to 23 % less than with 2048, one 0.6 % more).
         const long long rows = (long long)max_q * G < kFewRows ? (long long)max_q * G : kFewRows;
         const long long items = (long long)num_seqs * Hk, room = (bits == 16 ? 2 : rows <= 8 ? 4 : 3) * sms;
         const long long per_row = (bits == 16 ? room : room - sms) / items;
         const auto round64 = [](long long n) { return (n + 63) / 64 * 64; };
         long long chunk = round64((max_kv * items + room - 1) / room);
-        chunk = chunk < 384 ? 384 : chunk > 2048 ? 2048 : chunk;
+        const long long longest = bits == 16 ? 2048 : 1280;
+        chunk = chunk < 384 ? 384 : chunk > longest ? longest : chunk;
         if (bits != 16 && per_row < 2 && max_kv <= 2048) chunk = 2048;
         // Beside the kernel for many rows they come up as SMs become free, some beside its blocks and most when those end: a
         // cluster would wait for its last place, and short blocks fill what is left (512-token chunk and 15 single tokens over
