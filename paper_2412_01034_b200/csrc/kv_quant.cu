@@ -9,7 +9,7 @@
 // rounded scale: half a step more range at the most, and the products with it are exact in the kernels that read it.
 //
 // Both kernels are one pass.  Append: a thread turns 8 pairs or takes 16 values, the D / 16 threads of a head find its range by
-// shuffles.  4200 tokens of 32 + 32 + 32 heads of 128: 61.7 us with 8 bits, 68 with 4, where the copy rate would allow 35 and 31: it
+// shuffles.  5466 tokens of 32 + 32 + 32 heads of 128: 61.7 us with 8 bits, 68 with 4, where the copy rate would allow 35 and 31: it
 // waits for instructions, 330 a warp, and for their latency (73 us with a division per code; with 62 registers a thread instead of
 // 40, which six blocks an SM allow, 69).  Read-back: a warp takes up to 512 values of a token's keys and the same of its values;
 // the same tokens 25.6 and 23.7 us, 81 and 73 % of the copy rate.
