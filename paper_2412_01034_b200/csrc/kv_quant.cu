@@ -9,10 +9,10 @@
 // rounded scale: half a step more range at the most, and the products with it are exact in the kernels that read it.
 //
 // Both kernels are one pass.  Append: a thread turns 8 pairs or takes 16 values, the D / 16 threads of a head find its range by
-// shuffles.  5466 tokens of 32 + 32 + 32 heads of 128: 61.7 us with 8 bits, 68 with 4, where the copy rate would allow 35 and 31: it
-// waits for instructions, 330 a warp, and for their latency (73 us with a division per code; with 62 registers a thread instead of
-// 40, which six blocks an SM allow, 69).  Read-back: a warp takes up to 512 values of a token's keys and the same of its values;
-// the same tokens 25.6 and 23.7 us, 81 and 73 % of the copy rate.
+// shuffles.  5466 tokens of 32 + 32 + 32 heads of 128: 57.1 us with 8 bits, 64.5 with 4, where the copy rate would allow 35 and 31: it
+// waits for instructions, about 400 a warp, and for their latency (73 us with a division per code; with 62 registers a thread instead of
+// 40, which six blocks an SM allow, 69; with the page by a division and a choice for every value of a head without codes, 61.7).  Read-back: a warp takes up to 512 values of a token's keys and the same of its values;
+// the same tokens 26.0 and 23.1 us, 79 and 75 % of the copy rate.
 #include "kv_quant.cuh"
 
 namespace qil {
@@ -20,6 +20,8 @@ namespace qil {
 namespace {
 
 constexpr int kThreads = 256;
+
+__device__ __forceinline__ int page_shift(int page_size) { return 31 - __clz(page_size); }   // (a power of two)
 
 // rint(v / s) + 1.5 2^23 by the reciprocal of s, where that decides: v times it is off by 2^-24 of 128 (8e-6) at most, so that the
 // division itself has to be taken only within 2e-5 of a half (`far` collects the distances from whole numbers).
@@ -69,7 +71,7 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_b
     size_t row = 0;   // of the cache: (page, head, slot)
     bool there = head < H;
     if (!there && known) {
-        const int page_at = pos / c.page_size, slot = pos - page_at * c.page_size;
+        const int page_at = pos >> page_shift(c.page_size), slot = pos & (c.page_size - 1);
         const int page = page_at < c.max_pages ? __ldg(c.block_table + (size_t)seq * c.max_pages + page_at) : -1;
         there = page >= 0 && page < c.num_pages;
         row = ((size_t)(there ? page : 0) * Hk + (head - H - (turn ? 0 : Hk))) * c.page_size + slot;
@@ -138,9 +140,9 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_b
     if (kBits == 4 && codes) z = rintf(__fdiv_rn(-low, s));
     float qu[8], qv[8], far = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {   // (no codes: 0 times whatever it is may be a NaN)
-        qu[e] = rounded(codes ? u[e] : 0.f, inv, far);
-        qv[e] = rounded(codes ? v[e] : 0.f, inv, far);
+    for (int e = 0; e < 8; ++e) {   // (0 times an infinity: NaN, which `far` passes over; the words are cleared below)
+        qu[e] = rounded(u[e], inv, far);
+        qv[e] = rounded(v[e], inv, far);
     }
     if (far > 0.49998f) {
 #pragma unroll
@@ -151,7 +153,8 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_b
     }
     if (kBits == 8) {
         unsigned char* dst = static_cast<unsigned char*>(turn ? kvq.k : kvq.v) + row * kDim;
-        const uint2 x = bytes8(qu), y = bytes8(qv);
+        uint2 x = bytes8(qu), y = bytes8(qv);
+        if (!codes) x = y = make_uint2(0u, 0u);
         if (turn) {
             *reinterpret_cast<uint2*>(dst + o) = x;
             *reinterpret_cast<uint2*>(dst + o + kHalf) = y;
@@ -160,11 +163,13 @@ __global__ void __launch_bounds__(kThreads, 6) rope_append_q_kernel(const __nv_b
         }
     } else {
         uint32_t* dst = static_cast<uint32_t*>(turn ? kvq.k : kvq.v) + row * (kDim / 8);
+        uint2 x = make_uint2(nibbles8(qu, z), nibbles8(qv, z));
+        if (!codes) x = make_uint2(0u, 0u);
         if (turn) {
-            dst[o / 8] = nibbles8(qu, z);
-            dst[(o + kHalf) / 8] = nibbles8(qv, z);
+            dst[o / 8] = x.x;
+            dst[(o + kHalf) / 8] = x.y;
         } else {
-            *reinterpret_cast<uint2*>(dst + 2 * o / 8) = make_uint2(nibbles8(qu, z), nibbles8(qv, z));
+            *reinterpret_cast<uint2*>(dst + 2 * o / 8) = x;
         }
     }
     if (o == 0) {
@@ -206,15 +211,16 @@ __global__ void __launch_bounds__(kThreads) kv_read_q_kernel(QuantCache kvq, Pag
                                                              __nv_bfloat16* __restrict__ v_out, int chunks) {
     constexpr int kPer = kDim / 16;
     wait_for_earlier_kernels();
-    const long long at = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    const int Hk = c.num_kv_heads, piece = (int)(at % chunks) * 32 + (threadIdx.x & 31);
-    if (at >= (long long)c.total_q * chunks) return;   // (whole warps)
-    const int t = (int)(at / chunks);
+    // (rows times heads are below 2^31, and so are the warps)
+    const unsigned at = blockIdx.x * (kThreads / 32u) + (threadIdx.x >> 5), row_at = at / (unsigned)chunks;
+    const int Hk = c.num_kv_heads, piece = (int)(at - row_at * chunks) * 32 + (threadIdx.x & 31);
+    if (row_at >= (unsigned)c.total_q) return;   // (whole warps)
+    const int t = (int)row_at;
     int seq = 0, lo = 0, hi = 0, kv = 0;
     const bool held = request_at_row(c.cu_q, c.kv_len, c.num_seqs, c.total_q, t, seq, lo, hi, kv);
     if (!held || t < lo || piece >= Hk * kPer) return;   // (a row of no request stays as it is)
     const int pos = kv - (hi - lo) + (t - lo), head = piece / kPer, o = (piece % kPer) * 16;
-    const int page_at = pos / c.page_size, slot = pos - page_at * c.page_size;
+    const int page_at = pos >> page_shift(c.page_size), slot = pos & (c.page_size - 1);
     const int page = pos >= 0 && page_at < c.max_pages ? __ldg(c.block_table + (size_t)seq * c.max_pages + page_at) : -1;
     const size_t to = ((size_t)t * Hk + head) * kDim + o;
     uint4 kw[2] = {}, vw[2] = {};
