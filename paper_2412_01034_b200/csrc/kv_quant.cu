@@ -9,10 +9,11 @@
 // rounded scale: half a step more range at the most, and the products with it are exact in the kernels that read it.
 //
 // Both kernels are one pass.  Append: a thread turns 8 pairs or takes 16 values, the D / 16 threads of a head find its range by
-// shuffles.  5466 tokens of 32 + 32 + 32 heads of 128: 57.1 us with 8 bits, 64.5 with 4, where the copy rate would allow 35 and 31: it
-// waits for instructions, about 400 a warp, and for their latency (73 us with a division per code; with 62 registers a thread instead of
-// 40, which six blocks an SM allow, 69; with the page by a division and a choice for every value of a head without codes, 61.7).  Read-back: a warp takes up to 512 values of a token's keys and the same of its values;
-// the same tokens 26.0 and 23.1 us, 79 and 75 % of the copy rate.
+// shuffles.  5466 tokens of 32 + 32 + 32 heads of 128: 57.1 us with 8 bits, 64.5 with 4, where the copy rate would allow 35 and 31:
+// it waits for instructions, about 400 a warp, and for their latency (73 us with a division per code; with 62 registers a thread
+// instead of 40, which six blocks an SM allow, 69; with the page by a division and a choice for every value of a head without
+// codes, 61.7).  Read-back: a warp takes up to 512 values of a token's keys and the same of its values; the same tokens 26.0 and
+// 23.1 us, 79 and 75 % of the copy rate.
 #include "kv_quant.cuh"
 
 namespace qil {
