@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             mbar_init(q_ready + 8 * i, 4);      // the group's warps: Q_i in fp16
             mbar_init(raw_full + 8 * i, 1);     // the copy of a tile of codes
             mbar_init(raw_free + 8 * i, 4);     // the decoding warps
-            mbar_init(e_full, 4);               // the decoding warps: exponents of keys and values
         }
+        if (kBits != 16) mbar_init(e_full, 4);  // the decoding warps: exponents of keys and values
         for (int s = 0; s < kStages; ++s) {
             mbar_init(k_full + 8 * s, kBits == 16 ? 1 : 4);   // a copy, or the decoding warps
             mbar_init(v_full + 8 * s, kBits == 16 ? 1 : 4);
