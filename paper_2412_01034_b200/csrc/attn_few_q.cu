@@ -212,7 +212,7 @@ __device__ __forceinline__ void attend(const AttnQuantParams& pq, unsigned char*
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         // (a row of numbers near fp32's smallest counts as zeros; one with an element that is none has no scores)
         const bool whole = most > 1e-30f && most < INFINITY;
-        const float up = whole ? __fdividef(32512.f, most) : 0.f;
+        const float up = whole ? 32512.f / most : 0.f;   // (once a row; the fast division gives zero above 2^126)
         float t = whole ? most * (1.f / 32512.f) : most < INFINITY ? 0.f : INFINITY - INFINITY;
         if (!whole) {   // (0 times an element that is no number)
 #pragma unroll
