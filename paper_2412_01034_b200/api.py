@@ -491,5 +491,6 @@ def lora_batch_add(x, a, b, y, cu_q, adapter, scales, out=None, workspace=None, 
 def sample(logits, u, temperature, top_k=None, top_p=None, min_p=None, out=None, stream=None):
     """One token (int32) per row of logits [B][V] (fp32, bf16 or fp16; rows may be slices of wider ones), from uniform numbers u [B]
     in [0, 1).  temperature [B] (0: the largest logit), top_k [B] int32 (0: off), top_p [B] (1: off) and min_p [B] (0: off) are each
-    row's own; ties go to the lowest index, the token is the first in the vocabulary whose running weight exceeds u of the total."""
+    row's own; ties go to the lowest index, the token is the first in the vocabulary whose running weight exceeds u of the total.
+    A row without a logit above -inf (a NaN counts as -inf) has no token: -1."""
     return _call("sample", stream, logits, u, temperature, top_k, top_p, min_p, out)

@@ -191,7 +191,8 @@ class TokenHead:
         return self.head(x, self.workspace)
 
     def forward(self, h, residual, batch: Requests, u, temperature, top_k=None, top_p=None, min_p=None):
-        """The next tokens, int32 [requests], from uniform numbers u [requests] and the requests' settings (see api.sample)."""
+        """The next tokens, int32 [requests], from uniform numbers u [requests] and the requests' settings (see api.sample).  A request
+        whose logits are all NaN or -inf has none: -1, whatever range the head chooses from."""
         first, end = self.tokens
         chosen = api.sample(self.logits(h, residual, batch)[:, first:end], u, temperature, top_k, top_p, min_p)
-        return chosen + first if first else chosen
+        return torch.where(chosen < 0, chosen, chosen + first) if first else chosen
