@@ -770,7 +770,8 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_ready + 8 * i);
                 ok = mbar_wait(e_full, 0);
-                if (p.scale_log2 != 0.f) scale = ldexpf(scale, exponents[0] + q_exponent);
+                // (at least the smallest normal number: scores that small are all alike, and -inf times zero would be NaN)
+                if (p.scale_log2 != 0.f) scale = fmaxf(ldexpf(scale, exponents[0] + q_exponent), 1.17549435e-38f);
                 value_scale = ldexpf(1.f, exponents[1]);
             }
         }

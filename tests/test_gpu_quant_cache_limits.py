@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from tests.test_gpu_layer_ops import gen
+from tests.test_gpu_layer_ops import gen, ints, starts
 from tests.test_gpu_quant_cache import check_quant_attention, quant_attention_inputs
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +33,15 @@ def test_queries_near_the_largest_number(api, q_lens, kv_lens, most, bits):
     assert torch.isfinite(q).all() and (q.double().abs().amax(dim=2) > most * (1 - 2.0 ** -7)).all()
     cache = scaled(cache, "k_scale", -117)
     check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens, scale=2.0 ** -6)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("q_lens,kv_lens,D", [([1, 5], [300, 129], 128), ([200], [260], 128), ([130, 1], [1000, 70], 64)])
+def test_scores_too_small_for_their_factor(api, q_lens, kv_lens, D, bits):
+    """Keys and queries so small that a score's factor is no number above zero: weights are all the same, as they are with a scale
+    of zero."""
+    q, cache, table, tab = quant_attention_inputs(api, gen(1410), q_lens, kv_lens, 4, 2, D, 32, bits, q_std=1e-13)
+    cache = scaled(cache, "k_scale", -110)
+    args = (ints(starts(q_lens)), ints(kv_lens), table, max(q_lens), max(kv_lens))
+    assert torch.equal(api.attn_paged_q(q, cache, *args), api.attn_paged_q(q, cache, *args, scale=0.0))
+    check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens)
