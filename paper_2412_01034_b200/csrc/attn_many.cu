@@ -889,7 +889,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
             // group's query tile (8 KB a time, pieces permuted by the row; the tile has been read, the last S is long there)
             // and writes 16 bytes a lane, whole rows at once.
             const bool whole = p.splits == 1;
-            const float inv = value_scale / sum;
+            const float inv = 1.f / sum;   // (value_scale, a power of two, is applied apart: over a sum it may be too small a number)
             const size_t items = (size_t)p.c.total_q * H;
             const int item = live ? (q_lo + token0 + i * p.tile_tokens + token) * H + kvh * G + (r - token * G) : 0;   // this thread's (token, head)
             unsigned char* turn = smem + i * kTileBytes + (warp & 3) * (32 * kDim * 2);
@@ -923,7 +923,7 @@ __global__ void __launch_bounds__(kThreadsOf<kBits>, 1) attn_many_kernel(const _
                         for (int e = 0; e < 16; e += 8) {
                             float f[8];
 #pragma unroll
-                            for (int x = 0; x < 8; ++x) f[x] = sum == 0.f ? 0.f : __uint_as_float(o[e + x]) * inv;
+                            for (int x = 0; x < 8; ++x) f[x] = sum == 0.f ? 0.f : __uint_as_float(o[e + x]) * inv * value_scale;
                             const int at = (c + e) / 8;
                             *reinterpret_cast<uint4*>(turn + lane * (kUnit * 16) + ((at & ~7) | ((at ^ lane) & 7)) * 16) = pack8(f);
                         }

@@ -1,8 +1,9 @@
 """Attention over the quantised cache near the ends of fp32's range."""
+import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_layer_ops import gen, ints, starts
+from tests.test_gpu_layer_ops import f64, gen, ints, starts
 from tests.test_gpu_quant_cache import check_quant_attention, quant_attention_inputs
 
 pytestmark = pytest.mark.gpu
@@ -45,3 +46,21 @@ def test_scores_too_small_for_their_factor(api, q_lens, kv_lens, D, bits):
     args = (ints(starts(q_lens)), ints(kv_lens), table, max(q_lens), max(kv_lens))
     assert torch.equal(api.attn_paged_q(q, cache, *args), api.attn_paged_q(q, cache, *args, scale=0.0))
     check_quant_attention(api, q, cache, table, tab, q_lens, kv_lens)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("q_lens,kv_lens,D", [([200], [500], 128), ([60, 40], [510, 333], 64), ([200], [700], 128), ([60, 40], [3000, 2500], 64)])
+def test_values_near_the_smallest_number(api, q_lens, kv_lens, D, bits):
+    """Of prompts, in one part of the cache and in several: values by a power of two smaller give results by that power smaller, up
+    to bf16's own smallest step."""
+    q, cache, table, _ = quant_attention_inputs(api, gen(1420), q_lens, kv_lens, 2, 2, D, 64, bits, q_std=0.1)
+    args = (ints(starts(q_lens)), ints(kv_lens), table, max(q_lens), max(kv_lens))
+    if bits == 8:   # values of one sign: results of their size
+        cache.v.clamp_(min=0)
+    else:
+        cache.v_scale[..., 1] = 0
+    power = 119 if bits == 8 else 122   # (scales of 2^-126 to 2^-124)
+    want = api.attn_paged_q(q, cache, *args)
+    got = api.attn_paged_q(q, scaled(cache, "v_scale", -power), *args)
+    # results below 2^-126 are whole numbers of 2^-133: each is off by half of one, and the two roundings by one together
+    assert np.abs(f64(got) * 2.0 ** power - f64(want)).max() <= 2.0 ** (power - 133)
