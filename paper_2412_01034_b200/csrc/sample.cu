@@ -28,7 +28,7 @@ typedef unsigned long long u64;
 
 constexpr int kMostThreads = 512, kBuckets = 1024, kCap = 1024, kMostBlocks = 8;
 constexpr double kOne = 4398046511104.0;   // 2^42
-constexpr double kDeepest = 29.8;          // exp(-29.8) 2^42 = 0.504: the last weight that is not zero
+constexpr double kDeepest = 29.81;         // beyond 43 log(2) = 29.8053, below which a weight rounds to zero (this far 2^y still has y > -43.5)
 constexpr int kRanked = 512;               // lists of up to so many are put in order by counting
 static_assert(QIL_SAMPLE_MAX_VOCAB <= 1 << 18, "an index has 18 bits beside a weight's 43");
 
