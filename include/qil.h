@@ -455,7 +455,7 @@ qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, v
  * cached tokens 0 ... p of its request:
  *     out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,   k_j, v_j of key head h / (num_heads / num_kv_heads)
  *   A token that sees nothing (kv_len < q_len) gets zeros.  q, out [total_q][num_heads][head_dim], which must not overlap.
- *   The weights exp(score - maximum) enter the product with v as bf16, the type of v (2^-9 of each weight at most), and their
+ *   The weights exp(score - maximum) enter the product with v as bf16, the type of v (2^-8 of each weight at most), and their
  *   sum in fp32: on normal data an output is off by 0.0019 to 0.0023 of its size (root mean square), 0.0017 of which are its
  *   own rounding to bf16.
  *   What lies in the caches behind the tokens that a token sees, be it infinite or NaN, has no influence on it.
@@ -507,12 +507,19 @@ qil_status qil_kv_read_q(const void* k_codes, const void* v_codes, const void* k
                          qil_stream_t stream);
 
 /* qil_attn_paged_q: qil_attn_paged over such a cache (arguments, bounds and workspace as there, with a size of its own; the
- *   two may take turns on one workspace that is large enough for either).  Of a request with at most 16 query rows (new tokens x
- *   query heads of a key head) the scores take codes as they are and a query row in 16 bits (off by 2^-16 of its largest element),
- *   and a weight times its value's scale is rounded to bf16: outputs are off by 0.0023 of their size.  Of one with more, values
- *   (q - z) s, queries and weights enter the products as fp16, over powers of two of the largest of them (2^-11 of each; a value
- *   whose scale is below 2^-22 of the request's largest, and a weight below 2^-14 of the largest, have fewer bits): 0.0017.  Query
- *   rows of the first kind whose largest element is below 1e-30 count as zeros.
+ *   two may take turns on one workspace that is large enough for either).  What is rounded on the way to the results' bf16
+ *   (which costs 0.0017 of their size, root mean square):
+ *   Requests with at most 16 query rows (new tokens x query heads of a key head): a query row is held in steps of 2^-15 of its
+ *   largest element, so that its small elements have fewer bits than came in, and a score is off by 2^-16 max |q| sum_d |k_d|
+ *   |scale| at most.  A weight times its value's scale is rounded to bf16, 2^-8 of it at most.  Outputs are off by 0.0017 (few
+ *   weights that count) to 0.0023 of their size, and by no more where a few channels are 300 times as large as the others.  Rows
+ *   whose largest element is below 1e-30 count as zeros; values whose scale is below 2^-108 have fewer bits.
+ *   Requests with more: queries, weights and the values (q - z) s of keys and values enter the products as fp16, over powers of
+ *   two of the largest of them: 2^-11 of each at most.  For keys this makes a score off by 2^-11 sum_d |q_d k_d| |scale| at most,
+ *   so that the error grows with the scores: at head_dim 128 outputs are off by 0.0017 of their size with queries and keys of
+ *   unit size, by 0.0019 with queries 8 times as large, 0.0020 with 16 times and 0.0023 with 30 times, and the worst rows (two
+ *   tokens that share the weight) by 0.5, 0.9 and 1.3 % of theirs.  A key or value whose scale is below 2^-22 of the request's
+ *   largest, and a weight below 2^-14 of the largest, have fewer bits.
  *   A head that reads as NaN makes the results of the tokens that see it NaN and has no influence on others.
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE, CUDA. */
 size_t qil_attn_paged_q_workspace_size(int total_q, int num_seqs, int num_heads, int num_kv_heads, int head_dim, int bits,

@@ -33,7 +33,8 @@
 // is the copies of all blocks starting at once).
 //
 // A cache of 8 or 4-bit codes (kBits): the same products in fp16, which holds what 8 or 4 bits and a scale of 8 give to 2^-11
-// where bf16 would give 2^-9 (0.0034 of an output's size instead of 0.0017), at the same rate.  So that fp16's range holds them
+// where bf16 would give 2^-8 (0.0034 of an output's size instead of 0.0017 with scores of ordinary size; a key's rounding grows with
+// the scores, and with queries 30 times as large it is 0.0023), at the same rate.  So that fp16's range holds them
 // the values are divided by a power of two of the largest scale that the block's tokens have, and a query row by one of its
 // largest element; the products' results are multiplied back with the scores' factor and at the end.
 //   A fourth group of 128 threads decodes: thread t takes token t of a tile, a key's codes to a tile of K and a value's to one of
