@@ -21,8 +21,8 @@
 // Codes are finite whatever they are, so nothing behind a request's last token can reach a result: its weight is replaced by
 // zero after its scale has been applied.
 //
-// Measured (one B200): 8 bits, 32 requests of up to 4099 tokens, 32 key heads of 128 (0.70 GB): 118 to 126 us, 85 to 91 % of the
-// copy rate.  4 bits, 48 requests of up to 9001 tokens, 8 key heads (0.28 GB): 80 us, 54 %: 360 warp instructions a tile of 16
+// Measured (one B200): 8 bits, 32 requests of up to 4099 tokens, 32 key heads of 128 (0.70 GB): 117 to 132 us, 81 to 91 % of the
+// copy rate.  4 bits, 48 requests of up to 9001 tokens, 8 key heads (0.28 GB): 79 to 81 us, 54 %: 360 warp instructions a tile of 16
 // tokens, 167 of them on the integer pipe, which would take 41 us alone; the rest is latency and blocks of unequal length (the
 // SMs are busy for 81 % of the time on average).  Tried and slower: blocks of 1, 2 and 8 warps (171, 95, 85 us), blocks of 768, 512 or
 // 384 tokens (83, 92, 101 us: a block's start and join cost 5 us), shifts as multiplications (100 us).  Batches of middling size

@@ -42,9 +42,11 @@
 //   ring that bulk copies fill, shorter ones straight from memory into registers one step ahead (a row is at most one line, so
 //   nothing is read twice; staging them costs 8 % more).  Its registers come from the producing warps (setmaxnreg).
 //   Codes mean finite values: nothing is cleared behind the last token, and a NaN scale there is replaced.
-// Measured, 4096 new tokens over 8192, 32 heads of 128, 8 bits: 490 to 530 us (780 to 840 TFLOP/s) against 372 to 410 for bf16
-// pages in the same minutes.  The products' thread is the longest path of a step, 3600 of 4300 cycles: the decoded tiles' stores
-// meet the products' reads of shared memory.  Tried and slower: 128-byte rows without the ring (730 us).
+// Measured, 4096 new tokens over 8192, 32 heads of 128: 8 bits 474 to 536 us (770 to 870 TFLOP/s), 4 bits 512 to 560, against 365
+// to 410 for bf16 pages in the same minutes.  Every block decodes all tiles of its key head that its rows see, so that 16 blocks
+// decode the same ones here.  The products' thread is the longest path of a step, 3600 of 4300 cycles: the decoded tiles' stores
+// meet the products' reads of shared memory.  Tried and slower: 128-byte rows without the ring (730 us).  At 128 registers a
+// thread at launch the instances spill 16 bytes (8 bits, D = 128) to 102 (8 bits, D = 64); those for bf16 pages 32.
 #include <cuda.h>
 
 #include <mutex>

@@ -12,7 +12,9 @@
 // shuffles.  5466 tokens of 32 + 32 + 32 heads of 128: 57.1 us with 8 bits, 64.5 with 4, where the copy rate would allow 35 and 31:
 // it waits for instructions, about 400 a warp, and for their latency (73 us with a division per code; with 62 registers a thread
 // instead of 40, which six blocks an SM allow, 69; with the page by a division and a choice for every value of a head without
-// codes, 61.7).  Read-back: a warp takes up to 512 values of a token's keys and the same of its values; the same tokens 26.0 and
+// codes, 61.7).  They are the definition's separate roundings, and what every thread does for its one head: the request and the
+// page, 64 bytes of cosines and sines for 32 bytes of a turned head, and the 52 (4 bits: 76) bytes that 40 registers do not hold.
+// Read-back: a warp takes up to 512 values of a token's keys and the same of its values; the same tokens 26.0 and
 // 23.1 us, 79 and 75 % of the copy rate.
 #include "kv_quant.cuh"
 

@@ -11,9 +11,10 @@
 // counts) gives the step in which the k-th value, or the p-th part of the weight, lies; what lies in it and above, mostly a
 // few dozen values, is gathered in one block and finished there by sorting.  Where more than 1024 values remain the step alone
 // is gathered (or cut again), which gives the last kept value, and a pass over the row sums and selects.
-// Latency bound: every step of a row is a trip between its blocks (about 0.6 us).  Measured: one row of 32 000 (bf16, top-k
-// and top-p) 12 us, 64 such rows 21 us; 64 rows of 128 003 (fp32, two rounds of blocks) greedy 16 us, top-k and top-p 60 us,
-// settings of every kind 101 us.
+// Latency bound: every step of a row is a trip between its blocks (about 0.6 us), and the last pass over a row that does not end
+// in the list has one warp that looks for the token in its share again.  Measured: one row of 32 000 (bf16, top-k and top-p) 12 to
+// 13 us, 64 such rows 21 us; 64 rows of 128 003 (fp32, two rounds of blocks) greedy 14 to 16 us, top-k and top-p 58 to 60 us,
+// settings of every kind 94 to 112 us, by the settings.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -727,8 +728,9 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) sample_kernel(const 
 
 qil_status launch_sample(const void* logits, qil_dtype type, long long ld, const float* u, const float* temperature, const int* top_k,
                          const float* top_p, const float* min_p, int* out, int B, int V, cudaStream_t st) {
-    // Blocks of a row: of 4096 logits or more, eight at most; fewer where the rows alone fill the GPU twice over, as long as two
-    // blocks fit an SM's shared memory (64 rows of 32 000: 39 us with eight, 22 us with four).
+    // Blocks of a row: of 4096 logits or more, eight at most (one row of 32 000, top-k and top-p: 12.3 us with eight, 14.7 with four,
+    // 20.0 with two, 25.2 with one, of 512 threads each); fewer where the rows alone fill the GPU twice over, as long as two
+    // blocks fit an SM's shared memory (64 rows of 32 000: 30.6 us with eight, 21.2 with four, of 256 threads each).
     unsigned blocks = 1;
     while (blocks < (unsigned)kMostBlocks && V > 4096 * (int)blocks) blocks *= 2;
     const auto part_of = [&](unsigned n) { return ((V + (int)n - 1) / (int)n + 7) & ~7; };
@@ -742,8 +744,8 @@ qil_status launch_sample(const void* logits, qil_dtype type, long long ld, const
     };
     auto of = [&](auto* x) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
-        // 512 threads where every block has an SM (one row of 32 000: 16.0 us, with 256 17.4), else 256, two blocks an SM (64 rows of
-        // 32 000: 79 and 39 us)
+        // 512 threads where every block has an SM (one row of 32 000: 12.3 us, with 256 13.0), else 256, two blocks an SM (64 rows of
+        // 32 000, four blocks each: 29.5 us with 512, 21.2 with 256; 64 of 128 003, eight each, settings of every kind: 105 and 94)
         static std::atomic<unsigned long long> a{0}, b{0}, c{0}, d{0};
         if ((long long)B * blocks <= num_sms())
             return blocks == 1 ? go(sample_kernel<T, 512, false>, 512, x, a) : go(sample_kernel<T, 512, true>, 512, x, b);

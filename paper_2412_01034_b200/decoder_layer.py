@@ -66,7 +66,8 @@ def linear_workspace_size(max_tokens, linears, gate_up, linears8=()):
 class DecoderLayer:
     """weights: fp32 CUDA tensors norm1, norm2 [hidden], qkv [(H + 2 Hk) D][hidden], o [hidden][H D], gate, up [ffn][hidden],
     down [hidden][ffn].  adapters: None or (a [n][r][hidden], b [n][(H + 2 Hk) D][r], scales [n]) beside the qkv projection.
-    kv_bits: 16 (bf16 cache: k_cache, v_cache), 8 or 4 (quantised cache: cache).
+    kv_bits: 16 (bf16 cache: k_cache, v_cache), 8 or 4 (quantised cache: cache).  A quantised cache is a half or a quarter of the size and
+    makes the attention of single tokens over long contexts 1.6 to 2 times as fast; that of prompts takes up to 1.45 times as long.
     The caches and workspaces are the layer's own: its calls belong on one stream, or have to be ordered by the caller.
     Steps may be captured in CUDA graphs."""
 
