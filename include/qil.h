@@ -459,6 +459,8 @@ qil_status qil_rope_append(const void* qkv, const float* cos_sin, void* q_out, v
  *   sum in fp32: on normal data an output is off by 0.0019 to 0.0023 of its size (root mean square), 0.0017 of which are its
  *   own rounding to bf16.
  *   What lies in the caches behind the tokens that a token sees, be it infinite or NaN, has no influence on it.
+ *   Weights times values are summed before they are divided by the weights' sum, with weights of up to 2^8: values above
+ *   2^120 / kv_len may give infinite results.
  *   max_q_len, max_kv_len: bounds on the requests' q_len and kv_len that the host knows.  They choose how the work is
  *   split; a request that exceeds them gets unspecified results, the others keep theirs.
  *   workspace: qil_attn_paged_workspace_size() bytes, the first QIL_ATTN_PAGED_ZEROED_BYTES of them zero-filled once (status

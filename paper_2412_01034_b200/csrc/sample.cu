@@ -14,7 +14,7 @@
 // Latency bound: every step of a row is a trip between its blocks (about 0.6 us), and the last pass over a row that does not end
 // in the list has one warp that looks for the token in its share again.  Measured: one row of 32 000 (bf16, top-k and top-p) 12 to
 // 13 us, 64 such rows 21 us; 64 rows of 128 003 (fp32, two rounds of blocks) greedy 14 to 16 us, top-k and top-p 58 to 60 us,
-// settings of every kind 94 to 112 us, by the settings.
+// settings of every kind 94 to 114 us, by the settings.
 #include <cuda_fp16.h>
 
 #include <type_traits>
